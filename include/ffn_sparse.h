@@ -148,7 +148,9 @@ int ffn_lopa_dense_forward(ffn_dtype_t wdt, int T, int d, int d_ff, int r, const
  * the two values; silu_up or rms_norm not 0 or 1; exactly one of g_idx, g_sign NULL; G or
  * the norm with standard gating; rms_norm with an invalid rms_eps; rms_gain without
  * rms_norm. */
-typedef enum { FFN_ACT_RELU = 0, FFN_ACT_RSPLUS = 1 } ffn_act_t;
+/* FFN_ACT_SILU, u sigma(u) of u = h - t on both sides of zero, is for the calls of ffn_gated.h
+ * only: it has no zeros to skip, and the calls here refuse it (FFN_ERR_OPTION). */
+typedef enum { FFN_ACT_RELU = 0, FFN_ACT_RSPLUS = 1, FFN_ACT_SILU = 2 } ffn_act_t;
 
 typedef struct {
   ffn_act_t act;

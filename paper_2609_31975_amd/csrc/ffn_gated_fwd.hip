@@ -1,0 +1,70 @@
+// The hidden layer of the gated block: both projections, the activation and their product in one
+// kernel, z = A(x W1^T - t) U(x W3^T).
+#include "ffn_gemm_host.h"
+
+namespace ffn {
+namespace {
+
+template <class E>
+struct EpiGated {
+  BlockForm form;
+  int d_ff, ldf;
+  typename E::T* z;
+  float *g, *v;  // or null
+
+  __device__ __forceinline__ void select(GemmArgs&) const {}
+  __device__ __forceinline__ void put(const GemmArgs&, int, int, int, f32x4_t) const {}
+  __device__ __forceinline__ void pair(int m, int n, f32x4_t h, f32x4_t u) const {
+    if (n >= ldf) return;
+    const size_t at = (size_t)m * ldf + n;
+    f32x4_t gg, zz;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      gg[i] = h[i] - form.t;
+      zz[i] = n + i < d_ff ? block_act(form.act, gg[i]) * up_value(form.silu_up, u[i]) : 0.f;
+    }
+    store4<E>(z + at, zz);
+    if (g) {
+      *reinterpret_cast<f32x4_t*>(g + at) = gg;
+      *reinterpret_cast<f32x4_t*>(v + at) = u;
+    }
+  }
+};
+
+template <class E, class C>
+hipError_t run(const GemmArgs& a, const EpiGated<E>& epi, hipStream_t st) {
+  return a.lr.ids ? launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st)
+                  : launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
+}
+
+template <class E>
+hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const void* w_up, const BlockForm& form,
+                  const AdapterSet& ad, const void* const v2[2], const void* const b2[2], void* z, float* g, float* v,
+                  hipStream_t st) {
+  GemmArgs a{};
+  a.a = Operand{{x, nullptr}, s.dp, s.T};
+  a.b = Operand{{w_gate, w_up}, s.dp, s.d_ff};
+  a.M = s.T;
+  a.N = s.d_ff;
+  a.K = s.d;
+  a.products = 1;
+  a.splits = 1;
+  if (ad.ids) a.lr = low_rank(ad, v2, b2, s.d_ff);
+  const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
+  if (s.T <= 16) return run<E, TileT16>(a, epi, st);
+  if (s.T <= 64) return run<E, TileT64>(a, epi, st);
+  if constexpr (E::EPC == 8)
+    if (ceil_div(s.T, 256) * ceil_div(s.d_ff, 128) >= 2 * kCUs) return run<E, TileT256>(a, epi, st);
+  return run<E, TileT128>(a, epi, st);
+}
+
+}  // namespace
+
+hipError_t launch_block_hidden(bool f32, const BlockShape& s, const void* x, const void* w_gate, const void* w_up,
+                               const BlockForm& form, const AdapterSet& ad, const void* const v2[2],
+                               const void* const b2[2], void* z, float* g, float* v, hipStream_t st) {
+  return f32 ? hidden<EF32>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, st)
+             : hidden<EBf16>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, st);
+}
+
+}  // namespace ffn

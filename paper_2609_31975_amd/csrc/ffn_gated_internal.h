@@ -1,0 +1,61 @@
+// Internal declarations of the gated block's and the adapters' launches.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace ffn {
+
+constexpr int kCUs = 256;
+
+// Gate activation, threshold and the up side of one call.
+struct BlockForm {
+  int act, silu_up;
+  float t;
+};
+
+// Adapters of one product (internal form): ids, stack sizes, and the v rows computed for them.
+struct AdapterSet {
+  int n = 0, r = 0, rp = 0;
+  const int32_t* ids = nullptr;
+  const float* scale = nullptr;
+};
+
+// Shapes: rows of dp elements (d rounded up to whole chunks), hidden rows of ldf (d_ff rounded up to 64).
+struct BlockShape {
+  int T, d, d_ff, dp, ldf;
+};
+
+// z = A(x W1^T - t) U(x W3^T), and g, v in fp32 when g is not null.  v2: A_j x of the two projections'
+// adapters (null: none), b2 their B stacks.
+hipError_t launch_block_hidden(bool f32, const BlockShape& s, const void* x, const void* w_gate, const void* w_up,
+                               const BlockForm& form, const AdapterSet& ad, const void* const v2[2],
+                               const void* const b2[2], void* z, float* g, float* v, hipStream_t st);
+// out [T][n] = z W (W [k][n], k strided) with adapters (b null: none), or the sum of two such products.
+struct TokenProduct {
+  const void* a[2];  // [T][lda]
+  const void* b[2];  // KS: [k][ldb]; KC: [n][ldb]
+  int products, T, n, k, lda, ldb, ldo;
+  void* out;
+  float* part;  // splits x T x round_up(n, 4) fp32 where token_splits(...) > 1
+  AdapterSet ad;
+  const void* v;
+  const void* ab;
+};
+int token_splits(bool f32, int T, int n, int steps);
+hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st);
+hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t st);
+// dg, dv [T][ldf] from dz = dy W2 and the saved g, v.
+hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const void* w_down_t, const BlockForm& form,
+                           const float* g, const float* v, void* dg, void* dv, hipStream_t st);
+// up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
+hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
+                           void* const out[3], hipStream_t st);
+// v[i] [T][rp] = scale_j A_j x for up to two stacks
+hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
+                            const void* const a[2], void* const v[2], hipStream_t st);
+// rows of n elements to rows of np, the rest zero
+hipError_t launch_pad_rows(bool f32, int64_t rows, int n, int np, const void* src, void* dst, hipStream_t st);
+
+}  // namespace ffn

@@ -1,0 +1,479 @@
+// The tiled matrix product behind the gated block, its backward pass and the adapters (gfx950).
+// Not part of the public ABI.
+//
+//   acc[m][n] = sum over k of A(m, k) B(n, k)
+//
+// Either operand lies in memory with k contiguous ([rows][k]: "KC") or strided ([k][rows]: "KS"),
+// so the forward products (x W^T: KC, KC; z W2t: KC, KS), the token gradient (dg W1: KC, KS) and
+// the weight gradients (dg^T x: KS, KS) are one kernel.  A workgroup owns a BM x BN tile of the
+// result and walks k in steps of 128 bytes (64 bf16, 32 fp32).  Both tiles of a step go from memory
+// into LDS without passing through registers (buffer_load ... lds, 16 bytes a lane), S steps deep:
+// the loads of step i + S - 1 are in flight while step i is multiplied, and the only waits of a step
+// are for its own loads and for the workgroup to have left the buffer that is loaded next.
+//
+// LDS images.  A load writes 64 consecutive 16-byte chunks, so a swizzle can only choose which chunk
+// of memory a lane fetches:
+//   KC  row r holds its 8 chunks of the step, chunk c in place c ^ (r & 7): the 8 rows that a fragment
+//       read touches at once then cover all banks.
+//   KS  row k holds the tile's columns; for bf16 the 32-byte pieces are exchanged by k & 3 and bit 3
+//       of k, and fragments are read with the transposing LDS read (ds_read_b64_tr_b16), whose 16 lanes
+//       cover 4 rows k; for fp32 the 64-byte pieces are exchanged by bits 2..3 of k and read by element.
+// Rows, columns and k beyond the operand are fetched from a buffer offset past its end, which reads
+// as zero: tails need no other code.
+//
+// The products run as mfma(B fragment, A fragment), which leaves a lane with four consecutive n of one
+// m, what a row-major store wants.  Sums are fp32 throughout.
+#pragma once
+
+#include "ffn_mfma.h"
+
+namespace ffn {
+namespace {
+
+struct EBf16 {
+  typedef __bf16 T;
+  static constexpr int EPC = 8;  // elements of a 16-byte chunk
+};
+struct EF32 {
+  typedef float T;
+  static constexpr int EPC = 4;
+};
+template <class E>
+constexpr int esz() {
+  return 16 / E::EPC;
+}
+template <class E>
+constexpr int step_k() {  // k of one step: 128 bytes of a KC row
+  return 8 * E::EPC;
+}
+
+// One operand: p[0], and p[1] for a second one of the same layout (the other factor of a sum of two
+// products, or W_up beside W_gate).  rows: the extent that is not k; a KS operand's rows are whole
+// chunks (its memory is padded to them).
+struct Operand {
+  const void* p[2];
+  int64_t ld;
+  int rows;
+};
+
+// Adapters of a product (see ffn_adapter.h for v): B_j of adapter j is b + j out r, [out][r], and
+// token m adds sum over k of v[m][k] B_ids[m][n][k].  rp: r in whole chunks, the row length of v.
+struct LowRank {
+  const void* v[2];
+  const void* b[2];
+  const int32_t* ids;
+  int n, r, rp, out;
+};
+
+struct GemmArgs {
+  Operand a, b;
+  int M, N;      // of the result (N neurons for a dual product)
+  int K;         // of one product
+  int products;  // 1, or 2: the sum over p[0] and p[1] of both operands
+  int ntm, ntn;
+  int splits;    // shares of the steps, one workgroup each
+  LowRank lr;
+};
+
+template <int BM_, int BN_, int WM_, int WN_, int S_>
+struct Config {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, S = S_;
+  static constexpr int NW = WM * WN, threads = NW * kWave;
+  static constexpr int WTM = BM / WM, WTN = BN / WN, MT = WTM / 16, NT = WTN / 16;
+  static constexpr int stage = (BM + BN) * 128;
+};
+
+enum class Lay { KC, KS };
+
+__device__ __forceinline__ void lds_load16(const Buf& b, char* dst, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b.r, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
+}
+
+// Waits until at most n of this wave's loads are in flight and its LDS reads have returned.
+template <int n>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | ((n >> 4) << 14));
+}
+// All waves of the workgroup; nothing of one side is moved to the other.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ------------------------------------------------------------------ memory to LDS
+// A tile of ROWS (not-k) x one step, loaded by NW waves: instruction j of ROWS / 8 fills the chunks
+// 64 j .. 64 j + 63; a wave takes every NW-th (where there are fewer than waves, some load the same
+// chunks: the wait counts of all waves are then equal).
+template <class E, Lay L, int ROWS, int NW>
+struct Loader {
+  static constexpr int CPR = ROWS / E::EPC;  // KS: chunks of a row k
+  static constexpr int total = ROWS / 8, per = (total + NW - 1) / NW;
+  static_assert(total % NW == 0 || NW % total == 0, "loads divide over the waves");
+  uint32_t off[per];  // byte offset from the step's base, kOOB outside the operand
+  int kpos[per];      // first k of the chunk within the step
+
+  __device__ __forceinline__ static int instr(int i, int wave) { return (i * NW + wave) % total; }
+  // KS: the swizzle of row k, in chunks
+  __device__ __forceinline__ static int swz(int k) {
+    if constexpr (E::EPC == 8) return ((k & 3) | (CPR >= 16 ? ((k >> 3) & 1) << 2 : 0)) << 1;
+    else return ((k >> 2) & 3) << 2;
+  }
+  // row(r): the operand's row that LDS row r holds, or -1
+  template <class RowOf>
+  __device__ __forceinline__ void init(int64_t ld, int rows, int r0, RowOf row) {
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+      const int j = instr(i, wave);
+      if constexpr (L == Lay::KC) {
+        const int c = (lane & 7) ^ (lane >> 3), rr = row(j * 8 + (lane >> 3));
+        kpos[i] = c * E::EPC;
+        off[i] = rr >= 0 && rr + r0 < rows ? (uint32_t)rr * (uint32_t)(ld * esz<E>()) + c * 16 : kOOB;
+      } else {
+        const int s = j * kWave + lane, k = s / CPR, c = (s % CPR) ^ swz(k);
+        kpos[i] = k;
+        off[i] = r0 + c * E::EPC < rows ? (uint32_t)k * (uint32_t)(ld * esz<E>()) + c * 16 : kOOB;
+      }
+    }
+  }
+  // one step from `base` (its first k), k_left of k left
+  __device__ __forceinline__ void issue(const char* base, int k_left, char* dst) const {
+    issue(k_left, dst, [base](int) { return base; });
+  }
+  // base(j): where the rows of instruction j lie
+  template <class Base>
+  __device__ __forceinline__ void issue(int k_left, char* dst, Base base) const {
+    const int wave = uniform(threadIdx.x / kWave);
+    if (k_left >= step_k<E>()) {
+#pragma unroll
+      for (int i = 0; i < per; ++i) {
+        const int j = instr(i, wave);
+        lds_load16(make_buf(base(j), 0x7fffffffu), dst + j * 1024, off[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < per; ++i) {
+        const int j = instr(i, wave);
+        lds_load16(make_buf(base(j), 0x7fffffffu), dst + j * 1024, kpos[i] < k_left ? off[i] : kOOB);
+      }
+    }
+  }
+  // bytes from one step to the next
+  __device__ __forceinline__ static int64_t stride(int64_t ld) {
+    return L == Lay::KC ? 128 : (int64_t)step_k<E>() * ld * esz<E>();
+  }
+};
+
+// ------------------------------------------------------------------ LDS to fragments
+// Fragment of half kk (0, 1) of a step for the 16 rows from tile row r: lane l holds row r + l % 16 and
+// chunk l / 16 of the half (bf16: k = 8 (l / 16) .. + 7; fp32: component j is k = 4 (l / 16) + j).
+template <class E, Lay L, int ROWS, int TILES>
+struct Reader {
+  typedef Loader<E, L, ROWS, 1> Ld;
+  static constexpr int CPR = Ld::CPR;
+  int off[L == Lay::KC ? 2 : TILES];
+
+  __device__ __forceinline__ explicit Reader(int row0) {
+    const int lane = lane_id();
+    if constexpr (L == Lay::KC) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        off[kk] = (row0 + (lane & 15)) * 128 + (((kk * 4 + (lane >> 4)) ^ (lane & 7)) << 4);
+    } else {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        if constexpr (E::EPC == 8) {
+          const int k = 8 * (lane >> 4) + ((lane >> 2) & 3), c = (row0 + t * 16) / 8 + ((lane >> 1) & 1);
+          off[t] = k * CPR * 16 + ((c ^ Ld::swz(k)) << 4) + (lane & 1) * 8;
+        } else {
+          const int k = 4 * (lane >> 4), c = (row0 + t * 16) / 4 + ((lane >> 2) & 3);
+          off[t] = k * CPR * 16 + ((c ^ Ld::swz(k)) << 4) + (lane & 3) * 4;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ uint4 get(const char* s, int kk, int t) const {
+    if constexpr (L == Lay::KC) {
+      return *reinterpret_cast<const uint4*>(s + off[kk] + t * 2048);
+    } else if constexpr (E::EPC == 8) {
+      const char* p = s + off[t] + kk * 32 * CPR * 16;
+      const uint2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * CPR * 16);
+      return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    } else {
+      const char* p = s + off[t] + kk * 16 * CPR * 16;
+      return make_uint4(*reinterpret_cast<const uint32_t*>(p), *reinterpret_cast<const uint32_t*>(p + CPR * 16),
+                        *reinterpret_cast<const uint32_t*>(p + 2 * CPR * 16),
+                        *reinterpret_cast<const uint32_t*>(p + 3 * CPR * 16));
+    }
+  }
+};
+
+template <class E>
+__device__ __forceinline__ f32x4_t product(const uint4& b, const uint4& a, f32x4_t c) {
+  if constexpr (E::EPC == 8) {
+    return mfma16(bf8(b), bf8(a), c);
+  } else {
+    c = mfma16f(comp<0>(b), comp<0>(a), c);
+    c = mfma16f(comp<1>(b), comp<1>(a), c);
+    c = mfma16f(comp<2>(b), comp<2>(a), c);
+    return mfma16f(comp<3>(b), comp<3>(a), c);
+  }
+}
+
+template <class E, class C, Lay LA, Lay LB>
+__device__ __forceinline__ void multiply(const char* sa, const char* sb, const Reader<E, LA, C::BM, C::MT>& ra,
+                                         const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT]) {
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    uint4 a[C::MT], b[C::NT];
+#pragma unroll
+    for (int i = 0; i < C::NT; ++i) b[i] = rb.get(sb, kk, i);
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i) a[i] = ra.get(sa, kk, i);
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
+  }
+}
+
+// ------------------------------------------------------------------ activations
+// A(g), and with its derivative; the same of the up side.  A gate value that is not above zero (NaN
+// too) gives zero and slope zero, but for SiLU.
+__device__ __forceinline__ float block_act(int act, float g) {
+  if (act == 0) return g > 0.f ? g : 0.f;
+  const float a = g / (1.f + expf(-g));
+  return act == 2 || g > 0.f ? a : 0.f;
+}
+__device__ __forceinline__ void silu_grad(float g, float& a, float& da) {
+  const float s = 1.f / (1.f + expf(-g));
+  a = g * s;
+  da = s * (1.f + g * (1.f - s));
+}
+__device__ __forceinline__ void block_act_grad(int act, float g, float& a, float& da) {
+  const bool on = act == 2 || g > 0.f;
+  float sa, sd;
+  if (act == 0) {
+    sa = g;
+    sd = 1.f;
+  } else {
+    silu_grad(g, sa, sd);
+  }
+  a = on ? sa : 0.f;
+  da = on ? sd : 0.f;
+}
+__device__ __forceinline__ void up_grad(int silu, float v, float& u, float& du) {
+  if (silu) {
+    silu_grad(v, u, du);
+  } else {
+    u = v;
+    du = 1.f;
+  }
+}
+
+// ------------------------------------------------------------------ which tile
+// Workgroups go to the 8 XCDs in turn, each with an L2 of its own: XCD x takes the x-th eighth of the
+// tiles, and walks it in bands of 8 tile rows, so that the tiles it works on at one time share rows of A
+// and of B.
+struct TileAt {
+  int m, n, split;
+};
+__device__ __forceinline__ TileAt tile_at(const GemmArgs& g) {
+  const int n = g.ntm * g.ntn * g.splits;
+  const int q = n / 8, rem = n % 8, x = blockIdx.x % 8, i = blockIdx.x / 8;
+  int t = x * q + min(x, rem) + i;
+  const int split = t % g.splits;
+  t /= g.splits;
+  constexpr int kBand = 8;
+  const int band = t / (kBand * g.ntn), rows = min(kBand, g.ntm - band * kBand), u = t - band * kBand * g.ntn;
+  return TileAt{band * kBand + u % rows, u / rows, split};
+}
+
+// ------------------------------------------------------------------ adapters within a product
+// The adapters of a tile's tokens, each once, in the order of their first token, in LDS, and every
+// token's place in that list (-1: none).  All threads call it.
+template <int BM>
+struct AdapterTile {
+  int ids[BM], list[BM], slot[BM], count;
+
+  __device__ void build(const LowRank& lr, int m0, int M) {
+    const int t = threadIdx.x;
+    if (t < BM) {
+      const int id = m0 + t < M ? lr.ids[m0 + t] : -1;
+      ids[t] = id >= 0 && id < lr.n ? id : -1;
+    }
+    __syncthreads();
+    int first = -1;  // the first token with this token's adapter
+    if (t < BM && ids[t] >= 0) {
+      first = t;
+      for (int s = 0; s < t; ++s)
+        if (ids[s] == ids[t]) {
+          first = s;
+          break;
+        }
+    }
+    if (t < BM) slot[t] = first;  // for now
+    __syncthreads();
+    int place = -1;
+    if (first >= 0) {
+      place = 0;
+      for (int s = 0; s < first; ++s) place += slot[s] == s;
+      if (first == t) list[place] = ids[t];
+    }
+    int n = 0;
+    if (t == 0)
+      for (int s = 0; s < BM; ++s) n += slot[s] == s;
+    __syncthreads();
+    if (t < BM) slot[t] = place;
+    if (t == 0) count = n;
+    __syncthreads();
+  }
+};
+
+// One step of the low-rank part: its k runs over (adapter of the tile, rank), rp to an adapter, in
+// chunks; row m of the A tile holds v[m] in its own adapter's chunks and zero in the others, row n of
+// the B tile B_j[n].  The pieces of a row lie at unrelated addresses, so they pass through registers;
+// they are few.  Both images are KC.
+template <class E, int ROWS, int THREADS, class Get>
+__device__ __forceinline__ void fill_kc(char* dst, Get get) {
+  for (int s = threadIdx.x; s < ROWS * 8; s += THREADS) {
+    const int r = s >> 3, c = s & 7;
+    *reinterpret_cast<uint4*>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = get(r, c);
+  }
+}
+// up to EPC elements from p, the rest zero
+template <class E>
+__device__ __forceinline__ uint4 load_part(const typename E::T* p, int n, bool whole) {
+  if (n <= 0) return make_uint4(0, 0, 0, 0);
+  if (whole) return *reinterpret_cast<const uint4*>(p);
+  typename E::T v[E::EPC];
+#pragma unroll
+  for (int i = 0; i < E::EPC; ++i) v[i] = i < n ? p[i] : (typename E::T)0.f;
+  return __builtin_bit_cast(uint4, v);
+}
+
+// ------------------------------------------------------------------ the kernel
+// DUAL: B's tile holds W_gate and W_up rows of the same BN / 2 neurons, a wave's columns being half of
+// either, so that its lanes end with both values of their neurons.  AD: adapters.
+template <class E, class C, Lay LA, Lay LB, bool DUAL, bool AD, class Epi>
+__global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
+  __shared__ __align__(1024) char lds[C::S * C::stage];
+  constexpr int G = C::WTN / 2;  // neurons of a wave, dual
+  constexpr int BNN = DUAL ? C::BN / 2 : C::BN;
+  const TileAt at = tile_at(g);
+  const int m0 = at.m * C::BM, n0 = at.n * BNN;
+  const int wave = uniform(threadIdx.x / kWave), wm = wave / C::WN, wn = wave % C::WN;
+  epi.select(g);
+
+  Loader<E, LA, C::BM, C::NW> la;
+  Loader<E, LB, C::BN, C::NW> lb;
+  la.init(g.a.ld, g.a.rows, m0, [](int r) { return r; });
+  if constexpr (DUAL) {
+    static_assert(LB == Lay::KC && G % 8 == 0, "an instruction loads 8 rows of one of the two matrices");
+    lb.init(g.b.ld, g.b.rows, n0, [](int r) { return r / C::WTN * G + r % G; });
+  } else {
+    lb.init(g.b.ld, g.b.rows, n0, [](int r) { return r; });
+  }
+  const int64_t sa = la.stride(g.a.ld), sb = lb.stride(g.b.ld);
+  const int64_t a0 = LA == Lay::KC ? (int64_t)m0 * g.a.ld * esz<E>() : (int64_t)m0 * esz<E>();
+  const int64_t b0 = LB == Lay::KC ? (int64_t)n0 * g.b.ld * esz<E>() : (int64_t)n0 * esz<E>();
+  const int kt = (g.K + step_k<E>() - 1) / step_k<E>();
+
+  auto issue = [&](int it, int buf) {
+    const int seg = it >= kt ? 1 : 0, k = it - seg * kt;
+    char* d = lds + buf * C::stage;
+    la.issue(static_cast<const char*>(g.a.p[seg]) + a0 + k * sa, g.K - k * step_k<E>(), d);
+    const int left = g.K - k * step_k<E>();
+    if constexpr (DUAL) {
+      const char *b_gate = static_cast<const char*>(g.b.p[0]) + b0 + k * sb,
+                 *b_up = static_cast<const char*>(g.b.p[1]) + b0 + k * sb;
+      lb.issue(left, d + C::BM * 128, [&](int j) { return j * 8 % C::WTN < G ? b_gate : b_up; });
+    } else {
+      lb.issue(static_cast<const char*>(g.b.p[seg]) + b0 + k * sb, left, d + C::BM * 128);
+    }
+  };
+
+  f32x4_t acc[C::MT][C::NT];
+#pragma unroll
+  for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  const Reader<E, LA, C::BM, C::MT> ra(wm * C::WTM);
+  const Reader<E, LB, C::BN, C::NT> rb(wn * C::WTN);
+  const Split shares(kt * g.products, g.splits);
+  const int it0 = shares.start(at.split), it1 = shares.start(at.split + 1);
+  constexpr int per_step = decltype(la)::per + decltype(lb)::per;
+  int buf = 0;
+#pragma unroll
+  for (int i = 0; i < C::S - 1; ++i)
+    if (it0 + i < it1) issue(it0 + i, i);
+  for (int it = it0; it < it1; ++it) {
+    // this step's loads: the steps behind it may stay in flight, of which near the end there are fewer
+    if (it + C::S - 2 < it1) wait_loads<(C::S - 2) * per_step>();
+    else wait_loads<0>();
+    meet();
+    const int next = buf == 0 ? C::S - 1 : buf - 1;
+    if (it + C::S - 1 < it1) issue(it + C::S - 1, next);
+    multiply<E, C, LA, LB>(lds + buf * C::stage, lds + buf * C::stage + C::BM * 128, ra, rb, acc);
+    buf = buf + 1 == C::S ? 0 : buf + 1;
+  }
+
+  if constexpr (AD) {
+    __shared__ AdapterTile<C::BM> ad;
+    if (at.split == g.splits - 1) {
+      ad.build(g.lr, m0, g.M);
+      const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
+      const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);
+      typedef typename E::T T;
+      const LowRank& lr = g.lr;
+      const int cpr = lr.rp / E::EPC, chunks = ad.count * cpr;
+      const bool whole = lr.r % E::EPC == 0;
+      // a dual product's v differ too: W_gate's adapters first, then W_up's, against rows of the other
+      // matrix that are zero
+      for (int which = 0; which < (DUAL ? 2 : 1); ++which) {
+        if (!lr.b[which]) continue;
+        for (int c0 = 0; c0 < chunks; c0 += 8) {
+          __syncthreads();
+          fill_kc<E, C::BM, C::threads>(lds, [&](int r, int c) {
+            const int q = c0 + c, slot = q / cpr, part = q - slot * cpr;
+            const bool mine = q < chunks && ad.slot[r] == slot;
+            const T* v = static_cast<const T*>(lr.v[which]) + (size_t)(m0 + r) * lr.rp + part * E::EPC;
+            return mine ? *reinterpret_cast<const uint4*>(v) : make_uint4(0, 0, 0, 0);
+          });
+          fill_kc<E, C::BN, C::threads>(lds + C::BM * 128, [&](int r, int c) {
+            const int q = c0 + c, slot = q / cpr, part = q - slot * cpr;
+            const int n = n0 + (DUAL ? r / C::WTN * G + r % G : r);
+            const bool on = q < chunks && n < lr.out && (!DUAL || (r % C::WTN >= G) == (which == 1));
+            const T* b = static_cast<const T*>(lr.b[which]) +
+                         ((size_t)(on ? ad.list[slot] : 0) * lr.out + (on ? n : 0)) * lr.r + part * E::EPC;
+            return load_part<E>(b, on ? lr.r - part * E::EPC : 0, whole);
+          });
+          __syncthreads();
+          multiply<E, C, Lay::KC, Lay::KC>(lds, lds + C::BM * 128, rva, rvb, acc);
+        }
+      }
+    }
+  }
+
+  // lane l of a 16 x 16 tile: m = l % 16, n = 4 (l / 16) .. + 3
+  const int lane = lane_id();
+#pragma unroll
+  for (int i = 0; i < C::MT; ++i) {
+    const int m = m0 + wm * C::WTM + i * 16 + (lane & 15);
+    if (m >= g.M) continue;
+    if constexpr (DUAL) {
+#pragma unroll
+      for (int j = 0; j < C::NT / 2; ++j)
+        epi.pair(m, n0 + wn * G + j * 16 + 4 * (lane >> 4), acc[i][j], acc[i][j + C::NT / 2]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j)
+        epi.put(g, at.split, m, n0 + wn * C::WTN + j * 16 + 4 * (lane >> 4), acc[i][j]);
+    }
+  }
+}
+
+}  // namespace
+}  // namespace ffn

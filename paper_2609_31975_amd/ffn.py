@@ -15,7 +15,7 @@ import re
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libffn_sparse.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "ffn_sparse.h")
-HEADERS = [HEADER, os.path.join(os.path.dirname(PKG), "include", "ffn_lopa_approx.h")]
+HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h")]
 
 FFN_F32 = 0
 FFN_BF16 = 1
@@ -27,6 +27,7 @@ STATUS = {0: "FFN_OK", -1: "FFN_ERR_NULL", -2: "FFN_ERR_SHAPE", -3: "FFN_ERR_DTY
 
 FFN_ACT_RELU = 0
 FFN_ACT_RSPLUS = 1
+FFN_ACT_SILU = 2  # the ffn_gated_* calls only
 
 
 class Scales(ctypes.Structure):
@@ -40,6 +41,12 @@ class Options(ctypes.Structure):
     _fields_ = [("act", ctypes.c_int), ("silu_up", ctypes.c_int), ("g_idx", ctypes.c_void_p),
                 ("g_sign", ctypes.c_void_p), ("rms_norm", ctypes.c_int), ("rms_gain", ctypes.c_void_p),
                 ("rms_eps", ctypes.c_float)]
+
+
+class AdapterStruct(ctypes.Structure):
+    """``ffn_adapters_t``: the adapters of a call's requests (device pointers)."""
+    _fields_ = [("n", ctypes.c_int), ("r", ctypes.c_int)] + [
+        (f, ctypes.c_void_p) for f in ("ids", "scale", "gate_a", "gate_b", "up_a", "up_b", "down_a", "down_b")]
 
 
 class FFNError(RuntimeError):
@@ -93,6 +100,16 @@ def lib() -> ctypes.CDLL:
         L.ffn_lopa_approx.restype = i
         L.ffn_lopa_approx.argtypes = [i, i, i, vp, i, vp, vp, vp, vp, ctypes.POINTER(ctypes.c_int),
                                       ctypes.POINTER(ctypes.c_double), vp, sz, vp]
+        ap = ctypes.POINTER(AdapterStruct)
+        for name, res, args in (
+                ("ffn_gated_save_bytes", sz, [i, i, i]),
+                ("ffn_gated_workspace_bytes", sz, [i, i, i, i, i, i]),
+                ("ffn_adapter_workspace_bytes", sz, [i, i, i, i, i]),
+                ("ffn_gated_forward", i, [i, i, i, i, vp, vp, vp, vp, f, op, ap, vp, vp, sz, vp, sz, vp]),
+                ("ffn_gated_backward", i, [i, i, i, i, vp, vp, vp, vp, op, vp, vp, sz, vp, vp, vp, vp, vp, sz, vp]),
+                ("ffn_adapter_forward", i, [i, i, i, i, vp, vp, ap, vp, vp, sz, vp])):
+            getattr(L, name).restype = res
+            getattr(L, name).argtypes = args
         L.ffn_status_string.restype = ctypes.c_char_p
         L.ffn_status_string.argtypes = [i]
         _lib = L
@@ -456,6 +473,172 @@ def ffn_lopa_approx(w, r: int, max_iters: int = 20, stream=None):
                                _dev(ws, "ws"), n, _stream(stream, w.device))
     _check("ffn_lopa_approx", rc)
     return g_idx, g_sign, U, V, it.value, obj.value
+
+
+# ---------------------------------------------------------------- the gated block over many tokens, adapters
+class Adapters:
+    """The adapters of a call's requests: the ``ffn_adapters_t`` and the tensors it points into."""
+
+    def __init__(self, ids, gate=None, up=None, down=None, scale=None):
+        torch = _torch()
+        self.stacks = {k: v for k, v in (("gate", gate), ("up", up), ("down", down)) if v is not None}
+        if not self.stacks:
+            raise ValueError("adapters of at least one projection are required")
+        if ids.dim() != 1 or ids.dtype != torch.int32:
+            raise ValueError(f"ids must be an int32 [T] tensor, got {ids.dtype} {tuple(ids.shape)}")
+        a0 = next(iter(self.stacks.values()))[0]
+        if a0.dim() != 3:
+            raise ValueError(f"a stack of first factors must be [n, r, in], got {tuple(a0.shape)}")
+        self.n, self.r = a0.shape[:2]
+        self.dtype, self.ids, self.scale = a0.dtype, ids, scale
+        for name, (a, b) in self.stacks.items():
+            if a.dim() != 3 or b.dim() != 3 or a.shape[:2] != (self.n, self.r) or b.shape[::2] != (self.n, self.r):
+                raise ValueError(f"{name}: stacks must be [{self.n}, {self.r}, in] and [{self.n}, out, {self.r}], got "
+                                 f"{tuple(a.shape)} and {tuple(b.shape)}")
+            if a.dtype != self.dtype or b.dtype != self.dtype:
+                raise ValueError(f"{name}: every stack must be {self.dtype}, got {a.dtype} and {b.dtype}")
+        if scale is not None and (scale.dtype != torch.float32 or scale.shape != (self.n,)):
+            raise ValueError(f"scale must be float32 [{self.n}], got {scale.dtype} {tuple(scale.shape)}")
+        tensors = [(ids, "ids"), (scale, "scale")] + [(w, n) for n, p in self.stacks.items() for w in p]
+        ptrs = {n: [_dev(w, n) for w in p] for n, p in self.stacks.items()}
+        if any(w is not None and w.device != ids.device for w, _ in tensors):
+            raise ValueError("ids, scale and the stacks must be on one device")
+        none = [None, None]
+        self.struct = AdapterStruct(self.n, self.r, _dev(ids, "ids"), _dev(scale, "scale"), *ptrs.get("gate", none),
+                                    *ptrs.get("up", none), *ptrs.get("down", none))
+
+    def check(self, x, sizes):
+        """sizes: {projection: (in, out)} of the call."""
+        if self.ids.shape[0] != x.shape[0] or self.ids.device != x.device or self.dtype != x.dtype:
+            raise ValueError(f"the adapters are {self.dtype} of {self.ids.shape[0]} tokens on {self.ids.device}, x is "
+                             f"{x.dtype} {tuple(x.shape)} on {x.device}")
+        for name, (a, b) in self.stacks.items():
+            if name not in sizes:
+                raise ValueError(f"this call has no {name} projection")
+            if (a.shape[2], b.shape[1]) != sizes[name]:
+                raise ValueError(f"{name}: adapters of [{b.shape[1]}, {a.shape[2]}], the projection is "
+                                 f"{list(sizes[name][::-1])}")
+
+
+def adapters(ids, gate=None, up=None, down=None, scale=None) -> Adapters:
+    """The adapters of a call: ids int32 [T] (a value outside [0, n): none), for each projection that has
+    some a pair (A [n, r, in], B [n, out, r]), and scale float32 [n] or None.  Device tensors."""
+    return Adapters(ids, gate, up, down, scale)
+
+
+def _type_of(dtype) -> int:
+    torch = _torch()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"tokens and weights must be bfloat16 or float32, got {dtype}")
+    return FFN_BF16 if dtype == torch.bfloat16 else FFN_F32
+
+
+def _bytes(n, name, device):
+    if n == 0:
+        raise FFNError(name, -2)
+    return _torch().empty(n, dtype=_torch().uint8, device=device)
+
+
+def alloc_gated_workspace(T, d, d_ff, dtype, r=0, backward=True, device="cuda"):
+    """Workspace of ffn_gated_forward (adapters of rank up to r) and, with backward, ffn_gated_backward."""
+    return _bytes(int(lib().ffn_gated_workspace_bytes(_type_of(dtype), T, d, d_ff, r, int(backward))),
+                  "ffn_gated_workspace_bytes", device)
+
+
+def alloc_gated_save(T, d_ff, dtype, device="cuda"):
+    """What a forward call keeps for its backward call."""
+    return _bytes(int(lib().ffn_gated_save_bytes(_type_of(dtype), T, d_ff)), "ffn_gated_save_bytes", device)
+
+
+def alloc_adapter_workspace(T, d, n_out, r, dtype, device="cuda"):
+    return _bytes(int(lib().ffn_adapter_workspace_bytes(_type_of(dtype), T, d, n_out, r)),
+                  "ffn_adapter_workspace_bytes", device)
+
+
+def _check_like(dev, dtype, tensors):
+    """tensors: (tensor, name, shape, may be None); all contiguous, of one device and dtype."""
+    for w, name, shape, optional in tensors:
+        if w is None:
+            if optional:
+                continue
+            raise ValueError(f"{name} is required")
+        if w.get_device() != dev or not w.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor on x's device")
+        if w.dtype is not dtype or w.shape != shape:
+            raise ValueError(f"{name} must be {dtype} {list(shape)}, got {w.dtype} {list(w.shape)}")
+
+
+def _check_buffers(dev, *buffers):
+    for b, name in buffers:
+        if b is not None and (b.get_device() != dev or not b.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous tensor on x's device")
+
+
+def _tokens(x):
+    if x.dim() != 2 or not x.is_cuda:
+        raise ValueError(f"x must be a [T, d] device tensor, got {tuple(x.shape)} on {x.device}")
+    return x.shape[0], x.shape[1], x.get_device(), _type_of(x.dtype)
+
+
+def _p(t):
+    return None if t is None else t.data_ptr()
+
+
+def _size(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def ffn_gated_forward(x, w_gate, w_up, w_down_t, t, opt, y, ws, save=None, adapters=None, stream=None):
+    """The gated block over x's tokens, every neuron evaluated: bfloat16 or float32 throughout.  save: None,
+    or a buffer of alloc_gated_save for ffn_gated_backward; adapters: None, or ffn.adapters(...)."""
+    T, d, dev, wdt = _tokens(x)
+    d_ff = w_up.shape[0]
+    w = (d_ff, d)
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (w_gate, "w_gate", w, False), (w_up, "w_up", w, False),
+                               (w_down_t, "w_down_t", w, False), (y, "y", x.shape, False)))
+    _check_buffers(dev, (ws, "ws"), (save, "save"))
+    ad = None
+    if adapters is not None:
+        adapters.check(x, {"gate": (d, d_ff), "up": (d, d_ff), "down": (d_ff, d)})
+        ad = ctypes.byref(adapters.struct)
+    rc = _function("ffn_gated_forward")(wdt, T, d, d_ff, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
+                                        w_down_t.data_ptr(), ctypes.c_float(t), _opt(opt), ad, y.data_ptr(), _p(save),
+                                        _size(save), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
+    _check("ffn_gated_forward", rc)
+    return y
+
+
+def ffn_gated_backward(x, w_gate, w_up, w_down_t, opt, dy, save, dx, dw_gate, dw_up, dw_down_t, ws, stream=None):
+    """Gradients of the block from dy and the forward call's save, written to dx, dw_gate, dw_up and dw_down_t
+    (None: not computed)."""
+    T, d, dev, wdt = _tokens(x)
+    d_ff = w_up.shape[0]
+    w = (d_ff, d)
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (w_gate, "w_gate", w, False), (w_up, "w_up", w, False),
+                               (w_down_t, "w_down_t", w, False), (dy, "dy", x.shape, False), (dx, "dx", x.shape, True),
+                               (dw_gate, "dw_gate", w, True), (dw_up, "dw_up", w, True),
+                               (dw_down_t, "dw_down_t", w, True)))
+    _check_buffers(dev, (ws, "ws"), (save, "save"))
+    rc = _function("ffn_gated_backward")(wdt, T, d, d_ff, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
+                                         w_down_t.data_ptr(), _opt(opt), dy.data_ptr(), _p(save), _size(save), _p(dx),
+                                         _p(dw_gate), _p(dw_up), _p(dw_down_t), ws.data_ptr(), _size(ws),
+                                         _raw_stream(stream, x))
+    _check("ffn_gated_backward", rc)
+    return dx, dw_gate, dw_up, dw_down_t
+
+
+def ffn_adapter_forward(x, w, adapters, y, ws, stream=None):
+    """One shared projection w [n_out, d] of x's tokens with the requests' adapters (the gate pair of
+    ffn.adapters(...))."""
+    T, d, dev, wdt = _tokens(x)
+    n_out = w.shape[0]
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (w, "w", (n_out, d), False), (y, "y", (T, n_out), False)))
+    _check_buffers(dev, (ws, "ws"))
+    adapters.check(x, {"gate": (d, n_out)})
+    rc = _function("ffn_adapter_forward")(wdt, T, d, n_out, x.data_ptr(), w.data_ptr(), ctypes.byref(adapters.struct),
+                                          y.data_ptr(), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
+    _check("ffn_adapter_forward", rc)
+    return y
 
 
 def ffn_status_string(code: int) -> str:
