@@ -166,6 +166,16 @@ struct Loader {
 };
 
 // ------------------------------------------------------------------ LDS to fragments
+// A 16-byte LDS read as a plain vector load.  Read as a struct (uint4), the load loses its type in the
+// compiler, which then takes it to depend on every load into LDS still in flight and waits for all of
+// them (vmcnt 0) in front of it.
+__device__ __forceinline__ uint4 lds_read16(const char* p) {
+  const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+// The transposing read (see lds_read_tr16), for the same reason through a pointer of its own scope.
+__device__ __forceinline__ uint2 lds_read_tr(const char* __restrict__ p) { return lds_read_tr16(p); }
+
 // Fragment of half kk (0, 1) of a step for the 16 rows from tile row r: lane l holds row r + l % 16 and
 // chunk l / 16 of the half (bf16: k = 8 (l / 16) .. + 7; fp32: component j is k = 4 (l / 16) + j).
 template <class E, Lay L, int ROWS, int TILES>
@@ -195,10 +205,10 @@ struct Reader {
   }
   __device__ __forceinline__ uint4 get(const char* s, int kk, int t) const {
     if constexpr (L == Lay::KC) {
-      return *reinterpret_cast<const uint4*>(s + off[kk] + t * 2048);
+      return lds_read16(s + off[kk] + t * 2048);
     } else if constexpr (E::EPC == 8) {
       const char* p = s + off[t] + kk * 32 * CPR * 16;
-      const uint2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * CPR * 16);
+      const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 4 * CPR * 16);
       return make_uint4(lo.x, lo.y, hi.x, hi.y);
     } else {
       const char* p = s + off[t] + kk * 16 * CPR * 16;
@@ -221,22 +231,24 @@ __device__ __forceinline__ f32x4_t product(const uint4& b, const uint4& a, f32x4
   }
 }
 
+// The fragments of half a step, and their products.
 template <class E, class C, Lay LA, Lay LB>
-__device__ __forceinline__ void multiply(const char* sa, const char* sb, const Reader<E, LA, C::BM, C::MT>& ra,
-                                         const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT]) {
+struct Half {
+  uint4 a[C::MT], b[C::NT];
+  __device__ __forceinline__ void load(const char* stage, int kk, const Reader<E, LA, C::BM, C::MT>& ra,
+                                       const Reader<E, LB, C::BN, C::NT>& rb) {
 #pragma unroll
-  for (int kk = 0; kk < 2; ++kk) {
-    uint4 a[C::MT], b[C::NT];
+    for (int i = 0; i < C::NT; ++i) b[i] = rb.get(stage + C::BM * 128, kk, i);
 #pragma unroll
-    for (int i = 0; i < C::NT; ++i) b[i] = rb.get(sb, kk, i);
-#pragma unroll
-    for (int i = 0; i < C::MT; ++i) a[i] = ra.get(sa, kk, i);
+    for (int i = 0; i < C::MT; ++i) a[i] = ra.get(stage, kk, i);
+  }
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT]) const {
 #pragma unroll
     for (int i = 0; i < C::MT; ++i)
 #pragma unroll
       for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
   }
-}
+};
 
 // ------------------------------------------------------------------ activations
 // A(g), and with its derivative; the same of the up side.  A gate value that is not above zero (NaN
@@ -405,19 +417,34 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
   const Split shares(kt * g.products, g.splits);
   const int it0 = shares.start(at.split), it1 = shares.start(at.split + 1);
   constexpr int per_step = decltype(la)::per + decltype(lb)::per;
-  int buf = 0;
+  // Half a step's fragments are read while the other half's products run: the second half of step i
+  // during the first half's products, the first half of step i + 1, behind the barrier that frees step
+  // i's buffer, during the second half's.  The matrix pipes then wait for no LDS read.
+  if (it0 < it1) {
 #pragma unroll
-  for (int i = 0; i < C::S - 1; ++i)
-    if (it0 + i < it1) issue(it0 + i, i);
-  for (int it = it0; it < it1; ++it) {
-    // this step's loads: the steps behind it may stay in flight, of which near the end there are fewer
-    if (it + C::S - 2 < it1) wait_loads<(C::S - 2) * per_step>();
+    for (int i = 0; i < C::S; ++i)
+      if (it0 + i < it1) issue(it0 + i, i);
+    if (it0 + C::S <= it1) wait_loads<(C::S - 1) * per_step>();
     else wait_loads<0>();
     meet();
-    const int next = buf == 0 ? C::S - 1 : buf - 1;
-    if (it + C::S - 1 < it1) issue(it + C::S - 1, next);
-    multiply<E, C, LA, LB>(lds + buf * C::stage, lds + buf * C::stage + C::BM * 128, ra, rb, acc);
-    buf = buf + 1 == C::S ? 0 : buf + 1;
+    Half<E, C, LA, LB> h0, h1;
+    h0.load(lds, 0, ra, rb);
+    int buf = 0;
+    for (int it = it0; it < it1; ++it) {
+      h1.load(lds + buf * C::stage, 1, ra, rb);
+      h0.multiply(acc);
+      issue_barrier();
+      if (it + 1 < it1) {
+        // step it + 1's loads: those behind it may stay in flight, of which near the end there are fewer
+        if (it + C::S <= it1) wait_loads<(C::S - 2) * per_step>();
+        else wait_loads<0>();
+        meet();
+        if (it + C::S < it1) issue(it + C::S, buf);
+        buf = buf + 1 == C::S ? 0 : buf + 1;
+        h0.load(lds + buf * C::stage, 0, ra, rb);
+      }
+      h1.multiply(acc);
+    }
   }
 
   if constexpr (AD) {
@@ -451,7 +478,12 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
             return load_part<E>(b, on ? lr.r - part * E::EPC : 0, whole);
           });
           __syncthreads();
-          multiply<E, C, Lay::KC, Lay::KC>(lds, lds + C::BM * 128, rva, rvb, acc);
+          Half<E, C, Lay::KC, Lay::KC> h;
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            h.load(lds, kk, rva, rvb);
+            h.multiply(acc);
+          }
         }
       }
     }
