@@ -137,27 +137,12 @@ struct Loader {
       }
     }
   }
-  // one step from `base` (its first k), k_left of k left
-  __device__ __forceinline__ void issue(const char* base, int k_left, char* dst) const {
-    issue(k_left, dst, [base](int) { return base; });
-  }
-  // base(j): where the rows of instruction j lie
+  // Instruction i of this wave for a step that starts at `base` with k_left of k left (none or less:
+  // zeros); base(j) where the rows of instruction j lie.
   template <class Base>
-  __device__ __forceinline__ void issue(int k_left, char* dst, Base base) const {
-    const int wave = uniform(threadIdx.x / kWave);
-    if (k_left >= step_k<E>()) {
-#pragma unroll
-      for (int i = 0; i < per; ++i) {
-        const int j = instr(i, wave);
-        lds_load16(make_buf(base(j), 0x7fffffffu), dst + j * 1024, off[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < per; ++i) {
-        const int j = instr(i, wave);
-        lds_load16(make_buf(base(j), 0x7fffffffu), dst + j * 1024, kpos[i] < k_left ? off[i] : kOOB);
-      }
-    }
+  __device__ __forceinline__ void issue(int i, int k_left, char* dst, Base base) const {
+    const int j = instr(i, uniform(threadIdx.x / kWave));
+    lds_load16(make_buf(base(j), 0x7fffffffu), dst + j * 1024, kpos[i] < k_left ? off[i] : kOOB);
   }
   // bytes from one step to the next
   __device__ __forceinline__ static int64_t stride(int64_t ld) {
@@ -234,19 +219,30 @@ __device__ __forceinline__ f32x4_t product(const uint4& b, const uint4& a, f32x4
 // The fragments of half a step, and their products.
 template <class E, class C, Lay LA, Lay LB>
 struct Half {
+  static constexpr int count = C::MT + C::NT;
   uint4 a[C::MT], b[C::NT];
-  __device__ __forceinline__ void load(const char* stage, int kk, const Reader<E, LA, C::BM, C::MT>& ra,
+  // fragments [f0, f1) in the order in which the products use them
+  __device__ __forceinline__ void load(int f0, int f1, const char* stage, int kk, const Reader<E, LA, C::BM, C::MT>& ra,
                                        const Reader<E, LB, C::BN, C::NT>& rb) {
 #pragma unroll
-    for (int i = 0; i < C::NT; ++i) b[i] = rb.get(stage + C::BM * 128, kk, i);
-#pragma unroll
-    for (int i = 0; i < C::MT; ++i) a[i] = ra.get(stage, kk, i);
+    for (int f = 0; f < count; ++f) {
+      if (f < f0 || f >= f1) continue;
+      if (f < C::NT) b[f] = rb.get(stage + C::BM * 128, kk, f);
+      else a[f - C::NT] = ra.get(stage, kk, f - C::NT);
+    }
   }
-  __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT]) const {
+  // between(i): work to issue in front of the products of fragment a[i].  LDS reads and loads into LDS
+  // are handed out among the products a few at a time: issued in one piece they fill their queues, and a
+  // wave that waits for a queue issues no products either.
+  template <class Between>
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT], Between between) const {
 #pragma unroll
-    for (int i = 0; i < C::MT; ++i)
+    for (int i = 0; i < C::MT; ++i) {
+      between(i);
 #pragma unroll
       for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
+      issue_barrier();
+    }
   }
 };
 
@@ -392,17 +388,23 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
   const int64_t b0 = LB == Lay::KC ? (int64_t)n0 * g.b.ld * esz<E>() : (int64_t)n0 * esz<E>();
   const int kt = (g.K + step_k<E>() - 1) / step_k<E>();
 
-  auto issue = [&](int it, int buf) {
-    const int seg = it >= kt ? 1 : 0, k = it - seg * kt;
+  const Split shares(kt * g.products, g.splits);
+  const int it0 = shares.start(at.split), it1 = shares.start(at.split + 1);
+  // loads [f0, f1) of this wave for step `it`; past the last step they fill the buffer with zeros, which
+  // nothing uses, so that every step has the same loads in flight
+  constexpr int per_step = decltype(la)::per + decltype(lb)::per;
+  auto issue = [&](int f0, int f1, int it, int buf) {
+    const int seg = it >= kt ? 1 : 0, k = it - seg * kt, left = it < it1 ? g.K - k * step_k<E>() : 0;
     char* d = lds + buf * C::stage;
-    la.issue(static_cast<const char*>(g.a.p[seg]) + a0 + k * sa, g.K - k * step_k<E>(), d);
-    const int left = g.K - k * step_k<E>();
-    if constexpr (DUAL) {
-      const char *b_gate = static_cast<const char*>(g.b.p[0]) + b0 + k * sb,
-                 *b_up = static_cast<const char*>(g.b.p[1]) + b0 + k * sb;
-      lb.issue(left, d + C::BM * 128, [&](int j) { return j * 8 % C::WTN < G ? b_gate : b_up; });
-    } else {
-      lb.issue(static_cast<const char*>(g.b.p[seg]) + b0 + k * sb, left, d + C::BM * 128);
+    const char* pa = static_cast<const char*>(g.a.p[seg]) + a0 + k * sa;
+    const char* pb = static_cast<const char*>(g.b.p[DUAL ? 0 : seg]) + b0 + k * sb;
+    const char* pb2 = static_cast<const char*>(g.b.p[1]) + b0 + k * sb;
+#pragma unroll
+    for (int f = 0; f < per_step; ++f) {
+      if (f < f0 || f >= f1) continue;
+      if (f < decltype(la)::per) la.issue(f, left, d, [&](int) { return pa; });
+      else lb.issue(f - decltype(la)::per, left, d + C::BM * 128,
+                    [&](int j) { return DUAL && j * 8 % C::WTN >= G ? pb2 : pb; });
     }
   };
 
@@ -414,38 +416,30 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
 
   const Reader<E, LA, C::BM, C::MT> ra(wm * C::WTM);
   const Reader<E, LB, C::BN, C::NT> rb(wn * C::WTN);
-  const Split shares(kt * g.products, g.splits);
-  const int it0 = shares.start(at.split), it1 = shares.start(at.split + 1);
-  constexpr int per_step = decltype(la)::per + decltype(lb)::per;
   // Half a step's fragments are read while the other half's products run: the second half of step i
   // during the first half's products, the first half of step i + 1, behind the barrier that frees step
-  // i's buffer, during the second half's.  The matrix pipes then wait for no LDS read.
-  if (it0 < it1) {
+  // i's buffer, during the second half's, and with it step i + S is loaded into that buffer.
 #pragma unroll
-    for (int i = 0; i < C::S; ++i)
-      if (it0 + i < it1) issue(it0 + i, i);
-    if (it0 + C::S <= it1) wait_loads<(C::S - 1) * per_step>();
-    else wait_loads<0>();
+  for (int i = 0; i < C::S; ++i) issue(0, per_step, it0 + i, i);
+  wait_loads<(C::S - 1) * per_step>();
+  meet();
+  Half<E, C, LA, LB> h0, h1;
+  h0.load(0, h0.count, lds, 0, ra, rb);
+  int buf = 0;
+  for (int it = it0; it < it1; ++it) {
+    h0.multiply(acc, [&](int i) {
+      h1.load(i * h1.count / C::MT, (i + 1) * h1.count / C::MT, lds + buf * C::stage, 1, ra, rb);
+    });
+    wait_loads<(C::S - 2) * per_step>();
     meet();
-    Half<E, C, LA, LB> h0, h1;
-    h0.load(lds, 0, ra, rb);
-    int buf = 0;
-    for (int it = it0; it < it1; ++it) {
-      h1.load(lds + buf * C::stage, 1, ra, rb);
-      h0.multiply(acc);
-      issue_barrier();
-      if (it + 1 < it1) {
-        // step it + 1's loads: those behind it may stay in flight, of which near the end there are fewer
-        if (it + C::S <= it1) wait_loads<(C::S - 2) * per_step>();
-        else wait_loads<0>();
-        meet();
-        if (it + C::S < it1) issue(it + C::S, buf);
-        buf = buf + 1 == C::S ? 0 : buf + 1;
-        h0.load(lds + buf * C::stage, 0, ra, rb);
-      }
-      h1.multiply(acc);
-    }
+    const int next = buf + 1 == C::S ? 0 : buf + 1;
+    h1.multiply(acc, [&](int i) {
+      h0.load(i * h0.count / C::MT, (i + 1) * h0.count / C::MT, lds + next * C::stage, 0, ra, rb);
+      issue(i * per_step / C::MT, (i + 1) * per_step / C::MT, it + C::S, buf);
+    });
+    buf = next;
   }
+  wait_loads<0>();  // LDS is free for others once no load into it is in flight
 
   if constexpr (AD) {
     __shared__ AdapterTile<C::BM> ad;
@@ -481,8 +475,8 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
           Half<E, C, Lay::KC, Lay::KC> h;
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk) {
-            h.load(lds, kk, rva, rvb);
-            h.multiply(acc);
+            h.load(0, h.count, lds, kk, rva, rvb);
+            h.multiply(acc, [](int) {});
           }
         }
       }
