@@ -64,14 +64,14 @@ size_t save_layout(ffn_dtype_t w, int T, int d_ff, void* base, Save* out) {
 }
 
 size_t part_bytes(ffn_dtype_t w, int T, int n, int k, int products) {
-  const int steps = products * ((k + 8 * chunk(w) - 1) / (8 * chunk(w)));
-  const int s = token_splits(w == FFN_F32, T, n, steps);
+  const int s = token_plan(w == FFN_F32, T, n, k, products).splits;
   return s > 1 ? (size_t)s * T * round_up_to(n, 4) * 4 : 0;
 }
 
 struct ForwardWs {
   void *z, *v[2], *v2, *x, *w_gate, *w_up, *w_down;
   float* part;
+  int32_t* plan;
 };
 size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, ForwardWs* out) {
   Carver c{static_cast<char*>(base)};
@@ -81,6 +81,7 @@ size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Fo
   if (rp) {
     for (void*& v : f.v) v = c.take(e * s.T * rp);
     f.v2 = c.take(e * s.T * rp);
+    f.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
   }
   f.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d, s.d_ff, 1)));
   if (s.dp != s.d) {
@@ -118,12 +119,14 @@ size_t backward_layout(ffn_dtype_t w, const BlockShape& s, void* base, BackwardW
 struct AdapterWs {
   void *v, *x, *w;
   float* part;
+  int32_t* plan;
 };
 size_t adapter_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, AdapterWs* out) {
   Carver c{static_cast<char*>(base)};
   AdapterWs a{};
   const size_t e = esize(w);
   a.v = c.take(e * s.T * rp);
+  a.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
   a.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d_ff, s.d, 1)));
   if (s.dp != s.d) {
     a.x = c.take(e * s.T * s.dp);
@@ -221,6 +224,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   if (ws_bytes < forward_layout(wdt, s, set.rp, ws, &f)) return FFN_ERR_WORKSPACE;
   Save sv{nullptr, nullptr, f.z};
   if (save && save_bytes < save_layout(wdt, T, d_ff, save, &sv)) return FFN_ERR_WORKSPACE;
+  set.plan = f.plan;
 
   const bool f32 = wdt == FFN_F32;
   FFN_TRY(padded(f32, s, T, &x, f.x, stream));
@@ -233,7 +237,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   if (b2[0] || b2[1]) {
     const void* a[2] = {b2[0] ? ad->gate_a : ad->up_a, ad->up_a};
     void* v[2] = {b2[0] ? f.v[0] : f.v[1], f.v[1]};
-    FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, stream));
+    FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, hidden_plan(f32, s).tile, stream));
   }
   AdapterSet hidden = b2[0] || b2[1] ? set : AdapterSet{};
   FFN_TRY(launch_block_hidden(f32, s, x, w_gate, w_up, form, hidden, v2, b2, sv.z, sv.g, sv.v, stream));
@@ -241,7 +245,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   if (down) {
     const void* a[2] = {ad->down_a, nullptr};
     void* v[2] = {f.v2, nullptr};
-    FFN_TRY(launch_adapter_v(f32, T, d_ff, s.ldf, sv.z, set, 1, a, v, stream));
+    FFN_TRY(launch_adapter_v(f32, T, d_ff, s.ldf, sv.z, set, 1, a, v, token_plan(f32, T, d, d_ff, 1).tile, stream));
   }
   const TokenProduct p{{sv.z, nullptr}, {w_down_t, nullptr}, 1, T, d, d_ff, s.ldf, s.dp, d, y, f.part,
                        down ? set : AdapterSet{}, f.v2, down ? ad->down_b : nullptr};
@@ -309,12 +313,13 @@ int ffn_adapter_forward(ffn_dtype_t wdt, int T, int d, int n_out, const void* x,
   const BlockShape s = shape_of(wdt, T, d, n_out);
   AdapterWs a;
   if (ws_bytes < adapter_layout(wdt, s, set.rp, ws, &a)) return FFN_ERR_WORKSPACE;
+  set.plan = a.plan;
   const bool f32 = wdt == FFN_F32;
   FFN_TRY(padded(f32, s, T, &x, a.x, stream));
   FFN_TRY(padded(f32, s, n_out, &w, a.w, stream));
   const void* aa[2] = {ad->gate_a, nullptr};
   void* v[2] = {a.v, nullptr};
-  FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, 1, aa, v, stream));
+  FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, 1, aa, v, token_plan(f32, T, n_out, d, 1).tile, stream));
   const TokenProduct p{{x, nullptr}, {w, nullptr}, 1, T, n_out, d, s.dp, s.dp, n_out, y, a.part, set, a.v, ad->gate_b};
   FFN_TRY(launch_token_product_kc(f32, p, stream));
   return FFN_OK;

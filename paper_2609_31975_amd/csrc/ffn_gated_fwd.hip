@@ -31,12 +31,6 @@ struct EpiGated {
   }
 };
 
-template <class E, class C>
-hipError_t run(const GemmArgs& a, const EpiGated<E>& epi, hipStream_t st) {
-  return a.lr.ids ? launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st)
-                  : launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
-}
-
 template <class E>
 hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const void* w_up, const BlockForm& form,
                   const AdapterSet& ad, const void* const v2[2], const void* const b2[2], void* z, float* g, float* v,
@@ -49,13 +43,13 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
   a.K = s.d;
   a.products = 1;
   a.splits = 1;
-  if (ad.ids) a.lr = low_rank(ad, v2, b2, s.d_ff);
+  if (ad.plan) a.lr = low_rank(ad, v2, b2, s.d_ff);
   const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
-  if (s.T <= 16) return run<E, TileT16>(a, epi, st);
-  if (s.T <= 64) return run<E, TileT64>(a, epi, st);
-  if constexpr (E::EPC == 8)
-    if (ceil_div(s.T, 256) * ceil_div(s.d_ff, 128) >= 2 * kCUs) return run<E, TileT256>(a, epi, st);
-  return run<E, TileT128>(a, epi, st);
+  return with_tile<E>(hidden_plan(E::EPC == 4, s).tile, [&](auto c) {
+    typedef decltype(c) C;
+    return a.lr.plan ? launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st)
+                     : launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
+  });
 }
 
 }  // namespace

@@ -20,7 +20,20 @@ struct AdapterSet {
   int n = 0, r = 0, rp = 0;
   const int32_t* ids = nullptr;
   const float* scale = nullptr;
+  int32_t* plan = nullptr;  // room for plan_ints(T); filled by launch_adapter_v
 };
+
+// The tile of a product with M rows and n columns over `steps` steps of 128 bytes, and the shares its sum is
+// cut into (1 where split is false).
+enum class Tile { T16, T64, T128, T128x256, T256 };
+struct Plan {
+  Tile tile;
+  int splits;
+};
+Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split);
+int tile_rows(Tile t);
+// Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.
+inline size_t plan_ints(int T) { return 2 * ((size_t)T + 256) + T / 16 + 1; }
 
 // Shapes: rows of dp elements (d rounded up to whole chunks), hidden rows of ldf (d_ff rounded up to 64).
 struct BlockShape {
@@ -38,12 +51,13 @@ struct TokenProduct {
   const void* b[2];  // KS: [k][ldb]; KC: [n][ldb]
   int products, T, n, k, lda, ldb, ldo;
   void* out;
-  float* part;  // splits x T x round_up(n, 4) fp32 where token_splits(...) > 1
+  float* part;  // splits x T x round_up(n, 4) fp32 where the sum is cut
   AdapterSet ad;
   const void* v;
   const void* ab;
 };
-int token_splits(bool f32, int T, int n, int steps);
+Plan token_plan(bool f32, int T, int n, int k, int products);
+Plan hidden_plan(bool f32, const BlockShape& s);
 hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st);
 hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t st);
 // dg, dv [T][ldf] from dz = dy W2 and the saved g, v.
@@ -52,9 +66,9 @@ hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const 
 // up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
                            void* const out[3], hipStream_t st);
-// v[i] [T][rp] = scale_j A_j x for up to two stacks
+// v[i] [T][rp] = scale_j A_j x for up to two stacks, and ad.plan for the product of tile `t` that reads them
 hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
-                            const void* const a[2], void* const v[2], hipStream_t st);
+                            const void* const a[2], void* const v[2], Tile t, hipStream_t st);
 // rows of n elements to rows of np, the rest zero
 hipError_t launch_pad_rows(bool f32, int64_t rows, int n, int np, const void* src, void* dst, hipStream_t st);
 

@@ -40,8 +40,15 @@ __global__ void __launch_bounds__(kBlock) k_join(int splits, int M, int N, int n
   for (size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x; i < total; i += (size_t)gridDim.x * kBlock) {
     const int m = (int)(i / q), n = (int)(i - (size_t)m * q) * 4;
     const float* p = part + (size_t)m * np + n;
-    f32x4_t v = *reinterpret_cast<const f32x4_t*>(p);
-    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4_t*>(p + s * plane);
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < splits; s0 += 8) {  // 8 loads in flight
+      f32x4_t u[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        u[s] = s0 + s < splits ? *reinterpret_cast<const f32x4_t*>(p + (s0 + s) * plane) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 8; ++s) v += u[s];
+    }
     typename E::T* o = out + (size_t)m * ldo + n;
     if (N % 4 == 0) {
       store4<E>(o, v);
@@ -50,20 +57,6 @@ __global__ void __launch_bounds__(kBlock) k_join(int splits, int M, int N, int n
         if (n + k < N) o[k] = (typename E::T)v[k];
     }
   }
-}
-
-template <class E, class C, Lay LB>
-hipError_t run(const GemmArgs& a, const EpiTok<E>& epi, hipStream_t st) {
-  return a.lr.ids ? launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st)
-                  : launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
-}
-
-enum class TokTile { T16, T64, T128, T256 };
-TokTile tile_for(bool f32, int T, int n) {
-  if (T <= 16) return TokTile::T16;
-  if (T <= 64) return TokTile::T64;
-  if (!f32 && (int64_t)ceil_div(T, 256) * ceil_div(n, 256) >= kCUs) return TokTile::T256;
-  return TokTile::T128;
 }
 
 template <class E, Lay LB>
@@ -75,20 +68,17 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   a.N = p.n;
   a.K = p.k;
   a.products = p.products;
-  a.splits = token_splits(E::EPC == 4, p.T, p.n, p.products * ceil_div(p.k, step_k<E>()));
+  const Plan plan = token_plan(E::EPC == 4, p.T, p.n, p.k, p.products);
+  a.splits = plan.splits;
   const void *v[2] = {p.v, nullptr}, *b[2] = {p.ab, nullptr};
-  if (p.ad.ids) a.lr = low_rank(p.ad, v, b, p.n);
+  if (p.ad.plan) a.lr = low_rank(p.ad, v, b, p.n);
   const int np = (p.n + 3) / 4 * 4;
   const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.part, p.ldo, np, p.n % 4 == 0};
-  hipError_t e;
-  switch (tile_for(E::EPC == 4, p.T, p.n)) {
-    case TokTile::T16: e = run<E, TileT16, LB>(a, epi, st); break;
-    case TokTile::T64: e = run<E, TileT64, LB>(a, epi, st); break;
-    case TokTile::T128: e = run<E, TileT128, LB>(a, epi, st); break;
-    default:
-      if constexpr (E::EPC == 8) e = run<E, TileT256, LB>(a, epi, st);
-      else e = hipErrorInvalidValue;  // not reached: tile_for gives fp32 at most T128
-  }
+  hipError_t e = with_tile<E>(plan.tile, [&](auto c) {
+    typedef decltype(c) C;
+    return a.lr.plan ? launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st)
+                     : launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
+  });
   if (e == hipSuccess && a.splits > 1) {
     const int64_t quads = (int64_t)p.T * np / 4;
     const int grid = (int)(quads / kBlock + 1 < 8 * kCUs ? quads / kBlock + 1 : 8 * kCUs);
@@ -99,67 +89,137 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ the adapters' first factor
-// v[m][k] = scale_j <A_j[k], x[m]>, j the adapter of token m.  A workgroup takes 16 tokens, one of
-// the adapters among them (blockIdx.x % 16; most find no such adapter and end) and 16 of the ranks; its
-// 16 waves share the row, each with loads of its own from memory to fragments, and are joined in LDS.
-// A product serves all 16 tokens, and those with another adapter are dropped.
-constexpr int kVWaves = 16;
+// v[m][k] = scale_j <A_j[k], x[m]>, j the adapter of token m.  A workgroup takes 16 tokens, 16 RC of
+// the ranks, and of the adapters among its tokens every lanes-th from the blockIdx.x % lanes-th on (one
+// each where there are few tokens, all of them where there are many); its waves share the row, each
+// with loads of its own from memory to fragments, and are joined in LDS.  A product serves all 16 tokens,
+// and those with another adapter are dropped.
+//
+// The last workgroups (one for each tile of bm tokens) make the plan of the product that reads v.
 struct AdapterV {
   const void* x;
   const void* a[2];
   void* v[2];
   const int32_t* ids;
   const float* scale;
-  int T, k, ldx, n, r, rp;
+  int32_t* plan;
+  int T, k, ldx, n, r, rp, lanes, blocks, bm;
 };
-template <class E>
-__global__ void __launch_bounds__(kVWaves * kWave) k_adapter_v(AdapterV p) {
+
+__device__ __forceinline__ int id_of(const AdapterV& p, int m) {
+  const int id = m < p.T ? p.ids[m] : -1;
+  return id >= 0 && id < p.n ? id : -1;
+}
+
+// Tile `tile` of the plan (LowRank): a token's first token with the same adapter, then that one's place
+// among the firsts.
+template <int THREADS>
+__device__ void make_plan(const AdapterV& p, int tile) {
+  __shared__ int ids[256], first[256], place[256], heads[4];
+  const int t = threadIdx.x, bm = p.bm;
+  if (t < 256) ids[t] = t < bm ? id_of(p, tile * bm + t) : -1;
+  __syncthreads();
+  if (t < 256) {
+    int f = t;
+    for (int s = 255; s >= 0; --s)
+      if (s < bm && ids[s] == ids[t] && s < f) f = s;
+    first[t] = ids[t] >= 0 ? f : -1;
+    const uint64_t b = __ballot(first[t] == t);
+    place[t] = rank_in_mask(b);
+    if (lane_id() == 0) heads[t / kWave] = __popcll(b);
+  }
+  __syncthreads();
+  int32_t* out = p.plan + (size_t)tile * (1 + 2 * bm);
+  if (t == 0) out[0] = heads[0] + heads[1] + heads[2] + heads[3];
+  if (t < bm) {
+    int at = -1;
+    if (first[t] >= 0) {
+      at = place[first[t]];
+      for (int w = 0; w < first[t] / kWave; ++w) at += heads[w];
+      if (first[t] == t) out[1 + at] = ids[t];
+    }
+    out[1 + bm + t] = at;
+  }
+}
+
+template <class E, int NW, int RC>
+__global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
   typedef typename E::T T;
-  __shared__ f32x4_t sum[kVWaves][kWave];
+  if ((int)blockIdx.x >= p.blocks) {
+    if (blockIdx.y == 0 && blockIdx.z == 0) make_plan<NW * kWave>(p, (int)blockIdx.x - p.blocks);
+    return;
+  }
+  __shared__ f32x4_t sum[NW][RC][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave;
-  const int m0 = (int)(blockIdx.x / 16) * 16, which = blockIdx.x % 16, k0 = blockIdx.y * 16;
-  const int m = m0 + (lane & 15);
-  int id = m < p.T ? p.ids[m] : -1;
-  if (id < 0 || id >= p.n) id = -1;
-  // the which-th adapter of the 16 tokens, in the order of its first token
+  const int m0 = (int)blockIdx.x / p.lanes * 16, k0 = blockIdx.y * 16 * RC;
+  const int m = m0 + (lane & 15), id = id_of(p, m);
   bool first = id >= 0 && lane < 16;
   for (int s = 0; s < 15; ++s)
     if (__shfl(id, s) == id && s < lane) first = false;
   uint64_t firsts = __ballot(first);
-  for (int s = 0; s < which && firsts; ++s) firsts &= firsts - 1;
-  if (!firsts) return;
-  const int j = __shfl(id, __ffsll((unsigned long long)firsts) - 1);
-
   const bool whole = p.k % E::EPC == 0;
-  const int col = k0 + (lane & 15), c0 = lane >> 4;
+  const int c0 = lane >> 4;
   const T* x = static_cast<const T*>(p.x) + (size_t)(m < p.T ? m : m0) * p.ldx;
-  const T* a = static_cast<const T*>(p.a[blockIdx.z]) + ((size_t)j * p.r + (col < p.r ? col : 0)) * p.k;
-  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   const int steps = (p.k + 4 * E::EPC - 1) / (4 * E::EPC);
-  constexpr int U = 8;  // steps in flight
-  for (int s0 = wave; s0 < steps; s0 += kVWaves * U) {
-    uint4 xv[U], av[U];
+  for (int w = 0; firsts; ++w) {
+    const int j = __shfl(id, __ffsll((unsigned long long)firsts) - 1);
+    firsts &= firsts - 1;
+    if (w % p.lanes != (int)blockIdx.x % p.lanes) continue;
+    const T* a[RC];
+    f32x4_t acc[RC];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = ((s0 + u * kVWaves) * 4 + c0) * E::EPC;
-      xv[u] = k < p.k ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
-      av[u] = load_part<E>(a + k, p.k - k, whole);
+    for (int c = 0; c < RC; ++c) {
+      const int col = k0 + 16 * c + (lane & 15);
+      a[c] = static_cast<const T*>(p.a[blockIdx.z]) + ((size_t)j * p.r + (col < p.r ? col : 0)) * p.k;
+      acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
+    constexpr int U = RC == 1 ? 8 : 4;  // steps in flight
+    for (int s0 = wave; s0 < steps; s0 += NW * U) {
+      uint4 xv[U], av[U][RC];
 #pragma unroll
-    for (int u = 0; u < U; ++u) acc = product<E>(av[u], xv[u], acc);
-  }
-  sum[wave][lane] = acc;
-  __syncthreads();
-  if (wave == 0 && id == j) {
-    for (int w = 1; w < kVWaves; ++w) acc += sum[w][lane];
-    const float sc = p.scale ? p.scale[j] : 1.f;
-    const int c = k0 + 4 * c0;
-    if (c < p.rp) {
+      for (int u = 0; u < U; ++u) {
+        const int k = ((s0 + u * NW) * 4 + c0) * E::EPC;
+        xv[u] = k < p.k ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = c + i < p.r ? acc[i] * sc : 0.f;
-      store4<E>(static_cast<T*>(p.v[blockIdx.z]) + (size_t)m * p.rp + c, acc);
+        for (int c = 0; c < RC; ++c) av[u][c] = load_part<E>(a[c] + k, p.k - k, whole);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int c = 0; c < RC; ++c) acc[c] = product<E>(av[u][c], xv[u], acc[c]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < RC; ++c) sum[wave][c][lane] = acc[c];
+    __syncthreads();
+    if (wave < RC && id == j) {
+      f32x4_t v = sum[0][wave][lane];
+      for (int s = 1; s < NW; ++s) v += sum[s][wave][lane];
+      const float sc = p.scale ? p.scale[j] : 1.f;
+      const int c = k0 + 16 * wave + 4 * c0;
+      if (c < p.rp) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = c + i < p.r ? v[i] * sc : 0.f;
+        store4<E>(static_cast<T*>(p.v[blockIdx.z]) + (size_t)m * p.rp + c, v);
+      }
     }
   }
+}
+
+template <class E>
+hipError_t adapter_v(AdapterV p, int count, hipStream_t st) {
+  const int tiles = ceil_div(p.T, 16), plans = ceil_div(p.T, p.bm);
+  if (tiles * count >= kCUs / 2) {
+    // many tokens: a workgroup for 16 of them and 64 ranks, all their adapters in turn
+    p.lanes = 1;
+    p.blocks = tiles;
+    k_adapter_v<E, 4, 4><<<dim3(p.blocks + plans, ceil_div(p.rp, 64), count), 4 * kWave, 0, st>>>(p);
+  } else {
+    p.lanes = p.T < 16 ? p.T : 16;
+    p.blocks = tiles * p.lanes;
+    k_adapter_v<E, 16, 1><<<dim3(p.blocks + plans, ceil_div(p.rp, 16), count), 16 * kWave, 0, st>>>(p);
+  }
+  return hipGetLastError();
 }
 
 template <class E>
@@ -176,17 +236,58 @@ __global__ void __launch_bounds__(kBlock) k_pad_rows(int64_t rows, int n, int np
 
 }  // namespace
 
-// Shares of a sum over `steps` steps: a product with too few tiles for the CUs is cut along k, so that
-// about two workgroups fall on a CU, but no share is under 4 steps (a share writes its whole tile in fp32).
-int token_splits(bool f32, int T, int n, int steps) {
-  const TokTile t = tile_for(f32, T, n);
-  if (t == TokTile::T256) return 1;
-  const int bm = t == TokTile::T16 ? 16 : t == TokTile::T64 ? 64 : 128;
-  const int64_t tiles = (int64_t)ceil_div(T, bm) * ceil_div(n, 128);
-  if (tiles >= kCUs) return 1;
-  int s = (int)(2 * kCUs / tiles);
-  if (s > steps / 4) s = steps / 4;
-  return s < 1 ? 1 : s > 32 ? 32 : s;
+int tile_rows(Tile t) {
+  switch (t) {
+    case Tile::T16: return Tile16::BM;
+    case Tile::T64: return Tile64::BM;
+    case Tile::T256: return Tile256::BM;
+    default: return Tile128::BM;
+  }
+}
+
+// By an estimate of the time, in us.  A product of more rows than a few tokens runs in rounds of tiles over
+// the CUs; a step of a round takes what was measured at sizes that fill the chip (two workgroups of 128 x
+// 128 share a CU; a lone one takes 0.66), a tile 6 us for its first loads and its stores.  Cutting the sum
+// in shares fills rounds that would stay empty; the shares' fp32 tiles are written and read once more, and
+// joined by a second launch.
+Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split) {
+  auto cut = [&](int64_t tiles, int slots, int least) {  // shares of at least `least` steps that fill the slots
+    int64_t s = split ? slots / tiles : 1;
+    if (s > steps / least) s = steps / least;
+    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+  };
+  auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
+  if (M <= 16) return Plan{Tile::T16, cut(tiles(16, 64), 2 * kCUs, 8)};
+  if (M <= 64 || f32) return Plan{Tile::T64, cut(tiles(64, 64), 2 * kCUs, 8)};
+  struct Kind {
+    Tile t;
+    int bm, bn, a_cu;
+    double step_us, lone_us;
+  };
+  static const Kind kinds[] = {{Tile::T256, 256, 256, 1, 1.45, 1.45},
+                               {Tile::T128x256, 128, 256, 1, 0.82, 0.82},
+                               {Tile::T128, 128, 128, 2, 1.04, 0.66}};
+  Plan best{Tile::T256, 1};
+  double least = 1e30;
+  for (const Kind& k : kinds) {
+    const int64_t nt = tiles(k.bm, k.bn);
+    const int s = cut(nt, kCUs * k.a_cu, 16);
+    const int64_t rounds = (nt * s + kCUs * k.a_cu - 1) / (kCUs * k.a_cu);
+    const double step = nt * s <= kCUs ? k.lone_us : k.step_us;
+    const double us = rounds * (step * ((steps + s - 1) / s) + 6.0) + (s > 1 ? 5.0 + 8e-6 * (double)(M * n) * s / 5.0 : 0.0);
+    if (us < least) {
+      least = us;
+      best = Plan{k.t, s};
+    }
+  }
+  return best;
+}
+
+Plan token_plan(bool f32, int T, int n, int k, int products) {
+  return choose_tile(f32, T, n, products * ceil_div(k, f32 ? step_k<EF32>() : step_k<EBf16>()), true);
+}
+Plan hidden_plan(bool f32, const BlockShape& s) {
+  return choose_tile(f32, s.T, 2 * (int64_t)s.d_ff, ceil_div(s.d, f32 ? step_k<EF32>() : step_k<EBf16>()), false);
 }
 
 hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st) {
@@ -197,12 +298,9 @@ hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t 
 }
 
 hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
-                            const void* const a[2], void* const v[2], hipStream_t st) {
-  const AdapterV p{x, {a[0], a[1]}, {v[0], v[1]}, ad.ids, ad.scale, T, k, ldx, ad.n, ad.r, ad.rp};
-  const dim3 grid(ceil_div(T, 16) * 16, ceil_div(ad.rp, 16), count);
-  if (f32) k_adapter_v<EF32><<<grid, kVWaves * kWave, 0, st>>>(p);
-  else k_adapter_v<EBf16><<<grid, kVWaves * kWave, 0, st>>>(p);
-  return hipGetLastError();
+                            const void* const a[2], void* const v[2], Tile t, hipStream_t st) {
+  const AdapterV p{x, {a[0], a[1]}, {v[0], v[1]}, ad.ids, ad.scale, ad.plan, T, k, ldx, ad.n, ad.r, ad.rp, 0, 0, tile_rows(t)};
+  return f32 ? adapter_v<EF32>(p, count, st) : adapter_v<EBf16>(p, count, st);
 }
 
 hipError_t launch_pad_rows(bool f32, int64_t rows, int n, int np, const void* src, void* dst, hipStream_t st) {

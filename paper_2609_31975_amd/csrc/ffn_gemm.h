@@ -56,13 +56,16 @@ struct Operand {
   int rows;
 };
 
-// Adapters of a product (see ffn_adapter.h for v): B_j of adapter j is b + j out r, [out][r], and
-// token m adds sum over k of v[m][k] B_ids[m][n][k].  rp: r in whole chunks, the row length of v.
+// Adapters of a product: token m adds sum over k of v[m][k] B_j[n][k] for its adapter j, with
+// v = scale_j A_j x computed before (k_adapter_v) and B_j = b + j out r, [out][r].  rp: r in whole
+// chunks, the row length of v.  plan: for every tile of BM tokens 1 + 2 BM entries, the number of
+// adapters among its tokens, those adapters in the order of their first token, and every token's place
+// in that list (-1: none).  Index 1 of v and b is W_up's, of a dual product.
 struct LowRank {
   const void* v[2];
   const void* b[2];
-  const int32_t* ids;
-  int n, r, rp, out;
+  const int32_t* plan;
+  int r, rp, out;
 };
 
 struct GemmArgs {
@@ -88,6 +91,14 @@ enum class Lay { KC, KS };
 __device__ __forceinline__ void lds_load16(const Buf& b, char* dst, uint32_t off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(b.r, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
 }
+
+// The same from an address of each lane's own.
+__device__ __forceinline__ void lds_load16(const void* p, char* dst) {
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)p,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+// what a lane with nothing to load reads there
+__device__ const uint4 zero_chunk = {0, 0, 0, 0};
 
 // Waits until at most n of this wave's loads are in flight and its LDS reads have returned.
 template <int n>
@@ -246,6 +257,17 @@ struct Half {
   }
 };
 
+// up to EPC elements from p, the rest zero
+template <class E>
+__device__ __forceinline__ uint4 load_part(const typename E::T* p, int n, bool whole) {
+  if (n <= 0) return make_uint4(0, 0, 0, 0);
+  if (whole) return *reinterpret_cast<const uint4*>(p);
+  typename E::T v[E::EPC];
+#pragma unroll
+  for (int i = 0; i < E::EPC; ++i) v[i] = i < n ? p[i] : (typename E::T)0.f;
+  return __builtin_bit_cast(uint4, v);
+}
+
 // ------------------------------------------------------------------ activations
 // A(g), and with its derivative; the same of the up side.  A gate value that is not above zero (NaN
 // too) gives zero and slope zero, but for SiLU.
@@ -298,75 +320,126 @@ __device__ __forceinline__ TileAt tile_at(const GemmArgs& g) {
   return TileAt{band * kBand + u % rows, u / rows, split};
 }
 
-// ------------------------------------------------------------------ adapters within a product
-// The adapters of a tile's tokens, each once, in the order of their first token, in LDS, and every
-// token's place in that list (-1: none).  All threads call it.
-template <int BM>
-struct AdapterTile {
-  int ids[BM], list[BM], slot[BM], count;
+// ------------------------------------------------------------------ the pipeline
+// Steps [it0, it1) into acc.  issue(f0, f1, it, buf): loads f0 .. f1 - 1 of this wave's PER for step `it`
+// into buffer `buf`; from it1 on they have to be zeros or anything else that nothing uses, so that
+// every step has the same loads in flight.
+//
+// Half a step's fragments are read while the other half's products run: the second half of step i
+// during the first half's products, the first half of step i + 1, behind the barrier that frees step i's
+// buffer, during the second half's, and with it step i + S is loaded into that buffer.
+template <class E, class C, Lay LA, Lay LB, int PER, class Issue>
+__device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Reader<E, LA, C::BM, C::MT>& ra,
+                                         const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT],
+                                         Issue issue) {
+#pragma unroll
+  for (int i = 0; i < C::S; ++i) issue(0, PER, it0 + i, i);
+  wait_loads<(C::S - 1) * PER>();
+  meet();
+  Half<E, C, LA, LB> h0, h1;
+  h0.load(0, h0.count, lds, 0, ra, rb);
+  int buf = 0;
+  for (int it = it0; it < it1; ++it) {
+    h0.multiply(acc, [&](int i) {
+      h1.load(i * h1.count / C::MT, (i + 1) * h1.count / C::MT, lds + buf * C::stage, 1, ra, rb);
+    });
+    wait_loads<(C::S - 2) * PER>();
+    meet();
+    const int next = buf + 1 == C::S ? 0 : buf + 1;
+    h1.multiply(acc, [&](int i) {
+      h0.load(i * h0.count / C::MT, (i + 1) * h0.count / C::MT, lds + next * C::stage, 0, ra, rb);
+      issue(i * PER / C::MT, (i + 1) * PER / C::MT, it + C::S, buf);
+    });
+    buf = next;
+  }
+  wait_loads<0>();  // LDS is free for others once no load into it is in flight
+}
 
-  __device__ void build(const LowRank& lr, int m0, int M) {
-    const int t = threadIdx.x;
-    if (t < BM) {
-      const int id = m0 + t < M ? lr.ids[m0 + t] : -1;
-      ids[t] = id >= 0 && id < lr.n ? id : -1;
+// ------------------------------------------------------------------ adapters within a product
+// The low-rank part is a product over k = (adapter of the tile, rank), rp to an adapter, in chunks:
+// row m of the A tile holds v[m] in its own adapter's chunks and zero in the others, row n of the B tile
+// B_j[n].  A dual product runs W_gate's adapters, with zeros in W_up's rows of the B tile, then
+// W_up's.  Both images are KC.
+//
+// Rows of whole chunks are loaded into LDS some steps ahead, each lane from an address of its own; odd
+// ranks are read by element and written to LDS, a step at a time.
+template <class E, class C, bool DUAL>
+struct AdapterSteps {
+  typedef typename E::T T;
+  static constexpr int G = C::WTN / 2;
+  typedef Loader<E, Lay::KC, C::BM, C::NW> LdA;
+  typedef Loader<E, Lay::KC, C::BN, C::NW> LdB;
+  static constexpr int per = LdA::per + LdB::per;
+  const LowRank& lr;
+  const int32_t* plan;  // the tile's, in LDS
+  int m0, n0, cpr, chunks, steps;  // steps of one matrix's adapters
+
+  __device__ __forceinline__ AdapterSteps(const LowRank& l, int32_t* lds_plan, int tile, int m0_, int n0_)
+      : lr(l), plan(lds_plan), m0(m0_), n0(n0_), cpr(l.rp / E::EPC) {
+    const int32_t* p = l.plan + (size_t)tile * (1 + 2 * C::BM);
+    for (int i = threadIdx.x; i < 1 + 2 * C::BM; i += C::threads) lds_plan[i] = p[i];
+    __syncthreads();
+    chunks = uniform(plan[0]) * cpr;
+    steps = (chunks + 7) / 8;
+  }
+  __device__ __forceinline__ int count() const { return (lr.b[0] ? steps : 0) + (DUAL && lr.b[1] ? steps : 0); }
+  // the matrix of step `it`, and the step within its adapters
+  __device__ __forceinline__ int matrix(int it) const { return DUAL && (!lr.b[0] || it >= steps) ? 1 : 0; }
+  __device__ __forceinline__ int within(int it) const { return lr.b[0] && it >= steps ? it - steps : it; }
+  __device__ __forceinline__ const T* v_at(int which, int m, int part) const {
+    return static_cast<const T*>(lr.v[which]) + (size_t)m * lr.rp + part * E::EPC;
+  }
+  __device__ __forceinline__ const T* b_at(int which, int j, int n, int part) const {
+    return static_cast<const T*>(lr.b[which]) + ((size_t)j * lr.out + n) * lr.r + part * E::EPC;
+  }
+  __device__ __forceinline__ int neuron(int r) const { return n0 + (DUAL ? r / C::WTN * G + r % G : r); }
+  __device__ __forceinline__ bool has(int which, int r) const { return !DUAL || (r % C::WTN >= G) == (which == 1); }
+
+  __device__ __forceinline__ void issue(int it, int it1, char* stage) const {
+    const int wave = uniform(threadIdx.x / kWave), lane = lane_id(), c = (lane & 7) ^ (lane >> 3);
+    const int which = matrix(it), q = within(it) * 8 + c;
+    const bool on = it < it1 && q < chunks;
+    const int slot = on ? q / cpr : 0, part = q - slot * cpr, j = plan[1 + slot];
+#pragma unroll
+    for (int f = 0; f < per; ++f) {
+      if (f < LdA::per) {
+        const int i = LdA::instr(f, wave), r = i * 8 + (lane >> 3);
+        const bool mine = on && plan[1 + C::BM + r] == slot;
+        lds_load16(mine ? static_cast<const void*>(v_at(which, m0 + r, part)) : &zero_chunk, stage + i * 1024);
+      } else {
+        const int i = LdB::instr(f - LdA::per, wave), r = i * 8 + (lane >> 3), n = neuron(r);
+        const bool mine = on && has(which, r) && n < lr.out;
+        lds_load16(mine ? static_cast<const void*>(b_at(which, j, n, part)) : &zero_chunk,
+                   stage + C::BM * 128 + i * 1024);
+      }
     }
-    __syncthreads();
-    int first = -1;  // the first token with this token's adapter
-    if (t < BM && ids[t] >= 0) {
-      first = t;
-      for (int s = 0; s < t; ++s)
-        if (ids[s] == ids[t]) {
-          first = s;
-          break;
-        }
+  }
+
+  __device__ __forceinline__ void fill(int it, char* stage) const {
+    const int which = matrix(it), q0 = within(it) * 8;
+    for (int s = threadIdx.x; s < (C::BM + C::BN) * 8; s += C::threads) {
+      const int row = s >> 3, c = s & 7, q = q0 + c, slot = q < chunks ? q / cpr : 0, part = q - slot * cpr;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (row < C::BM) {
+        if (q < chunks && plan[1 + C::BM + row] == slot) x = *reinterpret_cast<const uint4*>(v_at(which, m0 + row, part));
+      } else {
+        const int r = row - C::BM, n = neuron(r);
+        if (q < chunks && has(which, r) && n < lr.out)
+          x = load_part<E>(b_at(which, plan[1 + slot], n, part), lr.r - part * E::EPC, false);
+      }
+      *reinterpret_cast<uint4*>(stage + row * 128 + ((c ^ (row & 7)) << 4)) = x;
     }
-    if (t < BM) slot[t] = first;  // for now
-    __syncthreads();
-    int place = -1;
-    if (first >= 0) {
-      place = 0;
-      for (int s = 0; s < first; ++s) place += slot[s] == s;
-      if (first == t) list[place] = ids[t];
-    }
-    int n = 0;
-    if (t == 0)
-      for (int s = 0; s < BM; ++s) n += slot[s] == s;
-    __syncthreads();
-    if (t < BM) slot[t] = place;
-    if (t == 0) count = n;
-    __syncthreads();
   }
 };
-
-// One step of the low-rank part: its k runs over (adapter of the tile, rank), rp to an adapter, in
-// chunks; row m of the A tile holds v[m] in its own adapter's chunks and zero in the others, row n of
-// the B tile B_j[n].  The pieces of a row lie at unrelated addresses, so they pass through registers;
-// they are few.  Both images are KC.
-template <class E, int ROWS, int THREADS, class Get>
-__device__ __forceinline__ void fill_kc(char* dst, Get get) {
-  for (int s = threadIdx.x; s < ROWS * 8; s += THREADS) {
-    const int r = s >> 3, c = s & 7;
-    *reinterpret_cast<uint4*>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = get(r, c);
-  }
-}
-// up to EPC elements from p, the rest zero
-template <class E>
-__device__ __forceinline__ uint4 load_part(const typename E::T* p, int n, bool whole) {
-  if (n <= 0) return make_uint4(0, 0, 0, 0);
-  if (whole) return *reinterpret_cast<const uint4*>(p);
-  typename E::T v[E::EPC];
-#pragma unroll
-  for (int i = 0; i < E::EPC; ++i) v[i] = i < n ? p[i] : (typename E::T)0.f;
-  return __builtin_bit_cast(uint4, v);
-}
 
 // ------------------------------------------------------------------ the kernel
 // DUAL: B's tile holds W_gate and W_up rows of the same BN / 2 neurons, a wave's columns being half of
 // either, so that its lanes end with both values of their neurons.  AD: adapters.
 template <class E, class C, Lay LA, Lay LB, bool DUAL, bool AD, class Epi>
 __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
-  __shared__ __align__(1024) char lds[C::S * C::stage];
+  // One array for all: with a second one the compiler marks the accesses of either, and with the marks it
+  // takes every LDS read to wait for the loads in flight (see lds_read16).
+  __shared__ __align__(1024) char lds[C::S * C::stage + (AD ? (1 + 2 * C::BM) * 4 : 0)];
   constexpr int G = C::WTN / 2;  // neurons of a wave, dual
   constexpr int BNN = DUAL ? C::BN / 2 : C::BN;
   const TileAt at = tile_at(g);
@@ -416,71 +489,42 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
 
   const Reader<E, LA, C::BM, C::MT> ra(wm * C::WTM);
   const Reader<E, LB, C::BN, C::NT> rb(wn * C::WTN);
-  // Half a step's fragments are read while the other half's products run: the second half of step i
-  // during the first half's products, the first half of step i + 1, behind the barrier that frees step
-  // i's buffer, during the second half's, and with it step i + S is loaded into that buffer.
-#pragma unroll
-  for (int i = 0; i < C::S; ++i) issue(0, per_step, it0 + i, i);
-  wait_loads<(C::S - 1) * per_step>();
-  meet();
-  Half<E, C, LA, LB> h0, h1;
-  h0.load(0, h0.count, lds, 0, ra, rb);
-  int buf = 0;
-  for (int it = it0; it < it1; ++it) {
-    h0.multiply(acc, [&](int i) {
-      h1.load(i * h1.count / C::MT, (i + 1) * h1.count / C::MT, lds + buf * C::stage, 1, ra, rb);
-    });
-    wait_loads<(C::S - 2) * per_step>();
-    meet();
-    const int next = buf + 1 == C::S ? 0 : buf + 1;
-    h1.multiply(acc, [&](int i) {
-      h0.load(i * h0.count / C::MT, (i + 1) * h0.count / C::MT, lds + next * C::stage, 0, ra, rb);
-      issue(i * per_step / C::MT, (i + 1) * per_step / C::MT, it + C::S, buf);
-    });
-    buf = next;
-  }
-  wait_loads<0>();  // LDS is free for others once no load into it is in flight
+  pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
 
   if constexpr (AD) {
-    __shared__ AdapterTile<C::BM> ad;
-    if (at.split == g.splits - 1) {
-      ad.build(g.lr, m0, g.M);
-      const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
-      const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);
-      typedef typename E::T T;
-      const LowRank& lr = g.lr;
-      const int cpr = lr.rp / E::EPC, chunks = ad.count * cpr;
-      const bool whole = lr.r % E::EPC == 0;
-      // a dual product's v differ too: W_gate's adapters first, then W_up's, against rows of the other
-      // matrix that are zero
-      for (int which = 0; which < (DUAL ? 2 : 1); ++which) {
-        if (!lr.b[which]) continue;
-        for (int c0 = 0; c0 < chunks; c0 += 8) {
-          __syncthreads();
-          fill_kc<E, C::BM, C::threads>(lds, [&](int r, int c) {
-            const int q = c0 + c, slot = q / cpr, part = q - slot * cpr;
-            const bool mine = q < chunks && ad.slot[r] == slot;
-            const T* v = static_cast<const T*>(lr.v[which]) + (size_t)(m0 + r) * lr.rp + part * E::EPC;
-            return mine ? *reinterpret_cast<const uint4*>(v) : make_uint4(0, 0, 0, 0);
-          });
-          fill_kc<E, C::BN, C::threads>(lds + C::BM * 128, [&](int r, int c) {
-            const int q = c0 + c, slot = q / cpr, part = q - slot * cpr;
-            const int n = n0 + (DUAL ? r / C::WTN * G + r % G : r);
-            const bool on = q < chunks && n < lr.out && (!DUAL || (r % C::WTN >= G) == (which == 1));
-            const T* b = static_cast<const T*>(lr.b[which]) +
-                         ((size_t)(on ? ad.list[slot] : 0) * lr.out + (on ? n : 0)) * lr.r + part * E::EPC;
-            return load_part<E>(b, on ? lr.r - part * E::EPC : 0, whole);
-          });
-          __syncthreads();
-          Half<E, C, Lay::KC, Lay::KC> h;
+    typedef AdapterSteps<E, C, DUAL> Steps;
+    int32_t* plan = reinterpret_cast<int32_t*>(lds + C::S * C::stage);
+    const Steps ad(g.lr, plan, at.m, m0, n0);  // behind its barrier the last step of the main part has been read
+    const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
+    const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);
+    const Split part(ad.count(), g.splits);
+    const int ad0 = part.start(at.split), ad1 = part.start(at.split + 1);
+    const bool whole = g.lr.r % E::EPC == 0;
+    constexpr int ahead = C::S - 1;
+    if (whole && ad0 < ad1) {
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) {
-            h.load(0, h.count, lds, kk, rva, rvb);
-            h.multiply(acc, [](int) {});
-          }
-        }
-      }
+      for (int i = 0; i < ahead; ++i) ad.issue(ad0 + i, ad1, lds + i * C::stage);
     }
+    int buf = 0;
+    for (int it = ad0; it < ad1; ++it) {
+      if (whole) {
+        wait_loads<(ahead - 1) * Steps::per>();
+        meet();
+        ad.issue(it + ahead, ad1, lds + (buf == 0 ? ahead : buf - 1) * C::stage);
+      } else {
+        __syncthreads();
+        ad.fill(it, lds + buf * C::stage);
+        __syncthreads();
+      }
+      Half<E, C, Lay::KC, Lay::KC> h;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        h.load(0, h.count, lds + buf * C::stage, kk, rva, rvb);
+        h.multiply(acc, [](int) {});
+      }
+      buf = buf + 1 == C::S ? 0 : buf + 1;
+    }
+    wait_loads<0>();
   }
 
   // lane l of a 16 x 16 tile: m = l % 16, n = 4 (l / 16) .. + 3

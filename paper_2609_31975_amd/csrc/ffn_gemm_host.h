@@ -8,10 +8,17 @@ namespace ffn {
 namespace {
 
 // Tiles: tokens (or weight-gradient rows) x columns, waves, steps in LDS.
-typedef Config<16, 128, 1, 4, 4> TileT16;    // a decode step: weights streamed, 3 steps in flight
-typedef Config<64, 128, 1, 4, 4> TileT64;
-typedef Config<128, 128, 2, 2, 2> TileT128;
-typedef Config<256, 256, 2, 4, 2> TileT256;
+//   16, 64      a few tokens: the weights are streamed past them, 3 steps in flight, 2 to 4 workgroups a
+//               CU (28672 x 4096 weights, 1..48 tokens: 36 to 38 us, 6.4 TB/s; 128 columns a tile 38 to 40)
+//   64 (fp32)   any number of tokens: the fp32 products bound it (4096^3: 134 TFLOP/s, the card's library
+//               product 133), and small tiles waste the least of odd sizes
+//   128, 128x256, 256  bf16, many tokens: 1030, 1150 and 1300 TFLOP/s where the tiles fill the chip
+//               (8192 x 4096 x 14336; the card's library product reaches 1360 to 1480)
+typedef Config<16, 64, 1, 2, 4> Tile16;
+typedef Config<64, 64, 2, 2, 4> Tile64;
+typedef Config<128, 128, 2, 2, 2> Tile128;
+typedef Config<128, 256, 2, 4, 3> Tile128x256;
+typedef Config<256, 256, 2, 4, 2> Tile256;
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -37,7 +44,24 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
 }
 
 inline LowRank low_rank(const AdapterSet& ad, const void* const v[2], const void* const b[2], int out) {
-  return LowRank{{v[0], v[1]}, {b[0], b[1]}, ad.ids, ad.n, ad.r, ad.rp, out};
+  return LowRank{{v[0], v[1]}, {b[0], b[1]}, ad.plan, ad.r, ad.rp, out};
+}
+
+// f(Config{}) for the tile that choose_tile picked
+template <class E, class F>
+hipError_t with_tile(Tile t, F f) {
+  switch (t) {
+    case Tile::T16: return f(Tile16{});
+    case Tile::T64: return f(Tile64{});
+    default: break;
+  }
+  if constexpr (E::EPC == 8) {
+    if (t == Tile::T128) return f(Tile128{});
+    if (t == Tile::T128x256) return f(Tile128x256{});
+    return f(Tile256{});
+  } else {
+    return hipErrorInvalidValue;  // not reached: fp32 products take the two tiles above
+  }
 }
 
 }  // namespace
