@@ -63,14 +63,20 @@ size_t save_layout(ffn_dtype_t w, int T, int d_ff, void* base, Save* out) {
   return c.off;
 }
 
-size_t part_bytes(ffn_dtype_t w, int T, int n, int k, int products) {
-  const int s = token_plan(w == FFN_F32, T, n, k, products).splits;
+size_t part_bytes(ffn_dtype_t w, int T, int n, int k, int products, bool adapters) {
+  const int s = token_plan(w == FFN_F32, T, n, k, products, adapters).splits;
   return s > 1 ? (size_t)s * T * round_up_to(n, 4) * 4 : 0;
+}
+
+// The largest sums of shares of the adapters' first factors; a call's two products take turns.
+size_t shares_bytes(ffn_dtype_t w, int T, int k, int rp, int count) {
+  const int s = adapter_shares(w == FFN_F32, T, k, rp, count);
+  return s > 1 ? (size_t)s * count * T * rp * 4 : 0;
 }
 
 struct ForwardWs {
   void *z, *v[2], *v2, *x, *w_gate, *w_up, *w_down;
-  float* part;
+  float *part, *shares;
   int32_t* plan;
 };
 size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, ForwardWs* out) {
@@ -82,8 +88,12 @@ size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Fo
     for (void*& v : f.v) v = c.take(e * s.T * rp);
     f.v2 = c.take(e * s.T * rp);
     f.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
+    const size_t both = std::max(shares_bytes(w, s.T, s.d, rp, 1), shares_bytes(w, s.T, s.d, rp, 2));
+    f.shares = static_cast<float*>(c.take(std::max(both, shares_bytes(w, s.T, s.d_ff, rp, 1))));
   }
-  f.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d, s.d_ff, 1)));
+  // with adapters, which may be of the gate and the up projection alone, the larger of both
+  f.part = static_cast<float*>(c.take(std::max(part_bytes(w, s.T, s.d, s.d_ff, 1, false),
+                                               rp ? part_bytes(w, s.T, s.d, s.d_ff, 1, true) : 0)));
   if (s.dp != s.d) {
     f.x = c.take(e * s.T * s.dp);
     f.w_gate = c.take(e * s.d_ff * s.dp);
@@ -104,7 +114,7 @@ size_t backward_layout(ffn_dtype_t w, const BlockShape& s, void* base, BackwardW
   const size_t e = esize(w);
   b.dg = c.take(e * s.T * s.ldf);
   b.dv = c.take(e * s.T * s.ldf);
-  b.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d, s.d_ff, 2)));
+  b.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d, s.d_ff, 2, false)));
   if (s.dp != s.d) {
     b.x = c.take(e * s.T * s.dp);
     b.dy = c.take(e * s.T * s.dp);
@@ -118,7 +128,7 @@ size_t backward_layout(ffn_dtype_t w, const BlockShape& s, void* base, BackwardW
 
 struct AdapterWs {
   void *v, *x, *w;
-  float* part;
+  float *part, *shares;
   int32_t* plan;
 };
 size_t adapter_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, AdapterWs* out) {
@@ -127,7 +137,8 @@ size_t adapter_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Ad
   const size_t e = esize(w);
   a.v = c.take(e * s.T * rp);
   a.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
-  a.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d_ff, s.d, 1)));
+  a.shares = static_cast<float*>(c.take(shares_bytes(w, s.T, s.d, rp, 1)));
+  a.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d_ff, s.d, 1, true)));
   if (s.dp != s.d) {
     a.x = c.take(e * s.T * s.dp);
     a.w = c.take(e * s.d_ff * s.dp);
@@ -225,6 +236,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   Save sv{nullptr, nullptr, f.z};
   if (save && save_bytes < save_layout(wdt, T, d_ff, save, &sv)) return FFN_ERR_WORKSPACE;
   set.plan = f.plan;
+  set.part = f.shares;
 
   const bool f32 = wdt == FFN_F32;
   FFN_TRY(padded(f32, s, T, &x, f.x, stream));
@@ -237,7 +249,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   if (b2[0] || b2[1]) {
     const void* a[2] = {b2[0] ? ad->gate_a : ad->up_a, ad->up_a};
     void* v[2] = {b2[0] ? f.v[0] : f.v[1], f.v[1]};
-    FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, hidden_plan(f32, s).tile, stream));
+    FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, hidden_plan(f32, s, true).tile, stream));
   }
   AdapterSet hidden = b2[0] || b2[1] ? set : AdapterSet{};
   FFN_TRY(launch_block_hidden(f32, s, x, w_gate, w_up, form, hidden, v2, b2, sv.z, sv.g, sv.v, stream));
@@ -245,7 +257,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
   if (down) {
     const void* a[2] = {ad->down_a, nullptr};
     void* v[2] = {f.v2, nullptr};
-    FFN_TRY(launch_adapter_v(f32, T, d_ff, s.ldf, sv.z, set, 1, a, v, token_plan(f32, T, d, d_ff, 1).tile, stream));
+    FFN_TRY(launch_adapter_v(f32, T, d_ff, s.ldf, sv.z, set, 1, a, v, token_plan(f32, T, d, d_ff, 1, true).tile, stream));
   }
   const TokenProduct p{{sv.z, nullptr}, {w_down_t, nullptr}, 1, T, d, d_ff, s.ldf, s.dp, d, y, f.part,
                        down ? set : AdapterSet{}, f.v2, down ? ad->down_b : nullptr};
@@ -314,12 +326,13 @@ int ffn_adapter_forward(ffn_dtype_t wdt, int T, int d, int n_out, const void* x,
   AdapterWs a;
   if (ws_bytes < adapter_layout(wdt, s, set.rp, ws, &a)) return FFN_ERR_WORKSPACE;
   set.plan = a.plan;
+  set.part = a.shares;
   const bool f32 = wdt == FFN_F32;
   FFN_TRY(padded(f32, s, T, &x, a.x, stream));
   FFN_TRY(padded(f32, s, n_out, &w, a.w, stream));
   const void* aa[2] = {ad->gate_a, nullptr};
   void* v[2] = {a.v, nullptr};
-  FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, 1, aa, v, token_plan(f32, T, n_out, d, 1).tile, stream));
+  FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, 1, aa, v, token_plan(f32, T, n_out, d, 1, true).tile, stream));
   const TokenProduct p{{x, nullptr}, {w, nullptr}, 1, T, n_out, d, s.dp, s.dp, n_out, y, a.part, set, a.v, ad->gate_b};
   FFN_TRY(launch_token_product_kc(f32, p, stream));
   return FFN_OK;

@@ -71,7 +71,7 @@ hipError_t dz(const BlockShape& s, const void* dy, const void* w_down_t, const B
   a.products = 1;
   a.splits = 1;
   const EpiDz<E> epi{form, s.d_ff, s.ldf, g, v, static_cast<typename E::T*>(dg), static_cast<typename E::T*>(dv)};
-  const Plan p = choose_tile(E::EPC == 4, s.T, s.ldf, ceil_div(s.d, step_k<E>()), false);
+  const Plan p = choose_tile(E::EPC == 4, s.T, s.ldf, ceil_div(s.d, step_k<E>()), false, false);
   return with_tile<E>(p.tile, [&](auto c) {
     return launch_gemm<E, decltype(c), Lay::KC, Lay::KC, false, false>(a, epi, 1, st);
   });
@@ -97,7 +97,7 @@ hipError_t dw(const BlockShape& s, int count, const void* const a[3], const void
   epi.ldo = s.d;
   epi.vec = s.d % 4 == 0;
   // rows of all gradients: their tiles are in one launch
-  const Plan p = choose_tile(E::EPC == 4, (int64_t)count * s.d_ff, s.d, ceil_div(s.T, step_k<E>()), false);
+  const Plan p = choose_tile(E::EPC == 4, (int64_t)count * s.d_ff, s.d, ceil_div(s.T, step_k<E>()), false, false);
   return with_tile<E>(p.tile == Tile::T16 ? Tile::T64 : p.tile, [&](auto c) {
     typedef decltype(c) C;
     if constexpr (C::BM >= 64) return launch_gemm<E, C, Lay::KS, Lay::KS, false, false>(g, epi, count, st);

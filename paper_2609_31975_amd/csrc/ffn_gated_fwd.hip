@@ -45,10 +45,11 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
   a.splits = 1;
   if (ad.plan) a.lr = low_rank(ad, v2, b2, s.d_ff);
   const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
-  return with_tile<E>(hidden_plan(E::EPC == 4, s).tile, [&](auto c) {
+  return with_tile<E>(hidden_plan(E::EPC == 4, s, ad.plan != nullptr).tile, [&](auto c) {
     typedef decltype(c) C;
-    return a.lr.plan ? launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st)
-                     : launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
+    if constexpr (C::BM <= 128)
+      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st);
+    return launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
   });
 }
 

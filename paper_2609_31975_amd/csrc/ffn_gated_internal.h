@@ -21,6 +21,7 @@ struct AdapterSet {
   const int32_t* ids = nullptr;
   const float* scale = nullptr;
   int32_t* plan = nullptr;  // room for plan_ints(T); filled by launch_adapter_v
+  float* part = nullptr;    // room for adapter_shares(...) x count x T x rp where there are several
 };
 
 // The tile of a product with M rows and n columns over `steps` steps of 128 bytes, and the shares its sum is
@@ -30,7 +31,7 @@ struct Plan {
   Tile tile;
   int splits;
 };
-Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split);
+Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters);
 int tile_rows(Tile t);
 // Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.
 inline size_t plan_ints(int T) { return 2 * ((size_t)T + 256) + T / 16 + 1; }
@@ -56,8 +57,8 @@ struct TokenProduct {
   const void* v;
   const void* ab;
 };
-Plan token_plan(bool f32, int T, int n, int k, int products);
-Plan hidden_plan(bool f32, const BlockShape& s);
+Plan token_plan(bool f32, int T, int n, int k, int products, bool adapters);
+Plan hidden_plan(bool f32, const BlockShape& s, bool adapters);
 hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st);
 hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t st);
 // dg, dv [T][ldf] from dz = dy W2 and the saved g, v.
@@ -66,6 +67,8 @@ hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const 
 // up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
                            void* const out[3], hipStream_t st);
+// Shares that the rows of k elements are cut into, of `count` stacks.
+int adapter_shares(bool f32, int T, int k, int rp, int count);
 // v[i] [T][rp] = scale_j A_j x for up to two stacks, and ad.plan for the product of tile `t` that reads them
 hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
                             const void* const a[2], void* const v[2], Tile t, hipStream_t st);

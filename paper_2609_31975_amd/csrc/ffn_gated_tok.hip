@@ -3,6 +3,22 @@
 #include "ffn_gemm_host.h"
 
 namespace ffn {
+
+// Whether a workgroup of the adapters' first factor takes 16 tokens and 64 ranks, all the tokens'
+// adapters in turn, or one of the adapters and 16 ranks.
+static bool many_tokens(int T, int count) { return (T + 15) / 16 * count >= kCUs / 2; }
+
+// Shares of a row, at most 8 (k_adapter_join), so that two workgroups come to a CU; a share is at
+// least half a round of loads of its 16 waves.
+int adapter_shares(bool f32, int T, int k, int rp, int count) {
+  if (many_tokens(T, count)) return 1;
+  const int steps = (k + (f32 ? 15 : 31)) / (f32 ? 16 : 32);
+  const int groups = (T + 15) / 16 * (T < 16 ? T : 16) * ((rp + 15) / 16) * count;
+  int s = 2 * kCUs / groups;
+  if (s > steps / 64) s = steps / 64;
+  return s < 1 ? 1 : s > 8 ? 8 : s;
+}
+
 namespace {
 
 template <class E>
@@ -68,7 +84,7 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   a.N = p.n;
   a.K = p.k;
   a.products = p.products;
-  const Plan plan = token_plan(E::EPC == 4, p.T, p.n, p.k, p.products);
+  const Plan plan = token_plan(E::EPC == 4, p.T, p.n, p.k, p.products, p.ad.plan != nullptr);
   a.splits = plan.splits;
   const void *v[2] = {p.v, nullptr}, *b[2] = {p.ab, nullptr};
   if (p.ad.plan) a.lr = low_rank(p.ad, v, b, p.n);
@@ -76,8 +92,9 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.part, p.ldo, np, p.n % 4 == 0};
   hipError_t e = with_tile<E>(plan.tile, [&](auto c) {
     typedef decltype(c) C;
-    return a.lr.plan ? launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st)
-                     : launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
+    if constexpr (C::BM <= 128)
+      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st);
+    return launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
   });
   if (e == hipSuccess && a.splits > 1) {
     const int64_t quads = (int64_t)p.T * np / 4;
@@ -95,7 +112,12 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
 // with loads of its own from memory to fragments, and are joined in LDS.  A product serves all 16 tokens,
 // and those with another adapter are dropped.
 //
-// The last workgroups (one for each tile of bm tokens) make the plan of the product that reads v.
+// Few tokens leave most CUs without a workgroup, and one CU alone reads a row slowly, so the row is cut
+// in `shares` too: these write fp32 sums, and k_adapter_join adds them up (16 tokens with an adapter each,
+// rank 16, rows of 14336: 33 us in one share, 11 us in 7).
+//
+// With one share the last workgroups (one for each tile of bm tokens) make the plan of the product
+// that reads v; else k_adapter_join does.
 struct AdapterV {
   const void* x;
   const void* a[2];
@@ -103,7 +125,8 @@ struct AdapterV {
   const int32_t* ids;
   const float* scale;
   int32_t* plan;
-  int T, k, ldx, n, r, rp, lanes, blocks, bm;
+  float* part;  // [shares][count][T][rp]
+  int T, k, ldx, n, r, rp, lanes, blocks, bm, shares, count;
 };
 
 __device__ __forceinline__ int id_of(const AdapterV& p, int m) {
@@ -112,19 +135,20 @@ __device__ __forceinline__ int id_of(const AdapterV& p, int m) {
 }
 
 // Tile `tile` of the plan (LowRank): a token's first token with the same adapter, then that one's place
-// among the firsts.
-template <int THREADS>
+// among the firsts.  At least 256 threads.
 __device__ void make_plan(const AdapterV& p, int tile) {
-  __shared__ int ids[256], first[256], place[256], heads[4];
+  __shared__ int ids[256], place[256], heads[4];
   const int t = threadIdx.x, bm = p.bm;
-  if (t < 256) ids[t] = t < bm ? id_of(p, tile * bm + t) : -1;
+  const int id = t < bm ? id_of(p, tile * bm + t) : -1;
+  if (t < 256) ids[t] = id;
   __syncthreads();
+  int first = -1;
   if (t < 256) {
-    int f = t;
-    for (int s = 255; s >= 0; --s)
-      if (s < bm && ids[s] == ids[t] && s < f) f = s;
-    first[t] = ids[t] >= 0 ? f : -1;
-    const uint64_t b = __ballot(first[t] == t);
+    if (id >= 0) first = t;
+#pragma unroll 8
+    for (int s = bm - 1; s >= 0; --s)
+      if (ids[s] == id && s < first) first = s;
+    const uint64_t b = __ballot(first == t);
     place[t] = rank_in_mask(b);
     if (lane_id() == 0) heads[t / kWave] = __popcll(b);
   }
@@ -133,38 +157,49 @@ __device__ void make_plan(const AdapterV& p, int tile) {
   if (t == 0) out[0] = heads[0] + heads[1] + heads[2] + heads[3];
   if (t < bm) {
     int at = -1;
-    if (first[t] >= 0) {
-      at = place[first[t]];
-      for (int w = 0; w < first[t] / kWave; ++w) at += heads[w];
-      if (first[t] == t) out[1 + at] = ids[t];
+    if (first >= 0) {
+      at = place[first];
+      for (int w = 0; w < first / kWave; ++w) at += heads[w];
+      if (first == t) out[1 + at] = id;
     }
     out[1 + bm + t] = at;
   }
 }
 
-template <class E, int NW, int RC>
+template <class E>
+__device__ __forceinline__ void put_v(const AdapterV& p, int which, int m, int c, int id, f32x4_t v) {
+  const float sc = p.scale ? p.scale[id] : 1.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = c + i < p.r ? v[i] * sc : 0.f;
+  store4<E>(static_cast<typename E::T*>(p.v[which]) + (size_t)m * p.rp + c, v);
+}
+
+// WHOLE: rows of whole chunks
+template <class E, int NW, int RC, bool WHOLE>
 __global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
   typedef typename E::T T;
   if ((int)blockIdx.x >= p.blocks) {
-    if (blockIdx.y == 0 && blockIdx.z == 0) make_plan<NW * kWave>(p, (int)blockIdx.x - p.blocks);
+    if (blockIdx.y == 0 && blockIdx.z == 0) make_plan(p, (int)blockIdx.x - p.blocks);
     return;
   }
   __shared__ f32x4_t sum[NW][RC][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave;
-  const int m0 = (int)blockIdx.x / p.lanes * 16, k0 = blockIdx.y * 16 * RC;
+  const int share = (int)blockIdx.x % p.shares, block = (int)blockIdx.x / p.shares;
+  const int m0 = block / p.lanes * 16, k0 = blockIdx.y * 16 * RC;
   const int m = m0 + (lane & 15), id = id_of(p, m);
   bool first = id >= 0 && lane < 16;
+#pragma unroll
   for (int s = 0; s < 15; ++s)
-    if (__shfl(id, s) == id && s < lane) first = false;
+    if (__builtin_amdgcn_readlane(id, s) == id && s < lane) first = false;
   uint64_t firsts = __ballot(first);
-  const bool whole = p.k % E::EPC == 0;
   const int c0 = lane >> 4;
   const T* x = static_cast<const T*>(p.x) + (size_t)(m < p.T ? m : m0) * p.ldx;
-  const int steps = (p.k + 4 * E::EPC - 1) / (4 * E::EPC);
+  const Split cut((p.k + 4 * E::EPC - 1) / (4 * E::EPC), p.shares);
+  const int step0 = cut.start(share), step1 = cut.start(share + 1);
   for (int w = 0; firsts; ++w) {
-    const int j = __shfl(id, __ffsll((unsigned long long)firsts) - 1);
+    const int j = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)firsts) - 1);
     firsts &= firsts - 1;
-    if (w % p.lanes != (int)blockIdx.x % p.lanes) continue;
+    if (w % p.lanes != block % p.lanes) continue;
     const T* a[RC];
     f32x4_t acc[RC];
 #pragma unroll
@@ -174,14 +209,15 @@ __global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
       acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     constexpr int U = RC == 1 ? 8 : 4;  // steps in flight
-    for (int s0 = wave; s0 < steps; s0 += NW * U) {
+    for (int s0 = step0 + wave; s0 < step1; s0 += NW * U) {
       uint4 xv[U], av[U][RC];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int k = ((s0 + u * NW) * 4 + c0) * E::EPC;
-        xv[u] = k < p.k ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
+        const int s = s0 + u * NW, k = (s * 4 + c0) * E::EPC;
+        const bool in = s < step1 && k < p.k;
+        xv[u] = in ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int c = 0; c < RC; ++c) av[u][c] = load_part<E>(a[c] + k, p.k - k, whole);
+        for (int c = 0; c < RC; ++c) av[u][c] = load_part<E>(a[c] + k, in ? p.k - k : 0, WHOLE);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -192,32 +228,63 @@ __global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
 #pragma unroll
     for (int c = 0; c < RC; ++c) sum[wave][c][lane] = acc[c];
     __syncthreads();
-    if (wave < RC && id == j) {
+    const int c = k0 + 16 * wave + 4 * c0;
+    if (wave < RC && id == j && c < p.rp) {
       f32x4_t v = sum[0][wave][lane];
       for (int s = 1; s < NW; ++s) v += sum[s][wave][lane];
-      const float sc = p.scale ? p.scale[j] : 1.f;
-      const int c = k0 + 16 * wave + 4 * c0;
-      if (c < p.rp) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = c + i < p.r ? v[i] * sc : 0.f;
-        store4<E>(static_cast<T*>(p.v[blockIdx.z]) + (size_t)m * p.rp + c, v);
-      }
+      if (p.shares == 1)
+        put_v<E>(p, blockIdx.z, m, c, j, v);
+      else
+        *reinterpret_cast<f32x4_t*>(p.part + (((size_t)share * p.count + blockIdx.z) * p.T + m) * p.rp + c) = v;
     }
   }
 }
 
+// Adds up the shares of v, in their order; the last workgroups make the plan.
 template <class E>
-hipError_t adapter_v(AdapterV p, int count, hipStream_t st) {
+__global__ void __launch_bounds__(kBlock) k_adapter_join(AdapterV p, int blocks) {
+  if ((int)blockIdx.x >= blocks) {
+    make_plan(p, (int)blockIdx.x - blocks);
+    return;
+  }
+  const int q = p.rp / 4, i = blockIdx.x * kBlock + threadIdx.x, row = i / q, c = (i - row * q) * 4;
+  if (row >= p.count * p.T) return;
+  const int which = row / p.T, m = row - which * p.T, id = id_of(p, m);
+  if (id < 0) return;
+  const size_t plane = (size_t)p.count * p.T * p.rp;
+  const float* at = p.part + (size_t)row * p.rp + c;
+  f32x4_t u[8], v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    u[s] = s < p.shares ? *reinterpret_cast<const f32x4_t*>(at + s * plane) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < 8; ++s) v += u[s];
+  put_v<E>(p, which, m, c, id, v);
+}
+
+template <class E, int NW, int RC>
+void start_v(const AdapterV& p, int plans, hipStream_t st) {
+  const dim3 grid(p.blocks + plans, ceil_div(p.rp, 16 * RC), p.count);
+  if (p.k % E::EPC == 0) k_adapter_v<E, NW, RC, true><<<grid, NW * kWave, 0, st>>>(p);
+  else k_adapter_v<E, NW, RC, false><<<grid, NW * kWave, 0, st>>>(p);
+}
+
+template <class E>
+hipError_t adapter_v(AdapterV p, hipStream_t st) {
   const int tiles = ceil_div(p.T, 16), plans = ceil_div(p.T, p.bm);
-  if (tiles * count >= kCUs / 2) {
-    // many tokens: a workgroup for 16 of them and 64 ranks, all their adapters in turn
+  p.shares = adapter_shares(E::EPC == 4, p.T, p.k, p.rp, p.count);
+  if (many_tokens(p.T, p.count)) {
     p.lanes = 1;
     p.blocks = tiles;
-    k_adapter_v<E, 4, 4><<<dim3(p.blocks + plans, ceil_div(p.rp, 64), count), 4 * kWave, 0, st>>>(p);
+    start_v<E, 4, 4>(p, plans, st);
   } else {
     p.lanes = p.T < 16 ? p.T : 16;
-    p.blocks = tiles * p.lanes;
-    k_adapter_v<E, 16, 1><<<dim3(p.blocks + plans, ceil_div(p.rp, 16), count), 16 * kWave, 0, st>>>(p);
+    p.blocks = tiles * p.lanes * p.shares;
+    start_v<E, 16, 1>(p, p.shares == 1 ? plans : 0, st);
+    if (p.shares > 1) {
+      const int blocks = ceil_div(p.count * p.T * (p.rp / 4), kBlock);
+      k_adapter_join<E><<<blocks + plans, kBlock, 0, st>>>(p, blocks);
+    }
   }
   return hipGetLastError();
 }
@@ -250,15 +317,15 @@ int tile_rows(Tile t) {
 // 128 share a CU; a lone one takes 0.66), a tile 6 us for its first loads and its stores.  Cutting the sum
 // in shares fills rounds that would stay empty; the shares' fp32 tiles are written and read once more, and
 // joined by a second launch.
-Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split) {
+Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters) {
   auto cut = [&](int64_t tiles, int slots, int least) {  // shares of at least `least` steps that fill the slots
     int64_t s = split ? slots / tiles : 1;
     if (s > steps / least) s = steps / least;
     return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
   };
   auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
-  if (M <= 16) return Plan{Tile::T16, cut(tiles(16, 64), 2 * kCUs, 8)};
-  if (M <= 64 || f32) return Plan{Tile::T64, cut(tiles(64, 64), 2 * kCUs, 8)};
+  if (M <= 16) return Plan{Tile::T16, cut(tiles(16, 64), kCUs * 3 / 2, 8)};
+  if (M <= 64 || f32) return Plan{Tile::T64, cut(tiles(64, 64), kCUs * 3 / 2, 8)};
   struct Kind {
     Tile t;
     int bm, bn, a_cu;
@@ -270,6 +337,7 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split) {
   Plan best{Tile::T256, 1};
   double least = 1e30;
   for (const Kind& k : kinds) {
+    if (adapters && k.t == Tile::T256) continue;  // its sums and the adapters' need more registers than there are
     const int64_t nt = tiles(k.bm, k.bn);
     const int s = cut(nt, kCUs * k.a_cu, 16);
     const int64_t rounds = (nt * s + kCUs * k.a_cu - 1) / (kCUs * k.a_cu);
@@ -283,11 +351,11 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split) {
   return best;
 }
 
-Plan token_plan(bool f32, int T, int n, int k, int products) {
-  return choose_tile(f32, T, n, products * ceil_div(k, f32 ? step_k<EF32>() : step_k<EBf16>()), true);
+Plan token_plan(bool f32, int T, int n, int k, int products, bool adapters) {
+  return choose_tile(f32, T, n, products * ceil_div(k, f32 ? step_k<EF32>() : step_k<EBf16>()), true, adapters);
 }
-Plan hidden_plan(bool f32, const BlockShape& s) {
-  return choose_tile(f32, s.T, 2 * (int64_t)s.d_ff, ceil_div(s.d, f32 ? step_k<EF32>() : step_k<EBf16>()), false);
+Plan hidden_plan(bool f32, const BlockShape& s, bool adapters) {
+  return choose_tile(f32, s.T, 2 * (int64_t)s.d_ff, ceil_div(s.d, f32 ? step_k<EF32>() : step_k<EBf16>()), false, adapters);
 }
 
 hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st) {
@@ -299,8 +367,9 @@ hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t 
 
 hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
                             const void* const a[2], void* const v[2], Tile t, hipStream_t st) {
-  const AdapterV p{x, {a[0], a[1]}, {v[0], v[1]}, ad.ids, ad.scale, ad.plan, T, k, ldx, ad.n, ad.r, ad.rp, 0, 0, tile_rows(t)};
-  return f32 ? adapter_v<EF32>(p, count, st) : adapter_v<EBf16>(p, count, st);
+  const AdapterV p{x, {a[0], a[1]}, {v[0], v[1]}, ad.ids, ad.scale, ad.plan, ad.part,
+                   T, k, ldx, ad.n, ad.r, ad.rp, 0, 0, tile_rows(t), 1, count};
+  return f32 ? adapter_v<EF32>(p, st) : adapter_v<EBf16>(p, st);
 }
 
 hipError_t launch_pad_rows(bool f32, int64_t rows, int n, int np, const void* src, void* dst, hipStream_t st) {

@@ -362,7 +362,9 @@ __device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Read
 // W_up's.  Both images are KC.
 //
 // Rows of whole chunks are loaded into LDS some steps ahead, each lane from an address of its own; odd
-// ranks are read by element and written to LDS, a step at a time.
+// ranks are read by element and written to LDS, a step at a time.  (As further steps of the main part's
+// pipeline they cost its loop more than the drained pipeline between the parts does: 48 tokens, 14336 x
+// 4096, rank 16, 35 against 31 us.)
 template <class E, class C, bool DUAL>
 struct AdapterSteps {
   typedef typename E::T T;
@@ -374,11 +376,8 @@ struct AdapterSteps {
   const int32_t* plan;  // the tile's, in LDS
   int m0, n0, cpr, chunks, steps;  // steps of one matrix's adapters
 
-  __device__ __forceinline__ AdapterSteps(const LowRank& l, int32_t* lds_plan, int tile, int m0_, int n0_)
+  __device__ __forceinline__ AdapterSteps(const LowRank& l, const int32_t* lds_plan, int m0_, int n0_)
       : lr(l), plan(lds_plan), m0(m0_), n0(n0_), cpr(l.rp / E::EPC) {
-    const int32_t* p = l.plan + (size_t)tile * (1 + 2 * C::BM);
-    for (int i = threadIdx.x; i < 1 + 2 * C::BM; i += C::threads) lds_plan[i] = p[i];
-    __syncthreads();
     chunks = uniform(plan[0]) * cpr;
     steps = (chunks + 7) / 8;
   }
@@ -395,6 +394,7 @@ struct AdapterSteps {
   __device__ __forceinline__ int neuron(int r) const { return n0 + (DUAL ? r / C::WTN * G + r % G : r); }
   __device__ __forceinline__ bool has(int which, int r) const { return !DUAL || (r % C::WTN >= G) == (which == 1); }
 
+  // this wave's loads of step `it`, zeros from it1 on
   __device__ __forceinline__ void issue(int it, int it1, char* stage) const {
     const int wave = uniform(threadIdx.x / kWave), lane = lane_id(), c = (lane & 7) ^ (lane >> 3);
     const int which = matrix(it), q = within(it) * 8 + c;
@@ -411,6 +411,39 @@ struct AdapterSteps {
         const bool mine = on && has(which, r) && n < lr.out;
         lds_load16(mine ? static_cast<const void*>(b_at(which, j, n, part)) : &zero_chunk,
                    stage + C::BM * 128 + i * 1024);
+      }
+    }
+  }
+
+  // The products of half kk of step `it`.  A token's zeros do not shield it from an Inf or NaN in another
+  // request's B (0 x Inf is NaN), so B's fragments are looked at first, and a half that holds such a value
+  // goes chunk by chunk, each into sums of its own that only its own tokens take.
+  template <class H>
+  __device__ __forceinline__ void multiply(const H& h, int it, int kk, int wm, f32x4_t (&acc)[C::MT][C::NT]) const {
+    constexpr uint32_t e = E::EPC == 8 ? 0x7f807f80u : 0x7f800000u, one = E::EPC == 8 ? 0x00800080u : 0x00800000u,
+                       top = E::EPC == 8 ? 0x80008000u : 0x80000000u;
+    uint32_t odd = 0;  // an exponent of all ones carries into its sign's place
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j)
+      odd |= ((h.b[j].x & e) + one) | ((h.b[j].y & e) + one) | ((h.b[j].z & e) + one) | ((h.b[j].w & e) + one);
+    if (__ballot((odd & top) != 0) == 0) {
+      h.multiply(acc, [](int) {});
+      return;
+    }
+    const int lane = lane_id();
+    for (int c = 0; c < 4; ++c) {
+      const int slot = (within(it) * 8 + kk * 4 + c) / cpr;
+      const bool here = (lane >> 4) == c;
+#pragma unroll
+      for (int i = 0; i < C::MT; ++i) {
+        const bool mine = plan[1 + C::BM + wm * C::WTM + i * 16 + (lane & 15)] == slot;
+        const uint4 a = here ? h.a[i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j) {
+          const f32x4_t v = product<E>(here ? h.b[j] : make_uint4(0, 0, 0, 0), a, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + v[k] : acc[i][j][k];
+        }
       }
     }
   }
@@ -489,17 +522,22 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
 
   const Reader<E, LA, C::BM, C::MT> ra(wm * C::WTM);
   const Reader<E, LB, C::BN, C::NT> rb(wn * C::WTN);
-  pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
-
-  if constexpr (AD) {
+  if constexpr (!AD) {
+    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
+  } else {
     typedef AdapterSteps<E, C, DUAL> Steps;
     int32_t* plan = reinterpret_cast<int32_t*>(lds + C::S * C::stage);
-    const Steps ad(g.lr, plan, at.m, m0, n0);  // behind its barrier the last step of the main part has been read
-    const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
-    const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);
+    for (int i = threadIdx.x; i < 1 + 2 * C::BM; i += C::threads)
+      plan[i] = g.lr.plan[(size_t)at.m * (1 + 2 * C::BM) + i];
+    __syncthreads();
+    const Steps ad(g.lr, plan, m0, n0);
     const Split part(ad.count(), g.splits);
     const int ad0 = part.start(at.split), ad1 = part.start(at.split + 1);
     const bool whole = g.lr.r % E::EPC == 0;
+    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
+    meet();  // the last step has been read
+    const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
+    const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);
     constexpr int ahead = C::S - 1;
     if (whole && ad0 < ad1) {
 #pragma unroll
@@ -520,7 +558,7 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         h.load(0, h.count, lds + buf * C::stage, kk, rva, rvb);
-        h.multiply(acc, [](int) {});
+        ad.multiply(h, it, kk, wm, acc);
       }
       buf = buf + 1 == C::S ? 0 : buf + 1;
     }
