@@ -312,40 +312,46 @@ int tile_rows(Tile t) {
   }
 }
 
-// By an estimate of the time, in us.  A product of more rows than a few tokens runs in rounds of tiles over
-// the CUs; a step of a round takes what was measured at sizes that fill the chip (two workgroups of 128 x
-// 128 share a CU; a lone one takes 0.66), a tile 6 us for its first loads and its stores.  Cutting the sum
-// in shares fills rounds that would stay empty; the shares' fp32 tiles are written and read once more, and
-// joined by a second launch.
+// By an estimate of the time, in us.  The tiles, times the shares that each sum is cut into, spread evenly over
+// the CUs.  A step of a tile takes `step` of a CU that is full, and no less than `lone` where it has the CU for
+// itself (measured at sizes that fill the chip, and at ones that leave CUs empty); a tile's first loads and its
+// stores take 6 us, which `a_cu` tiles of a CU share.  A share writes its fp32 sums, and a second launch reads
+// them.  Few tokens are bound by the weights' bytes, whatever the tile: shares only fill CUs there.
 Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters) {
-  auto cut = [&](int64_t tiles, int slots, int least) {  // shares of at least `least` steps that fill the slots
-    int64_t s = split ? slots / tiles : 1;
-    if (s > steps / least) s = steps / least;
-    return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
-  };
   auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
-  if (M <= 16) return Plan{Tile::T16, cut(tiles(16, 64), kCUs * 3 / 2, 8)};
-  if (M <= 64 || f32) return Plan{Tile::T64, cut(tiles(64, 64), kCUs * 3 / 2, 8)};
+  if (M <= 64) {
+    const bool few = M <= 16;
+    int64_t s = split ? kCUs * 3 / 2 / tiles(few ? 16 : 64, 64) : 1;
+    if (s > steps / 8) s = steps / 8;
+    return Plan{few ? Tile::T16 : Tile::T64, (int)(s < 1 ? 1 : s > 32 ? 32 : s)};
+  }
   struct Kind {
     Tile t;
     int bm, bn, a_cu;
-    double step_us, lone_us;
+    double step, lone;
   };
-  static const Kind kinds[] = {{Tile::T256, 256, 256, 1, 1.45, 1.45},
-                               {Tile::T128x256, 128, 256, 1, 0.82, 0.82},
-                               {Tile::T128, 128, 128, 2, 1.04, 0.66}};
-  Plan best{Tile::T256, 1};
+  static const Kind bf16_kinds[] = {{Tile::T256, 256, 256, 1, 1.45, 1.45},
+                                    {Tile::T128x256, 128, 256, 1, 0.82, 0.82},
+                                    {Tile::T128, 128, 128, 2, 0.52, 0.66},
+                                    {Tile::T64, 64, 64, 3, 0.21, 0.30}};
+  static const Kind f32_kinds[] = {{Tile::T64, 64, 64, 3, 0.51, 0.60}};
+  const Kind* kinds = f32 ? f32_kinds : bf16_kinds;
+  const int count = f32 ? 1 : 4;
+  Plan best{Tile::T64, 1};
   double least = 1e30;
-  for (const Kind& k : kinds) {
+  for (int i = 0; i < count; ++i) {
+    const Kind& k = kinds[i];
     if (adapters && k.t == Tile::T256) continue;  // its sums and the adapters' need more registers than there are
     const int64_t nt = tiles(k.bm, k.bn);
-    const int s = cut(nt, kCUs * k.a_cu, 16);
-    const int64_t rounds = (nt * s + kCUs * k.a_cu - 1) / (kCUs * k.a_cu);
-    const double step = nt * s <= kCUs ? k.lone_us : k.step_us;
-    const double us = rounds * (step * ((steps + s - 1) / s) + 6.0) + (s > 1 ? 5.0 + 8e-6 * (double)(M * n) * s / 5.0 : 0.0);
-    if (us < least) {
-      least = us;
-      best = Plan{k.t, s};
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (s > 1 && (!split || s > steps / 8 || nt * s > 8 * kCUs)) break;
+      const int64_t on = (nt * s + kCUs - 1) / kCUs, rounds = (on + k.a_cu - 1) / k.a_cu;
+      const double step = on * k.step > rounds * k.lone ? on * k.step : rounds * k.lone;
+      const double us = step * ((steps + s - 1) / s) + 6.0 * rounds + (s > 1 ? 5.0 + 2e-6 * (double)(M * n) * s : 0.0);
+      if (us < least) {
+        least = us;
+        best = Plan{k.t, s};
+      }
     }
   }
   return best;

@@ -8,14 +8,14 @@ namespace ffn {
 namespace {
 
 // Tiles: tokens (or weight-gradient rows) x columns, waves, steps in LDS.
-//   16, 64      a few tokens: the weights are streamed past them, 3 steps in flight, 2 to 4 workgroups a
-//               CU (28672 x 4096 weights, 1..48 tokens: 36 to 38 us, 6.4 TB/s; 128 columns a tile 38 to 40)
-//   64 (fp32)   any number of tokens: the fp32 products bound it (4096^3: 134 TFLOP/s, the card's library
-//               product 133), and small tiles waste the least of odd sizes
+//   16, 64      a few tokens: the weights are streamed past them, 2 to 4 workgroups a CU (28672 x 4096 bf16
+//               weights, 1..48 tokens: 36 to 38 us, 6.4 TB/s; 128 columns a tile 38 to 40)
+//   64          fp32, any number of tokens: the fp32 products bound it (4096^3: 132 TFLOP/s, the card's
+//               library product 133), and small tiles waste the least of odd sizes
 //   128, 128x256, 256  bf16, many tokens: 1030, 1150 and 1300 TFLOP/s where the tiles fill the chip
 //               (8192 x 4096 x 14336; the card's library product reaches 1360 to 1480)
 typedef Config<16, 64, 1, 2, 4> Tile16;
-typedef Config<64, 64, 2, 2, 4> Tile64;
+typedef Config<64, 64, 2, 2, 3> Tile64;
 typedef Config<128, 128, 2, 2, 2> Tile128;
 typedef Config<128, 256, 2, 4, 3> Tile128x256;
 typedef Config<256, 256, 2, 4, 2> Tile256;
