@@ -1,0 +1,221 @@
+"""Low-rank adapters of many requests on the GPU against 64 bits (bounds: gated_ref)."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_31975_amd import ffn
+from tests import gated_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def normal(gen, shape, std, dtype):
+    return (torch.randn(shape, generator=gen, device="cuda") * std).to(dtype)
+
+
+def stacks(gen, n, r, k, m, dtype, size=1.0):
+    return normal(gen, (n, r, k), k ** -0.5, dtype), normal(gen, (n, m, r), size * r ** -0.5, dtype)
+
+
+def make_ids(gen, T, n, how):
+    if how == "mixed":
+        return torch.randint(-1, n, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    if how == "runs":
+        return (torch.arange(T, device="cuda", dtype=torch.int32) * 3 // T + 1) % n
+    if how == "none":
+        return torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    if how == "same":
+        return torch.full((T,), n - 1, dtype=torch.int32, device="cuda")
+    # each its own, as far as there are adapters, and values that name none
+    ids = torch.arange(T, device="cuda", dtype=torch.int32)
+    ids[ids >= n] = 2 ** 31 - 1
+    ids[T // 2] = -(2 ** 31)
+    return ids
+
+
+def projection(dtype, T, d, m, n, r, how, scale=True, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed + T + 3 * d + 5 * m + 7 * r)
+    x, w = normal(gen, (T, d), 1.0, dtype), normal(gen, (m, d), d ** -0.5, dtype)
+    a, b = stacks(gen, n, r, d, m, dtype)
+    sc = 0.5 + torch.rand(n, generator=gen, device="cuda") if scale else None
+    return x, w, a, b, make_ids(gen, T, n, how), sc
+
+
+def run(x, w, a, b, ids, sc, **kw):
+    T, m = x.shape[0], w.shape[0]
+    y = torch.full((T, m), math.nan, dtype=x.dtype, device="cuda")
+    ws = torch.full_like(ffn.alloc_adapter_workspace(T, x.shape[1], m, a.shape[1], x.dtype), 0xFF)
+    return ffn.ffn_adapter_forward(x, w, ffn.adapters(ids, gate=(a, b), scale=sc), y, ws, **kw)
+
+
+def want(x, w, a, b, ids, sc):
+    return x.double() @ w.double().t() + ref.low_rank(x.double(), ids, a, b, sc)
+
+
+CASES = [(1, 64, 64, 1, 8, "same"), (1, 8, 1, 3, 1, "same"), (2, 520, 333, 4, 16, "each"), (7, 500, 1111, 3, 5, "mixed"),
+         (16, 264, 200, 20, 16, "each"), (17, 64, 65, 40, 3, "each"), (33, 136, 130, 5, 24, "mixed"),
+         (48, 1024, 512, 64, 16, "each"), (64, 72, 100, 2, 128, "runs"), (64, 256, 300, 64, 64, "each"),
+         (65, 128, 260, 7, 12, "mixed"), (130, 515, 97, 130, 9, "each"), (300, 256, 520, 4, 33, "runs"),
+         (600, 512, 1000, 600, 8, "each"), (2100, 136, 2100, 5, 16, "runs"), (2100, 64, 260, 3, 200, "mixed")]
+
+
+@pytest.mark.parametrize("T,d,m,n,r,how", CASES)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_projection(dtype, T, d, m, n, r, how):
+    p = projection(dtype, T, d, m, n, r, how)
+    # A x on its way into the second factor, and the output
+    ref.check(run(*p), want(*p), dtype, 2 if dtype == BF16 else 4, d + r)
+
+
+@pytest.mark.parametrize("T", [1, 20, 100, 300])
+def test_no_adapter_anywhere_is_the_projection(T):
+    x, w, a, b, ids, sc = projection(BF16, T, 128, 200, 4, 16, "none")
+    y = run(x, w, a, b, ids, sc)
+    ref.check(y, x.double() @ w.double().t(), BF16, 1, 128)
+    # ids beyond the stacks are none too, whatever the stacks hold
+    far = torch.full_like(ids, 4)
+    assert torch.equal(run(x, w, a, b, far, sc), y)
+
+
+def test_without_scales():
+    p = projection(F32, 40, 64, 80, 6, 8, "mixed", scale=False)
+    ref.check(run(*p), want(*p), F32, 4, 72)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,r", [(12, 8), (12, 5), (60, 16), (150, 4), (400, 16)])
+def test_requests_are_kept_apart(dtype, T, r):
+    """NaN and Inf in one request's factors reach its own tokens only.  The others' sums may then be added
+    up in another order (each adapter's own first), so they are held to the bound of any order."""
+    x, w, a, b, ids, sc = projection(dtype, T, 136, 200, 9, r, "mixed")
+    clean, exact = run(x, w, a, b, ids, sc), want(x, w, a, b, ids, sc)
+    for value in (math.nan, math.inf, -math.inf):
+        for stack in (a, b):
+            bad = stack.clone()
+            bad[4, 2, 1] = value
+            got = run(x, w, *((bad, b) if stack is a else (a, bad)), ids, sc)
+            others = ids != 4
+            ref.check(got[others], exact[others], dtype, 2 if dtype == BF16 else 4, 136 + r, f"{value}")
+            if bool((~others).any()):
+                assert not bool(torch.isfinite(got[~others]).all())
+    # an adapter that no token of the call uses
+    none = torch.where(ids == 4, torch.full_like(ids, 3), ids)
+    bad_a, bad_b = a.clone(), b.clone()
+    bad_a[4], bad_b[4] = math.nan, math.nan
+    assert torch.equal(run(x, w, bad_a, bad_b, none, sc), run(x, w, a, b, none, sc))
+    # a token's own NaN
+    x2 = x.clone()
+    x2[T // 3, 5] = math.nan
+    got = run(x2, w, a, b, ids, sc)
+    others = torch.arange(T, device="cuda") != T // 3
+    assert torch.equal(got[others], clean[others]) and bool(torch.isnan(got[T // 3]).all())
+
+
+@pytest.mark.parametrize("dtype,T,d,d_ff,n,r", [(BF16, 1, 128, 300, 2, 8), (BF16, 16, 256, 512, 5, 16),
+                                                (F32, 9, 72, 130, 4, 6), (BF16, 70, 136, 333, 6, 24),
+                                                (F32, 100, 64, 200, 3, 16), (BF16, 600, 264, 1000, 9, 12),
+                                                (F32, 33, 67, 77, 3, 5)])
+def test_block_with_adapters(dtype, T, d, d_ff, n, r):
+    """Adapters on all three projections, and on each alone."""
+    gen = torch.Generator(device="cuda").manual_seed(T + d)
+    x = normal(gen, (T, d), 1.0, dtype)
+    w = [normal(gen, (d_ff, d), d ** -0.5, dtype), normal(gen, (d_ff, d), d ** -0.5, dtype),
+         normal(gen, (d_ff, d), d_ff ** -0.5, dtype)]
+    pairs = {"gate": stacks(gen, n, r, d, d_ff, dtype, 0.2), "up": stacks(gen, n, r, d, d_ff, dtype, 0.2),
+             "down": stacks(gen, n, r, d_ff, d, dtype, 0.2)}
+    ids = make_ids(gen, T, n, "mixed")
+    ids[0] = n - 1
+    sc = 0.5 + torch.rand(n, generator=gen, device="cuda")
+    ws = ffn.alloc_gated_workspace(T, d, d_ff, dtype, r, backward=False)
+    for names in (("gate", "up", "down"), ("gate",), ("up",), ("down",), ("gate", "down")):
+        some = {k: pairs[k] for k in names}
+        y = torch.full_like(x, math.nan)
+        ws.fill_(0xFF)
+        ffn.ffn_gated_forward(x, *w, 0.1, ffn.options(act=2, silu_up=True), y, ws,
+                              adapters=ffn.adapters(ids, scale=sc, **some))
+        f = ref.forward(x, *w, 0.1, 2, True, dict(some, ids=ids, scale=sc))
+        # z, A z, and the output; A x on its way into g and v
+        ref.check(y, f["y"], dtype, 4 if dtype == BF16 else 10, d + d_ff + 2 * r, "+".join(names))
+
+
+def test_block_is_its_projections():
+    """The block with adapters is what the projection calls and the activation give one after the other: the
+    same roundings but for z's second operand path, so twice one call's bound."""
+    T, d, d_ff, n, r = 24, 256, 640, 8, 16
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = normal(gen, (T, d), 1.0, F32)
+    w = [normal(gen, (d_ff, d), d ** -0.5, F32), normal(gen, (d_ff, d), d ** -0.5, F32), normal(gen, (d_ff, d), d_ff ** -0.5, F32)]
+    pairs = {"gate": stacks(gen, n, r, d, d_ff, F32), "up": stacks(gen, n, r, d, d_ff, F32),
+             "down": stacks(gen, n, r, d_ff, d, F32)}
+    ids = make_ids(gen, T, n, "mixed")
+    y = torch.empty_like(x)
+    ffn.ffn_gated_forward(x, *w, 0.0, ffn.options(act=2), y, ffn.alloc_gated_workspace(T, d, d_ff, F32, r),
+                          adapters=ffn.adapters(ids, **pairs))
+    h = run(x, w[0], *pairs["gate"], ids, None)
+    v = run(x, w[1], *pairs["up"], ids, None)
+    z = (torch.nn.functional.silu(h) * v).contiguous()
+    y2 = run(z, w[2].t().contiguous(), *pairs["down"], ids, None)
+    assert float((y - y2).norm()) <= 2 * ref.bound(F32, 10, d + d_ff + 2 * r) * float(y2.norm())
+
+
+def test_stacks_past_32_bits():
+    """20000 adapters: A passes 2^31 elements, B 2^32 bytes; the last ones are used."""
+    n, r, d, m, T = 20000, 16, 8192, 7000, 6
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    a = torch.zeros((n, r, d), dtype=BF16, device="cuda")
+    b = torch.zeros((n, m, r), dtype=BF16, device="cuda")
+    use = [0, 9999, 16384, 19998, 19999]
+    for j in use:
+        a[j] = normal(gen, (r, d), d ** -0.5, BF16)
+        b[j] = normal(gen, (m, r), r ** -0.5, BF16)
+    x, w = normal(gen, (T, d), 1.0, BF16), normal(gen, (m, d), d ** -0.5, BF16)
+    ids = torch.tensor(use + [19999], dtype=torch.int32, device="cuda")
+    ref.check(run(x, w, a, b, ids, None), want(x, w, a, b, ids, None), BF16, 2, d + r)
+
+
+def test_graph_and_stream():
+    """Captured and replayed with other ids, tokens and weights of the adapters in the same buffers."""
+    x, w, a, b, ids, sc = projection(BF16, 40, 256, 300, 8, 16, "mixed")
+    ad = ffn.adapters(ids, gate=(a, b), scale=sc)
+    y, ws = torch.empty((40, 300), dtype=BF16, device="cuda"), ffn.alloc_adapter_workspace(40, 256, 300, 16, BF16)
+    ffn.ffn_adapter_forward(x, w, ad, y, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ffn.ffn_adapter_forward(x, w, ad, y, ws)
+    for seed in (1, 2, 3):
+        q = projection(BF16, 40, 256, 300, 8, 16, ("mixed", "each", "none")[seed - 1], seed=seed)
+        for dst, src in zip((x, w, a, b, ids, sc), q):
+            dst.copy_(src)
+        y.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, run(*q))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ffn.ffn_adapter_forward(x, w, ad, y, ws, stream=side)
+    side.synchronize()
+    assert torch.equal(y, run(x, w, a, b, ids, sc))
+
+
+def test_refusals():
+    x, w, a, b, ids, sc = projection(BF16, 6, 64, 100, 4, 8, "mixed")
+    y, ws = torch.empty((6, 100), dtype=BF16, device="cuda"), ffn.alloc_adapter_workspace(6, 64, 100, 8, BF16)
+    bad = [lambda: ffn.adapters(ids), lambda: ffn.adapters(ids.long(), gate=(a, b)),
+           lambda: ffn.adapters(ids, gate=(a, b.float())), lambda: ffn.adapters(ids, gate=(a, b[:3])),
+           lambda: ffn.adapters(ids, gate=(a, b.transpose(1, 2))), lambda: ffn.adapters(ids, gate=(a, b), scale=sc[:2]),
+           lambda: ffn.adapters(ids, gate=(a, b), scale=sc.double())]
+    for f in bad:
+        with pytest.raises((ValueError, TypeError)):
+            f()
+    good = ffn.adapters(ids, gate=(a, b), scale=sc)
+    for kw in (dict(x=x[:5]), dict(x=x.float()), dict(w=w[:50]), dict(y=y[:, :64]), dict(ad=ffn.adapters(ids, up=(a, b)))):
+        args = dict(dict(x=x, w=w, ad=good, y=y), **kw)
+        with pytest.raises((ValueError, TypeError)):
+            ffn.ffn_adapter_forward(args["x"], args["w"], args["ad"], args["y"], ws)
+    with pytest.raises(ffn.FFNError):
+        ffn.ffn_adapter_forward(x, w, good, y, ws[:64])
+    ffn.ffn_adapter_forward(x, w, good, y, ws)
+    ref.check(y, want(x, w, a, b, ids, sc), BF16, 2, 72)
