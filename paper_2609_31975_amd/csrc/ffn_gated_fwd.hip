@@ -47,7 +47,7 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
   const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
   return with_tile<E>(hidden_plan(E::EPC == 4, s, ad.plan != nullptr).tile, [&](auto c) {
     typedef decltype(c) C;
-    if constexpr (C::BM <= 128)
+    if constexpr (adapter_tile<C>())
       if (a.lr.plan) return launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st);
     return launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
   });

@@ -4,19 +4,23 @@
 
 namespace ffn {
 
-// Whether a workgroup of the adapters' first factor takes 16 tokens and 64 ranks, all the tokens'
-// adapters in turn, or one of the adapters and 16 ranks.
-static bool many_tokens(int T, int count) { return (T + 15) / 16 * count >= kCUs / 2; }
+// Whether the adapters' first factor goes through LDS tiles (k_adapter_v_tiles): with many tokens, and rows of
+// whole chunks.
+static bool v_tiles(bool f32, int T, int k, int count) {
+  return (T + 15) / 16 * count >= kCUs / 2 && k % (f32 ? 4 : 8) == 0;
+}
 
-// Shares of a row, at most 8 (k_adapter_join), so that two workgroups come to a CU; a share is at
-// least half a round of loads of its 16 waves.
+// Shares of a row, at most 8 (k_adapter_join), so that a few workgroups come to a CU; a share is at least
+// half a round of loads of k_adapter_v's 16 waves, or 8 steps of k_adapter_v_tiles.
 int adapter_shares(bool f32, int T, int k, int rp, int count) {
-  if (many_tokens(T, count)) return 1;
-  const int steps = (k + (f32 ? 15 : 31)) / (f32 ? 16 : 32);
-  const int groups = (T + 15) / 16 * (T < 16 ? T : 16) * ((rp + 15) / 16) * count;
-  int s = 2 * kCUs / groups;
-  if (s > steps / 64) s = steps / 64;
-  return s < 1 ? 1 : s > 8 ? 8 : s;
+  const bool tiles = v_tiles(f32, T, k, count);
+  const int step = f32 ? 16 : 32;  // k of a product
+  const int steps = (k + step - 1) / step;
+  const int64_t groups = (int64_t)((T + 15) / 16) * count *
+                         (tiles ? (rp + 63) / 64 : (T < 16 ? T : 16) * (int64_t)((rp + 15) / 16));
+  int64_t s = (tiles ? 3 : 2) * kCUs / groups;
+  if (s > steps / (tiles ? 16 : 64)) s = steps / (tiles ? 16 : 64);
+  return (int)(s < 1 ? 1 : s > 8 ? 8 : s);
 }
 
 namespace {
@@ -92,7 +96,7 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.part, p.ldo, np, p.n % 4 == 0};
   hipError_t e = with_tile<E>(plan.tile, [&](auto c) {
     typedef decltype(c) C;
-    if constexpr (C::BM <= 128)
+    if constexpr (adapter_tile<C>())
       if (a.lr.plan) return launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st);
     return launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
   });
@@ -106,18 +110,21 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ the adapters' first factor
-// v[m][k] = scale_j <A_j[k], x[m]>, j the adapter of token m.  A workgroup takes 16 tokens, 16 RC of
-// the ranks, and of the adapters among its tokens every lanes-th from the blockIdx.x % lanes-th on (one
-// each where there are few tokens, all of them where there are many); its waves share the row, each
-// with loads of its own from memory to fragments, and are joined in LDS.  A product serves all 16 tokens,
-// and those with another adapter are dropped.
+// v[m][k] = scale_j <A_j[k], x[m]>, j the adapter of token m.  A workgroup takes 16 tokens, some of the
+// ranks, a share of the row, and of the adapters among its tokens every lanes-th from its own on.  A product
+// serves all 16 tokens, and those with another adapter are dropped.
 //
-// Few tokens leave most CUs without a workgroup, and one CU alone reads a row slowly, so the row is cut
-// in `shares` too: these write fp32 sums, and k_adapter_join adds them up (16 tokens with an adapter each,
-// rank 16, rows of 14336: 33 us in one share, 11 us in 7).
+// Few tokens (k_adapter_v): 16 ranks, one adapter each, the row over 16 waves with loads of their own from
+// memory to fragments, joined in LDS.  One CU alone reads a row slowly, so the row is cut in `shares` over
+// workgroups too: these write fp32 sums, and k_adapter_join adds them up (16 tokens with an adapter each, rank
+// 16, rows of 14336: 33 us in one share, 9 + 4 us in 7).
 //
-// With one share the last workgroups (one for each tile of bm tokens) make the plan of the product
-// that reads v; else k_adapter_join does.
+// Many tokens (k_adapter_v_tiles): 64 ranks through the pipeline of the tiled product.  A fragment loaded
+// from memory takes 16 bytes of 16 rows at a time, a quarter of the cache's rate, which these hit (3000
+// tokens, rank 64, rows of 4096: 39 us, through LDS 16 + 5).
+//
+// The plan of the product that reads v is made by the last workgroups (one for each tile of bm tokens) of
+// k_adapter_v with one share, else of k_adapter_join.
 struct AdapterV {
   const void* x;
   const void* a[2];
@@ -174,25 +181,41 @@ __device__ __forceinline__ void put_v(const AdapterV& p, int which, int m, int c
   store4<E>(static_cast<typename E::T*>(p.v[which]) + (size_t)m * p.rp + c, v);
 }
 
+// The adapters of the 16 tokens from m0 on, one after the other (the lowest token of each): a mask over
+// the lanes below 16 that hold their first token.
+__device__ __forceinline__ uint64_t first_tokens(int id) {
+  const int lane = lane_id();
+  bool first = id >= 0 && lane < 16;
+#pragma unroll
+  for (int s = 0; s < 15; ++s)
+    if (__builtin_amdgcn_readlane(id, s) == id && s < lane) first = false;
+  return __ballot(first);
+}
+
+template <class E>
+__device__ __forceinline__ void put_share(const AdapterV& p, int share, int which, int m, int c, int id, f32x4_t v) {
+  if (p.shares == 1)
+    put_v<E>(p, which, m, c, id, v);
+  else
+    *reinterpret_cast<f32x4_t*>(p.part + (((size_t)share * p.count + which) * p.T + m) * p.rp + c) = v;
+}
+
 // WHOLE: rows of whole chunks
-template <class E, int NW, int RC, bool WHOLE>
-__global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
+constexpr int kVWaves = 16;
+template <class E, bool WHOLE>
+__global__ void __launch_bounds__(kVWaves * kWave) k_adapter_v(AdapterV p) {
   typedef typename E::T T;
   if ((int)blockIdx.x >= p.blocks) {
     if (blockIdx.y == 0 && blockIdx.z == 0) make_plan(p, (int)blockIdx.x - p.blocks);
     return;
   }
-  __shared__ f32x4_t sum[NW][RC][kWave];
+  __shared__ f32x4_t sum[kVWaves][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave;
   const int share = (int)blockIdx.x % p.shares, block = (int)blockIdx.x / p.shares;
-  const int m0 = block / p.lanes * 16, k0 = blockIdx.y * 16 * RC;
+  const int m0 = block / p.lanes * 16, k0 = blockIdx.y * 16;
   const int m = m0 + (lane & 15), id = id_of(p, m);
-  bool first = id >= 0 && lane < 16;
-#pragma unroll
-  for (int s = 0; s < 15; ++s)
-    if (__builtin_amdgcn_readlane(id, s) == id && s < lane) first = false;
-  uint64_t firsts = __ballot(first);
-  const int c0 = lane >> 4;
+  uint64_t firsts = first_tokens(id);
+  const int c0 = lane >> 4, col = k0 + (lane & 15);
   const T* x = static_cast<const T*>(p.x) + (size_t)(m < p.T ? m : m0) * p.ldx;
   const Split cut((p.k + 4 * E::EPC - 1) / (4 * E::EPC), p.shares);
   const int step0 = cut.start(share), step1 = cut.start(share + 1);
@@ -200,42 +223,77 @@ __global__ void __launch_bounds__(NW * kWave) k_adapter_v(AdapterV p) {
     const int j = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)firsts) - 1);
     firsts &= firsts - 1;
     if (w % p.lanes != block % p.lanes) continue;
-    const T* a[RC];
-    f32x4_t acc[RC];
-#pragma unroll
-    for (int c = 0; c < RC; ++c) {
-      const int col = k0 + 16 * c + (lane & 15);
-      a[c] = static_cast<const T*>(p.a[blockIdx.z]) + ((size_t)j * p.r + (col < p.r ? col : 0)) * p.k;
-      acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-    constexpr int U = RC == 1 ? 8 : 4;  // steps in flight
-    for (int s0 = step0 + wave; s0 < step1; s0 += NW * U) {
-      uint4 xv[U], av[U][RC];
+    const T* a = static_cast<const T*>(p.a[blockIdx.z]) + ((size_t)j * p.r + (col < p.r ? col : 0)) * p.k;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;  // steps in flight
+    // two steps after each other are the halves of a 128-byte line: one wave's
+    for (int s0 = step0 + 2 * wave; s0 < step1; s0 += kVWaves * U) {
+      uint4 xv[U], av[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int s = s0 + u * NW, k = (s * 4 + c0) * E::EPC;
+        const int s = s0 + u / 2 * 2 * kVWaves + u % 2, k = (s * 4 + c0) * E::EPC;
         const bool in = s < step1 && k < p.k;
         xv[u] = in ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int c = 0; c < RC; ++c) av[u][c] = load_part<E>(a[c] + k, in ? p.k - k : 0, WHOLE);
+        av[u] = load_part<E>(a + k, in ? p.k - k : 0, WHOLE);
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int c = 0; c < RC; ++c) acc[c] = product<E>(av[u][c], xv[u], acc[c]);
+      for (int u = 0; u < U; ++u) acc = product<E>(av[u], xv[u], acc);
     }
     __syncthreads();
-#pragma unroll
-    for (int c = 0; c < RC; ++c) sum[wave][c][lane] = acc[c];
+    sum[wave][lane] = acc;
     __syncthreads();
-    const int c = k0 + 16 * wave + 4 * c0;
-    if (wave < RC && id == j && c < p.rp) {
-      f32x4_t v = sum[0][wave][lane];
-      for (int s = 1; s < NW; ++s) v += sum[s][wave][lane];
-      if (p.shares == 1)
-        put_v<E>(p, blockIdx.z, m, c, j, v);
-      else
-        *reinterpret_cast<f32x4_t*>(p.part + (((size_t)share * p.count + blockIdx.z) * p.T + m) * p.rp + c) = v;
+    const int c = k0 + 4 * c0;
+    if (wave == 0 && id == j && c < p.rp) {
+      for (int s = 1; s < kVWaves; ++s) acc += sum[s][lane];
+      put_share<E>(p, share, blockIdx.z, m, c, j, acc);
+    }
+  }
+}
+
+template <class E>
+__global__ void __launch_bounds__(Tile16::threads) k_adapter_v_tiles(AdapterV p) {
+  typedef Tile16 C;
+  __shared__ __align__(1024) char lds[C::S * C::stage];
+  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave);
+  const int share = (int)blockIdx.x % p.shares, block = (int)blockIdx.x / p.shares;
+  const int m0 = block / p.lanes * 16, n0 = blockIdx.y * C::BN;
+  const int m = m0 + (lane & 15), id = id_of(p, m);
+  uint64_t firsts = first_tokens(id);
+  Loader<E, Lay::KC, C::BM, C::NW> la;
+  Loader<E, Lay::KC, C::BN, C::NW> lb;
+  la.init(p.ldx, p.T, m0, [](int r) { return r; });
+  lb.init(p.k, p.r, n0, [](int r) { return r; });
+  const Reader<E, Lay::KC, C::BM, C::MT> ra(0);
+  const Reader<E, Lay::KC, C::BN, C::NT> rb(wave * C::WTN);
+  const Split cut((p.k + step_k<E>() - 1) / step_k<E>(), p.shares);
+  const int it0 = cut.start(share), it1 = cut.start(share + 1);
+  const char* x = static_cast<const char*>(p.x) + (size_t)m0 * p.ldx * esz<E>();
+  for (int w = 0; firsts; ++w) {
+    const int j = __builtin_amdgcn_readlane(id, __ffsll((unsigned long long)firsts) - 1);
+    firsts &= firsts - 1;
+    if (w % p.lanes != block % p.lanes) continue;
+    const char* a = static_cast<const char*>(p.a[blockIdx.z]) + ((size_t)j * p.r + n0) * p.k * esz<E>();
+    f32x4_t acc[C::MT][C::NT];
+#pragma unroll
+    for (int i = 0; i < C::NT; ++i) acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr int pa = decltype(la)::per, per = pa + decltype(lb)::per;
+    meet();  // the last adapter's steps have been read
+    pipeline<E, C, Lay::KC, Lay::KC, per>(lds, it0, it1, ra, rb, acc, [&](int f0, int f1, int it, int buf) {
+      const int left = it < it1 ? p.k - it * step_k<E>() : 0;
+      char* d = lds + buf * C::stage;
+#pragma unroll
+      for (int f = 0; f < per; ++f) {
+        if (f < f0 || f >= f1) continue;
+        if (f < pa) la.issue(f, left, d, [&](int) { return x + (size_t)it * 128; });
+        else lb.issue(f - pa, left, d + C::BM * 128, [&](int) { return a + (size_t)it * 128; });
+      }
+    });
+    if (id == j) {
+#pragma unroll
+      for (int i = 0; i < C::NT; ++i) {
+        const int c = n0 + wave * C::WTN + i * 16 + 4 * (lane >> 4);
+        if (c < p.rp) put_share<E>(p, share, blockIdx.z, m, c, j, acc[0][i]);
+      }
     }
   }
 }
@@ -262,29 +320,26 @@ __global__ void __launch_bounds__(kBlock) k_adapter_join(AdapterV p, int blocks)
   put_v<E>(p, which, m, c, id, v);
 }
 
-template <class E, int NW, int RC>
-void start_v(const AdapterV& p, int plans, hipStream_t st) {
-  const dim3 grid(p.blocks + plans, ceil_div(p.rp, 16 * RC), p.count);
-  if (p.k % E::EPC == 0) k_adapter_v<E, NW, RC, true><<<grid, NW * kWave, 0, st>>>(p);
-  else k_adapter_v<E, NW, RC, false><<<grid, NW * kWave, 0, st>>>(p);
-}
-
 template <class E>
 hipError_t adapter_v(AdapterV p, hipStream_t st) {
   const int tiles = ceil_div(p.T, 16), plans = ceil_div(p.T, p.bm);
-  p.shares = adapter_shares(E::EPC == 4, p.T, p.k, p.rp, p.count);
-  if (many_tokens(p.T, p.count)) {
-    p.lanes = 1;
-    p.blocks = tiles;
-    start_v<E, 4, 4>(p, plans, st);
+  const bool f32 = E::EPC == 4, by_tiles = v_tiles(f32, p.T, p.k, p.count);
+  p.shares = adapter_shares(f32, p.T, p.k, p.rp, p.count);
+  if (by_tiles) {
+    // most tiles hold a prompt's tokens, of one request or of two
+    p.lanes = 2;
+    p.blocks = tiles * p.lanes * p.shares;
+    k_adapter_v_tiles<E><<<dim3(p.blocks, ceil_div(p.rp, Tile16::BN), p.count), Tile16::threads, 0, st>>>(p);
   } else {
     p.lanes = p.T < 16 ? p.T : 16;
     p.blocks = tiles * p.lanes * p.shares;
-    start_v<E, 16, 1>(p, p.shares == 1 ? plans : 0, st);
-    if (p.shares > 1) {
-      const int blocks = ceil_div(p.count * p.T * (p.rp / 4), kBlock);
-      k_adapter_join<E><<<blocks + plans, kBlock, 0, st>>>(p, blocks);
-    }
+    const dim3 grid(p.blocks + (p.shares == 1 ? plans : 0), ceil_div(p.rp, 16), p.count);
+    if (p.k % E::EPC == 0) k_adapter_v<E, true><<<grid, kVWaves * kWave, 0, st>>>(p);
+    else k_adapter_v<E, false><<<grid, kVWaves * kWave, 0, st>>>(p);
+  }
+  if (by_tiles || p.shares > 1) {
+    const int blocks = p.shares > 1 ? ceil_div(p.count * p.T * (p.rp / 4), kBlock) : 0;
+    k_adapter_join<E><<<blocks + plans, kBlock, 0, st>>>(p, blocks);
   }
   return hipGetLastError();
 }
@@ -341,7 +396,9 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Kind& k = kinds[i];
-    if (adapters && k.t == Tile::T256) continue;  // its sums and the adapters' need more registers than there are
+    // the adapters' sums beside T256's need more registers than there are; T128 holds too few steps to
+    // load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us against 122 for T128x256)
+    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128)) continue;
     const int64_t nt = tiles(k.bm, k.bn);
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (s > 1 && (!split || s > steps / 8 || nt * s > 8 * kCUs)) break;

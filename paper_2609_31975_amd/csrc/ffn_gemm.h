@@ -339,19 +339,44 @@ __device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Read
   Half<E, C, LA, LB> h0, h1;
   h0.load(0, h0.count, lds, 0, ra, rb);
   int buf = 0;
+  // An fp32 product adds its terms one after the other, so every four fp32 steps are summed from zero and
+  // then into the running sum: two short chains in place of a long one.
+  constexpr bool chain2 = E::EPC == 4;
+  f32x4_t step[chain2 ? C::MT : 1][chain2 ? C::NT : 1];
+  auto& sum = [&]() -> auto& {
+    if constexpr (chain2) return step;
+    else return acc;
+  }();
+  auto flush = [&] {
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) {
+        acc[i][j] += step[i][j];
+        step[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+  };
+  if constexpr (chain2)
+#pragma unroll
+    for (int i = 0; i < C::MT; ++i)
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) step[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int it = it0; it < it1; ++it) {
-    h0.multiply(acc, [&](int i) {
+    h0.multiply(sum, [&](int i) {
       h1.load(i * h1.count / C::MT, (i + 1) * h1.count / C::MT, lds + buf * C::stage, 1, ra, rb);
     });
     wait_loads<(C::S - 2) * PER>();
     meet();
     const int next = buf + 1 == C::S ? 0 : buf + 1;
-    h1.multiply(acc, [&](int i) {
+    h1.multiply(sum, [&](int i) {
       h0.load(i * h0.count / C::MT, (i + 1) * h0.count / C::MT, lds + next * C::stage, 0, ra, rb);
       issue(i * PER / C::MT, (i + 1) * PER / C::MT, it + C::S, buf);
     });
+    if constexpr (chain2)
+      if (((it - it0) & 3) == 3) flush();
     buf = next;
   }
+  if constexpr (chain2) flush();
   wait_loads<0>();  // LDS is free for others once no load into it is in flight
 }
 

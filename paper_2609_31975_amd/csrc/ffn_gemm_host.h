@@ -43,6 +43,12 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
   else *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, o);
 }
 
+// the tiles that choose_tile picks for products with adapters
+template <class C>
+constexpr bool adapter_tile() {
+  return C::BM <= 64 || C::S == 3;
+}
+
 inline LowRank low_rank(const AdapterSet& ad, const void* const v[2], const void* const b[2], int out) {
   return LowRank{{v[0], v[1]}, {b[0], b[1]}, ad.plan, ad.r, ad.rp, out};
 }
