@@ -27,8 +27,9 @@
  * a multiple of 8 bf16 or 4 fp32) are first copied to padded rows in the workspace, so such
  * widths cost a copy of the weights a call.
  *
- * Ownership, streams, errors: as in ffn_sparse.h.  The workspace needs no initialisation and
- * holds nothing from one call to the next.  `save` holds g, v and z of a forward call for the
+ * Ownership, streams, errors: as in ffn_sparse.h.  The workspace needs no initialisation,
+ * holds nothing from one call to the next, and serves calls of fewer tokens and lower ranks too (its
+ * size grows with both).  `save` holds g, v and z of a forward call for the
  * backward call of the same shape and options; it is read only by the backward call, which may
  * be repeated.  Outputs must not overlap inputs, each other, save or the workspace.
  *

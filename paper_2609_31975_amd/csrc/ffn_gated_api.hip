@@ -63,17 +63,7 @@ size_t save_layout(ffn_dtype_t w, int T, int d_ff, void* base, Save* out) {
   return c.off;
 }
 
-size_t part_bytes(ffn_dtype_t w, int T, int n, int k, int products, bool adapters) {
-  const int s = token_plan(w == FFN_F32, T, n, k, products, adapters).splits;
-  return s > 1 ? (size_t)s * T * round_up_to(n, 4) * 4 : 0;
-}
-
-// The largest sums of shares of the adapters' first factors; a call's two products take turns.
-size_t shares_bytes(ffn_dtype_t w, int T, int k, int rp, int count) {
-  const int s = adapter_shares(w == FFN_F32, T, k, rp, count);
-  return s > 1 ? (size_t)s * count * T * rp * 4 : 0;
-}
-
+// The regions below grow with T and with rp, so a workspace serves calls of fewer tokens and lower ranks too.
 struct ForwardWs {
   void *z, *v[2], *v2, *x, *w_gate, *w_up, *w_down;
   float *part, *shares;
@@ -88,12 +78,9 @@ size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Fo
     for (void*& v : f.v) v = c.take(e * s.T * rp);
     f.v2 = c.take(e * s.T * rp);
     f.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
-    const size_t both = std::max(shares_bytes(w, s.T, s.d, rp, 1), shares_bytes(w, s.T, s.d, rp, 2));
-    f.shares = static_cast<float*>(c.take(std::max(both, shares_bytes(w, s.T, s.d_ff, rp, 1))));
+    f.shares = static_cast<float*>(c.take(adapter_share_bytes_most(s.T, rp, 2)));
   }
-  // with adapters, which may be of the gate and the up projection alone, the larger of both
-  f.part = static_cast<float*>(c.take(std::max(part_bytes(w, s.T, s.d, s.d_ff, 1, false),
-                                               rp ? part_bytes(w, s.T, s.d, s.d_ff, 1, true) : 0)));
+  f.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d)));
   if (s.dp != s.d) {
     f.x = c.take(e * s.T * s.dp);
     f.w_gate = c.take(e * s.d_ff * s.dp);
@@ -114,7 +101,7 @@ size_t backward_layout(ffn_dtype_t w, const BlockShape& s, void* base, BackwardW
   const size_t e = esize(w);
   b.dg = c.take(e * s.T * s.ldf);
   b.dv = c.take(e * s.T * s.ldf);
-  b.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d, s.d_ff, 2, false)));
+  b.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d)));
   if (s.dp != s.d) {
     b.x = c.take(e * s.T * s.dp);
     b.dy = c.take(e * s.T * s.dp);
@@ -137,8 +124,8 @@ size_t adapter_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Ad
   const size_t e = esize(w);
   a.v = c.take(e * s.T * rp);
   a.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
-  a.shares = static_cast<float*>(c.take(shares_bytes(w, s.T, s.d, rp, 1)));
-  a.part = static_cast<float*>(c.take(part_bytes(w, s.T, s.d_ff, s.d, 1, true)));
+  a.shares = static_cast<float*>(c.take(adapter_share_bytes_most(s.T, rp, 1)));
+  a.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d_ff)));
   if (s.dp != s.d) {
     a.x = c.take(e * s.T * s.dp);
     a.w = c.take(e * s.d_ff * s.dp);

@@ -21,7 +21,7 @@ struct AdapterSet {
   const int32_t* ids = nullptr;
   const float* scale = nullptr;
   int32_t* plan = nullptr;  // room for plan_ints(T); filled by launch_adapter_v
-  float* part = nullptr;    // room for adapter_shares(...) x count x T x rp where there are several
+  float* part = nullptr;    // adapter_share_bytes_most(...)
 };
 
 // The tile of a product with M rows and n columns over `steps` steps of 128 bytes, and the shares its sum is
@@ -33,6 +33,7 @@ struct Plan {
 };
 Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters);
 int tile_rows(Tile t);
+size_t share_bytes_most(bool f32, int T, int n);
 // Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.
 inline size_t plan_ints(int T) { return 2 * ((size_t)T + 256) + T / 16 + 1; }
 
@@ -52,7 +53,7 @@ struct TokenProduct {
   const void* b[2];  // KS: [k][ldb]; KC: [n][ldb]
   int products, T, n, k, lda, ldb, ldo;
   void* out;
-  float* part;  // splits x T x round_up(n, 4) fp32 where the sum is cut
+  float* part;  // splits x T x round_up(n, 4) fp32 where the sum is cut: share_bytes_most(...)
   AdapterSet ad;
   const void* v;
   const void* ab;
@@ -67,8 +68,8 @@ hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const 
 // up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
                            void* const out[3], hipStream_t st);
-// Shares that the rows of k elements are cut into, of `count` stacks.
-int adapter_shares(bool f32, int T, int k, int rp, int count);
+// Room for the shares of the sums, for T tokens or fewer and ranks up to rp.
+size_t adapter_share_bytes_most(int T, int rp, int count);
 // v[i] [T][rp] = scale_j A_j x for up to two stacks, and ad.plan for the product of tile `t` that reads them
 hipError_t launch_adapter_v(bool f32, int T, int k, int ldx, const void* x, const AdapterSet& ad, int count,
                             const void* const a[2], void* const v[2], Tile t, hipStream_t st);

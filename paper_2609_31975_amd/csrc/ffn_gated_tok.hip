@@ -12,7 +12,11 @@ static bool v_tiles(bool f32, int T, int k, int count) {
 
 // Shares of a row, at most 8 (k_adapter_join), so that a few workgroups come to a CU; a share is at least
 // half a round of loads of k_adapter_v's 16 waves, or 8 steps of k_adapter_v_tiles.
-int adapter_shares(bool f32, int T, int k, int rp, int count) {
+size_t adapter_share_bytes_most(int T, int rp, int count) {
+  const int few = 16 * 3 * kCUs;  // beyond, one share
+  return (size_t)8 * count * (T < few ? T : few) * rp * 4;
+}
+static int adapter_shares(bool f32, int T, int k, int rp, int count) {
   const bool tiles = v_tiles(f32, T, k, count);
   const int step = f32 ? 16 : 32;  // k of a product
   const int steps = (k + step - 1) / step;
@@ -383,13 +387,14 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
   struct Kind {
     Tile t;
     int bm, bn, a_cu;
+    int most;  // tiles of all shares: their fp32 sums stay within share_bytes_most()
     double step, lone;
   };
-  static const Kind bf16_kinds[] = {{Tile::T256, 256, 256, 1, 1.45, 1.45},
-                                    {Tile::T128x256, 128, 256, 1, 0.82, 0.82},
-                                    {Tile::T128, 128, 128, 2, 0.52, 0.66},
-                                    {Tile::T64, 64, 64, 3, 0.21, 0.30}};
-  static const Kind f32_kinds[] = {{Tile::T64, 64, 64, 3, 0.51, 0.60}};
+  static const Kind bf16_kinds[] = {{Tile::T256, 256, 256, 1, 512, 1.45, 1.45},
+                                    {Tile::T128x256, 128, 256, 1, 512, 0.82, 0.82},
+                                    {Tile::T128, 128, 128, 2, 1024, 0.52, 0.66},
+                                    {Tile::T64, 64, 64, 3, 2048, 0.21, 0.30}};
+  static const Kind f32_kinds[] = {{Tile::T64, 64, 64, 3, 2048, 0.51, 0.60}};
   const Kind* kinds = f32 ? f32_kinds : bf16_kinds;
   const int count = f32 ? 1 : 4;
   Plan best{Tile::T64, 1};
@@ -401,7 +406,7 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
     if (adapters && (k.t == Tile::T256 || k.t == Tile::T128)) continue;
     const int64_t nt = tiles(k.bm, k.bn);
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (s > 1 && (!split || s > steps / 8 || nt * s > 8 * kCUs)) break;
+      if (s > 1 && (!split || s > steps / 8 || nt * s > k.most)) break;
       const int64_t on = (nt * s + kCUs - 1) / kCUs, rounds = (on + k.a_cu - 1) / k.a_cu;
       const double step = on * k.step > rounds * k.lone ? on * k.step : rounds * k.lone;
       const double us = step * ((steps + s - 1) / s) + 6.0 * rounds + (s > 1 ? 5.0 + 2e-6 * (double)(M * n) * s : 0.0);
@@ -412,6 +417,13 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
     }
   }
   return best;
+}
+
+// Room for the shares of a product of T tokens or fewer: grows with T and n, whatever the plans.
+size_t share_bytes_most(bool f32, int T, int n) {
+  const size_t tiles = f32 ? (size_t)2048 * 64 * 64 * 4 : (size_t)512 * 256 * 256 * 4;
+  const size_t rows = (size_t)32 * T * ((n + 3) / 4 * 4) * 4;
+  return rows < tiles ? rows : tiles;
 }
 
 Plan token_plan(bool f32, int T, int n, int k, int products, bool adapters) {

@@ -128,6 +128,24 @@ def test_sizes():
         ffn.alloc_gated_save(1, 8, torch.float16, device="cpu")
 
 
+@pytest.mark.parametrize("wdt", [0, 1])
+def test_a_workspace_serves_fewer_tokens_and_lower_ranks(wdt):
+    tokens = [1, 2, 7, 15, 16, 17, 48, 63, 64, 65, 100, 127, 128, 129, 255, 257, 400, 513, 777, 1000, 2047, 2049, 3000,
+              4096, 6000, 12288, 12289, 20000, 60000]
+    for d, d_ff in ((64, 128), (1000, 2731), (1001, 2731), (4096, 14336), (8192, 28672)):
+        for r in (0, 1, 8, 16, 17, 24, 33, 64, 128):
+            low = 0
+            for T in tokens:
+                for back in (0, 1):
+                    n = L.ffn_gated_workspace_bytes(wdt, T, d, d_ff, r, back)
+                    assert n >= L.ffn_gated_workspace_bytes(wdt, T, d, d_ff, max(0, r - 1), back) > 0
+                assert n >= low
+                low = n
+            if r:
+                sizes = [L.ffn_adapter_workspace_bytes(wdt, T, d, d_ff, r) for T in tokens]
+                assert sizes == sorted(sizes) and sizes[0] > 0
+
+
 def test_binding_refuses_host_tensors():
     x, w = torch.zeros(2, 8), torch.zeros(16, 8)
     with pytest.raises(ValueError):

@@ -176,6 +176,16 @@ def test_stacks_past_32_bits():
     ref.check(run(x, w, a, b, ids, None), want(x, w, a, b, ids, None), BF16, 2, d + r)
 
 
+def test_one_workspace_for_many_calls():
+    """Allocated for the most tokens and the highest rank, used for others in turn."""
+    ws = ffn.alloc_adapter_workspace(700, 264, 520, 64, BF16)
+    for T, r in ((700, 64), (1, 8), (33, 16), (64, 64), (65, 5), (130, 24), (500, 12), (2, 64)):
+        x, w, a, b, ids, sc = projection(BF16, T, 264, 520, 6, r, "mixed")
+        y = torch.empty((T, 520), dtype=BF16, device="cuda")
+        ffn.ffn_adapter_forward(x, w, ffn.adapters(ids, gate=(a, b), scale=sc), y, ws)
+        ref.check(y, want(x, w, a, b, ids, sc), BF16, 2, 264 + r, f"T={T} r={r}")
+
+
 def test_graph_and_stream():
     """Captured and replayed with other ids, tokens and weights of the adapters in the same buffers."""
     x, w, a, b, ids, sc = projection(BF16, 40, 256, 300, 8, 16, "mixed")
