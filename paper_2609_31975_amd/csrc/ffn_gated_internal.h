@@ -26,7 +26,7 @@ struct AdapterSet {
 
 // The tile of a product with M rows and n columns over `steps` steps of 128 bytes, and the shares its sum is
 // cut into (1 where split is false).
-enum class Tile { T16, T64, T128, T128x256, T256 };
+enum class Tile { T16, T64, T64x128, T128, T128x256, T256 };
 struct Plan {
   Tile tile;
   int splits;

@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(Tile16::threads) k_adapter_v_tiles(AdapterV p)
     for (int i = 0; i < C::NT; ++i) acc[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     constexpr int pa = decltype(la)::per, per = pa + decltype(lb)::per;
     meet();  // the last adapter's steps have been read
-    pipeline<E, C, Lay::KC, Lay::KC, per>(lds, it0, it1, ra, rb, acc, [&](int f0, int f1, int it, int buf) {
+    pipeline<E, C, Lay::KC, Lay::KC, per>(lds, it0, it1, ra, rb, acc, C::BM, false, [&](int f0, int f1, int it, int buf) {
       const int left = it < it1 ? p.k - it * step_k<E>() : 0;
       char* d = lds + buf * C::stage;
 #pragma unroll
@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(kBlock) k_pad_rows(int64_t rows, int n, int np
 int tile_rows(Tile t) {
   switch (t) {
     case Tile::T16: return Tile16::BM;
-    case Tile::T64: return Tile64::BM;
+    case Tile::T64:
+    case Tile::T64x128: return Tile64::BM;
     case Tile::T256: return Tile256::BM;
     default: return Tile128::BM;
   }
@@ -394,16 +395,16 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
                                     {Tile::T128x256, 128, 256, 1, 512, 0.82, 0.82},
                                     {Tile::T128, 128, 128, 2, 1024, 0.52, 0.66},
                                     {Tile::T64, 64, 64, 3, 2048, 0.21, 0.30}};
-  static const Kind f32_kinds[] = {{Tile::T64, 64, 64, 3, 2048, 0.51, 0.60}};
+  static const Kind f32_kinds[] = {{Tile::T64x128, 64, 128, 3, 1024, 0.93, 1.00}, {Tile::T64, 64, 64, 3, 2048, 0.51, 0.60}};
   const Kind* kinds = f32 ? f32_kinds : bf16_kinds;
-  const int count = f32 ? 1 : 4;
+  const int count = f32 ? 2 : 4;
   Plan best{Tile::T64, 1};
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Kind& k = kinds[i];
-    // the adapters' sums beside T256's need more registers than there are; T128 holds too few steps to
-    // load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us against 122 for T128x256)
-    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128)) continue;
+    // the adapters' sums beside T256's need more registers than there are; T128 and T64x128 hold too few
+    // steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us in T128, 122 in T128x256)
+    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128 || k.t == Tile::T64x128)) continue;
     const int64_t nt = tiles(k.bm, k.bn);
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (s > 1 && (!split || s > steps / 8 || nt * s > k.most)) break;

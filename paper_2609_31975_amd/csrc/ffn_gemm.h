@@ -245,13 +245,16 @@ struct Half {
   // between(i): work to issue in front of the products of fragment a[i].  LDS reads and loads into LDS
   // are handed out among the products a few at a time: issued in one piece they fill their queues, and a
   // wave that waits for a queue issues no products either.
-  template <class Between>
-  __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT], Between between) const {
+  // RAGGED: only the first `rows` of the 16-row pieces have any rows of the result.
+  template <bool RAGGED, class Between>
+  __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT], int rows, Between between) const {
 #pragma unroll
     for (int i = 0; i < C::MT; ++i) {
       between(i);
+      if (!RAGGED || i < rows) {
 #pragma unroll
-      for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
+        for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
+      }
       issue_barrier();
     }
   }
@@ -328,10 +331,12 @@ __device__ __forceinline__ TileAt tile_at(const GemmArgs& g) {
 // Half a step's fragments are read while the other half's products run: the second half of step i
 // during the first half's products, the first half of step i + 1, behind the barrier that frees step i's
 // buffer, during the second half's, and with it step i + S is loaded into that buffer.
-template <class E, class C, Lay LA, Lay LB, int PER, class Issue>
-__device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Reader<E, LA, C::BM, C::MT>& ra,
-                                         const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT],
-                                         Issue issue) {
+// rows: this wave's 16-row pieces that hold rows of the result; a tile at the last row, which has fewer than
+// all, leaves the others' products out (RAGGED).
+template <bool RAGGED, class E, class C, Lay LA, Lay LB, int PER, class Issue>
+__device__ __forceinline__ void run_steps(char* lds, int it0, int it1, const Reader<E, LA, C::BM, C::MT>& ra,
+                                          const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT], int rows,
+                                          Issue issue) {
 #pragma unroll
   for (int i = 0; i < C::S; ++i) issue(0, PER, it0 + i, i);
   wait_loads<(C::S - 1) * PER>();
@@ -362,13 +367,13 @@ __device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Read
 #pragma unroll
       for (int j = 0; j < C::NT; ++j) step[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   for (int it = it0; it < it1; ++it) {
-    h0.multiply(sum, [&](int i) {
+    h0.template multiply<RAGGED>(sum, rows, [&](int i) {
       h1.load(i * h1.count / C::MT, (i + 1) * h1.count / C::MT, lds + buf * C::stage, 1, ra, rb);
     });
     wait_loads<(C::S - 2) * PER>();
     meet();
     const int next = buf + 1 == C::S ? 0 : buf + 1;
-    h1.multiply(sum, [&](int i) {
+    h1.template multiply<RAGGED>(sum, rows, [&](int i) {
       h0.load(i * h0.count / C::MT, (i + 1) * h0.count / C::MT, lds + next * C::stage, 0, ra, rb);
       issue(i * PER / C::MT, (i + 1) * PER / C::MT, it + C::S, buf);
     });
@@ -378,6 +383,14 @@ __device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Read
   }
   if constexpr (chain2) flush();
   wait_loads<0>();  // LDS is free for others once no load into it is in flight
+}
+// left: rows of the result from the wave's first on
+template <class E, class C, Lay LA, Lay LB, int PER, class Issue>
+__device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Reader<E, LA, C::BM, C::MT>& ra,
+                                         const Reader<E, LB, C::BN, C::NT>& rb, f32x4_t (&acc)[C::MT][C::NT], int left,
+                                         bool ragged, Issue issue) {
+  if (C::MT == 1 || !ragged) run_steps<false, E, C, LA, LB, PER>(lds, it0, it1, ra, rb, acc, C::MT, issue);
+  else run_steps<true, E, C, LA, LB, PER>(lds, it0, it1, ra, rb, acc, left > 0 ? (left + 15) / 16 : 0, issue);
 }
 
 // ------------------------------------------------------------------ adapters within a product
@@ -452,7 +465,7 @@ struct AdapterSteps {
     for (int j = 0; j < C::NT; ++j)
       odd |= ((h.b[j].x & e) + one) | ((h.b[j].y & e) + one) | ((h.b[j].z & e) + one) | ((h.b[j].w & e) + one);
     if (__ballot((odd & top) != 0) == 0) {
-      h.multiply(acc, [](int) {});
+      h.template multiply<false>(acc, C::MT, [](int) {});
       return;
     }
     const int lane = lane_id();
@@ -548,7 +561,7 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
   const Reader<E, LA, C::BM, C::MT> ra(wm * C::WTM);
   const Reader<E, LB, C::BN, C::NT> rb(wn * C::WTN);
   if constexpr (!AD) {
-    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
+    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, g.M - m0 - wm * C::WTM, g.M - m0 < C::BM, issue);
   } else {
     typedef AdapterSteps<E, C, DUAL> Steps;
     int32_t* plan = reinterpret_cast<int32_t*>(lds + C::S * C::stage);
@@ -559,7 +572,7 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
     const Split part(ad.count(), g.splits);
     const int ad0 = part.start(at.split), ad1 = part.start(at.split + 1);
     const bool whole = g.lr.r % E::EPC == 0;
-    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, issue);
+    pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, g.M - m0 - wm * C::WTM, g.M - m0 < C::BM, issue);
     meet();  // the last step has been read
     const Reader<E, Lay::KC, C::BM, C::MT> rva(wm * C::WTM);
     const Reader<E, Lay::KC, C::BN, C::NT> rvb(wn * C::WTN);

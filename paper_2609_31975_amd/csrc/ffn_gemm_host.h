@@ -10,12 +10,14 @@ namespace {
 // Tiles: tokens (or weight-gradient rows) x columns, waves, steps in LDS.
 //   16, 64      a few tokens: the weights are streamed past them, 2 to 4 workgroups a CU (28672 x 4096 bf16
 //               weights, 1..48 tokens: 36 to 38 us, 6.4 TB/s; 128 columns a tile 38 to 40)
-//   64          fp32, any number of tokens: the fp32 products bound it (4096^3: 132 TFLOP/s, the card's
-//               library product 133), and small tiles waste the least of odd sizes
+//   64, 64x128  fp32, any number of tokens: the fp32 products bound it (512 x 28460 x
+//               3840: 123 and 138 TFLOP/s, the card's library product 133), and small tiles waste the least
+//               of odd sizes
 //   128, 128x256, 256  bf16, many tokens: 1030, 1150 and 1300 TFLOP/s where the tiles fill the chip
 //               (8192 x 4096 x 14336; the card's library product reaches 1360 to 1480)
 typedef Config<16, 64, 1, 2, 4> Tile16;
 typedef Config<64, 64, 2, 2, 3> Tile64;
+typedef Config<64, 128, 2, 4, 2> Tile64x128;
 typedef Config<128, 128, 2, 2, 2> Tile128;
 typedef Config<128, 256, 2, 4, 3> Tile128x256;
 typedef Config<256, 256, 2, 4, 2> Tile256;
@@ -46,7 +48,7 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
 // the tiles that choose_tile picks for products with adapters
 template <class C>
 constexpr bool adapter_tile() {
-  return C::BM <= 64 || C::S == 3;
+  return C::S >= 3;
 }
 
 inline LowRank low_rank(const AdapterSet& ad, const void* const v[2], const void* const b[2], int out) {
@@ -66,7 +68,7 @@ hipError_t with_tile(Tile t, F f) {
     if (t == Tile::T128x256) return f(Tile128x256{});
     return f(Tile256{});
   } else {
-    return hipErrorInvalidValue;  // not reached: fp32 products take the two tiles above
+    return f(Tile64x128{});
   }
 }
 
