@@ -80,7 +80,7 @@ size_t forward_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Fo
     f.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
     f.shares = static_cast<float*>(c.take(adapter_share_bytes_most(s.T, rp, 2)));
   }
-  f.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d)));
+  f.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, 1, s.T, std::max(s.d, 2 * s.d_ff), true)));
   if (s.dp != s.d) {
     f.x = c.take(e * s.T * s.dp);
     f.w_gate = c.take(e * s.d_ff * s.dp);
@@ -101,7 +101,9 @@ size_t backward_layout(ffn_dtype_t w, const BlockShape& s, void* base, BackwardW
   const size_t e = esize(w);
   b.dg = c.take(e * s.T * s.ldf);
   b.dv = c.take(e * s.T * s.ldf);
-  b.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d)));
+  // dz and dx, and the weight gradients
+  b.part = static_cast<float*>(c.take(std::max(share_bytes_most(w == FFN_F32, 1, s.T, std::max(s.d, s.ldf), true),
+                                               share_bytes_most(w == FFN_F32, 3, s.d_ff, s.d, false))));
   if (s.dp != s.d) {
     b.x = c.take(e * s.T * s.dp);
     b.dy = c.take(e * s.T * s.dp);
@@ -125,7 +127,7 @@ size_t adapter_layout(ffn_dtype_t w, const BlockShape& s, int rp, void* base, Ad
   a.v = c.take(e * s.T * rp);
   a.plan = static_cast<int32_t*>(c.take(4 * plan_ints(s.T)));
   a.shares = static_cast<float*>(c.take(adapter_share_bytes_most(s.T, rp, 1)));
-  a.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, s.T, s.d_ff)));
+  a.part = static_cast<float*>(c.take(share_bytes_most(w == FFN_F32, 1, s.T, s.d_ff, true)));
   if (s.dp != s.d) {
     a.x = c.take(e * s.T * s.dp);
     a.w = c.take(e * s.d_ff * s.dp);
@@ -239,7 +241,7 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
     FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, hidden_plan(f32, s, true).tile, stream));
   }
   AdapterSet hidden = b2[0] || b2[1] ? set : AdapterSet{};
-  FFN_TRY(launch_block_hidden(f32, s, x, w_gate, w_up, form, hidden, v2, b2, sv.z, sv.g, sv.v, stream));
+  FFN_TRY(launch_block_hidden(f32, s, x, w_gate, w_up, form, hidden, v2, b2, sv.z, sv.g, sv.v, f.part, stream));
   const bool down = ad && ad->down_b;
   if (down) {
     const void* a[2] = {ad->down_a, nullptr};
@@ -276,7 +278,7 @@ int ffn_gated_backward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, c
   FFN_TRY(padded(f32, s, T, &dy, b.dy, stream));
   if (hidden) {
     FFN_TRY(padded(f32, s, d_ff, &w_down_t, b.w_down, stream));
-    FFN_TRY(launch_block_dz(f32, s, dy, w_down_t, form, sv.g, sv.v, b.dg, b.dv, stream));
+    FFN_TRY(launch_block_dz(f32, s, dy, w_down_t, form, sv.g, sv.v, b.dg, b.dv, b.part, stream));
   }
   if (dx) {
     FFN_TRY(padded(f32, s, d_ff, &w_gate, b.w_gate, stream));
@@ -297,7 +299,7 @@ int ffn_gated_backward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, c
   want(dw_gate, b.dg, x);
   want(dw_up, b.dv, x);
   want(dw_down_t, sv.z, dy);
-  if (n) FFN_TRY(launch_block_dw(f32, s, n, wa, wb, wo, stream));
+  if (n) FFN_TRY(launch_block_dw(f32, s, n, wa, wb, wo, b.part, stream));
   return FFN_OK;
 }
 

@@ -14,7 +14,7 @@ struct EpiDz {
 
   __device__ __forceinline__ void select(GemmArgs&) const {}
   __device__ __forceinline__ void pair(int, int, f32x4_t, f32x4_t) const {}
-  __device__ __forceinline__ void put(const GemmArgs&, int, int m, int n, f32x4_t dz) const {
+  __device__ __forceinline__ void put(const GemmArgs&, int m, int n, f32x4_t dz) const {
     if (n >= ldf) return;
     const size_t at = (size_t)m * ldf + n;
     const f32x4_t gg = *reinterpret_cast<const f32x4_t*>(g + at), vv = *reinterpret_cast<const f32x4_t*>(v + at);
@@ -46,7 +46,7 @@ struct EpiDw {
     g.b.p[0] = b[blockIdx.y];
   }
   __device__ __forceinline__ void pair(int, int, f32x4_t, f32x4_t) const {}
-  __device__ __forceinline__ void put(const GemmArgs& g, int, int m, int n, f32x4_t v) const {
+  __device__ __forceinline__ void put(const GemmArgs& g, int m, int n, f32x4_t v) const {
     if (n >= g.N) return;
     typename E::T* o = out[blockIdx.y] + (size_t)m * ldo + n;
     if (vec) {
@@ -61,7 +61,7 @@ struct EpiDw {
 
 template <class E>
 hipError_t dz(const BlockShape& s, const void* dy, const void* w_down_t, const BlockForm& form, const float* g,
-              const float* v, void* dg, void* dv, hipStream_t st) {
+              const float* v, void* dg, void* dv, float* part, hipStream_t st) {
   GemmArgs a{};
   a.a = Operand{{dy, nullptr}, s.dp, s.T};
   a.b = Operand{{w_down_t, nullptr}, s.dp, s.d_ff};
@@ -69,17 +69,17 @@ hipError_t dz(const BlockShape& s, const void* dy, const void* w_down_t, const B
   a.N = s.ldf;
   a.K = s.d;
   a.products = 1;
-  a.splits = 1;
+  a.part = part;
   const EpiDz<E> epi{form, s.d_ff, s.ldf, g, v, static_cast<typename E::T*>(dg), static_cast<typename E::T*>(dv)};
-  const Plan p = choose_tile(E::EPC == 4, s.T, s.ldf, ceil_div(s.d, step_k<E>()), false, false);
+  const Plan p = choose_tile(E::EPC == 4, 1, s.T, s.ldf, ceil_div(s.d, step_k<E>()), false, true);
   return with_tile<E>(p.tile, [&](auto c) {
-    return launch_gemm<E, decltype(c), Lay::KC, Lay::KC, false, false>(a, epi, 1, st);
+    return launch_gemm<E, decltype(c), Lay::KC, Lay::KC, false, false>(a, epi, p, 1, st);
   });
 }
 
 template <class E>
 hipError_t dw(const BlockShape& s, int count, const void* const a[3], const void* const b[3], void* const out[3],
-              hipStream_t st) {
+              float* part, hipStream_t st) {
   GemmArgs g{};
   g.a = Operand{{nullptr, nullptr}, s.ldf, s.ldf};
   g.b = Operand{{nullptr, nullptr}, s.dp, s.dp};
@@ -87,7 +87,7 @@ hipError_t dw(const BlockShape& s, int count, const void* const a[3], const void
   g.N = s.d;
   g.K = s.T;
   g.products = 1;
-  g.splits = 1;
+  g.part = part;
   EpiDw<E> epi{};
   for (int i = 0; i < count; ++i) {
     epi.a[i] = a[i];
@@ -96,11 +96,10 @@ hipError_t dw(const BlockShape& s, int count, const void* const a[3], const void
   }
   epi.ldo = s.d;
   epi.vec = s.d % 4 == 0;
-  // rows of all gradients: their tiles are in one launch
-  const Plan p = choose_tile(E::EPC == 4, (int64_t)count * s.d_ff, s.d, ceil_div(s.T, step_k<E>()), false, false);
-  return with_tile<E>(p.tile == Tile::T16 ? Tile::T64 : p.tile, [&](auto c) {
+  const Plan p = choose_tile(E::EPC == 4, count, s.d_ff, s.d, ceil_div(s.T, step_k<E>()), false, false);
+  return with_tile<E>(p.tile, [&](auto c) {
     typedef decltype(c) C;
-    if constexpr (C::BM >= 64) return launch_gemm<E, C, Lay::KS, Lay::KS, false, false>(g, epi, count, st);
+    if constexpr (C::BM >= 64) return launch_gemm<E, C, Lay::KS, Lay::KS, false, false>(g, epi, p, count, st);
     else return hipErrorInvalidValue;  // not reached
   });
 }
@@ -108,12 +107,12 @@ hipError_t dw(const BlockShape& s, int count, const void* const a[3], const void
 }  // namespace
 
 hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const void* w_down_t, const BlockForm& form,
-                           const float* g, const float* v, void* dg, void* dv, hipStream_t st) {
-  return f32 ? dz<EF32>(s, dy, w_down_t, form, g, v, dg, dv, st) : dz<EBf16>(s, dy, w_down_t, form, g, v, dg, dv, st);
+                           const float* g, const float* v, void* dg, void* dv, float* part, hipStream_t st) {
+  return f32 ? dz<EF32>(s, dy, w_down_t, form, g, v, dg, dv, part, st) : dz<EBf16>(s, dy, w_down_t, form, g, v, dg, dv, part, st);
 }
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
-                           void* const out[3], hipStream_t st) {
-  return f32 ? dw<EF32>(s, count, a, b, out, st) : dw<EBf16>(s, count, a, b, out, st);
+                           void* const out[3], float* part, hipStream_t st) {
+  return f32 ? dw<EF32>(s, count, a, b, out, part, st) : dw<EBf16>(s, count, a, b, out, part, st);
 }
 
 }  // namespace ffn

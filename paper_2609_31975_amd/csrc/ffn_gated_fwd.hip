@@ -13,7 +13,7 @@ struct EpiGated {
   float *g, *v;  // or null
 
   __device__ __forceinline__ void select(GemmArgs&) const {}
-  __device__ __forceinline__ void put(const GemmArgs&, int, int, int, f32x4_t) const {}
+  __device__ __forceinline__ void put(const GemmArgs&, int, int, f32x4_t) const {}
   __device__ __forceinline__ void pair(int m, int n, f32x4_t h, f32x4_t u) const {
     if (n >= ldf) return;
     const size_t at = (size_t)m * ldf + n;
@@ -34,7 +34,7 @@ struct EpiGated {
 template <class E>
 hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const void* w_up, const BlockForm& form,
                   const AdapterSet& ad, const void* const v2[2], const void* const b2[2], void* z, float* g, float* v,
-                  hipStream_t st) {
+                  float* part, hipStream_t st) {
   GemmArgs a{};
   a.a = Operand{{x, nullptr}, s.dp, s.T};
   a.b = Operand{{w_gate, w_up}, s.dp, s.d_ff};
@@ -42,14 +42,15 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
   a.N = s.d_ff;
   a.K = s.d;
   a.products = 1;
-  a.splits = 1;
+  a.part = part;
   if (ad.plan) a.lr = low_rank(ad, v2, b2, s.d_ff);
   const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
-  return with_tile<E>(hidden_plan(E::EPC == 4, s, ad.plan != nullptr).tile, [&](auto c) {
+  const Plan plan = hidden_plan(E::EPC == 4, s, ad.plan != nullptr);
+  return with_tile<E>(plan.tile, [&](auto c) {
     typedef decltype(c) C;
     if constexpr (adapter_tile<C>())
-      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, 1, st);
-    return launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, 1, st);
+      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, plan, 1, st);
+    return launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, plan, 1, st);
   });
 }
 
@@ -57,9 +58,9 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
 
 hipError_t launch_block_hidden(bool f32, const BlockShape& s, const void* x, const void* w_gate, const void* w_up,
                                const BlockForm& form, const AdapterSet& ad, const void* const v2[2],
-                               const void* const b2[2], void* z, float* g, float* v, hipStream_t st) {
-  return f32 ? hidden<EF32>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, st)
-             : hidden<EBf16>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, st);
+                               const void* const b2[2], void* z, float* g, float* v, float* part, hipStream_t st) {
+  return f32 ? hidden<EF32>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, part, st)
+             : hidden<EBf16>(s, x, w_gate, w_up, form, ad, v2, b2, z, g, v, part, st);
 }
 
 }  // namespace ffn

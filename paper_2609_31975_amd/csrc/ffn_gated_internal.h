@@ -24,16 +24,18 @@ struct AdapterSet {
   float* part = nullptr;    // adapter_share_bytes_most(...)
 };
 
-// The tile of a product with M rows and n columns over `steps` steps of 128 bytes, and the shares its sum is
-// cut into (1 where split is false).
+// The tile of a product (or of `problems` alike, in one launch) with M rows and n columns over `steps` steps
+// of 128 bytes, and how many of all its tiles, the last ones, are cut along k, in how many shares.  tokens: the
+// rows are tokens (few of them take tiles of few rows).
 enum class Tile { T16, T64, T64x128, T128, T128x256, T256 };
 struct Plan {
   Tile tile;
-  int splits;
+  int cut, shares;
 };
-Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters);
+Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapters, bool tokens);
 int tile_rows(Tile t);
-size_t share_bytes_most(bool f32, int T, int n);
+// Room for the shares of a product of M rows or fewer and n columns, whatever its plan.
+size_t share_bytes_most(bool f32, int problems, int M, int64_t n, bool tokens);
 // Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.
 inline size_t plan_ints(int T) { return 2 * ((size_t)T + 256) + T / 16 + 1; }
 
@@ -42,18 +44,20 @@ struct BlockShape {
   int T, d, d_ff, dp, ldf;
 };
 
+// part, here and below: share_bytes_most(...) of the product.
+//
 // z = A(x W1^T - t) U(x W3^T), and g, v in fp32 when g is not null.  v2: A_j x of the two projections'
 // adapters (null: none), b2 their B stacks.
 hipError_t launch_block_hidden(bool f32, const BlockShape& s, const void* x, const void* w_gate, const void* w_up,
                                const BlockForm& form, const AdapterSet& ad, const void* const v2[2],
-                               const void* const b2[2], void* z, float* g, float* v, hipStream_t st);
+                               const void* const b2[2], void* z, float* g, float* v, float* part, hipStream_t st);
 // out [T][n] = z W (W [k][n], k strided) with adapters (b null: none), or the sum of two such products.
 struct TokenProduct {
   const void* a[2];  // [T][lda]
   const void* b[2];  // KS: [k][ldb]; KC: [n][ldb]
   int products, T, n, k, lda, ldb, ldo;
   void* out;
-  float* part;  // splits x T x round_up(n, 4) fp32 where the sum is cut: share_bytes_most(...)
+  float* part;
   AdapterSet ad;
   const void* v;
   const void* ab;
@@ -64,10 +68,10 @@ hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t 
 hipError_t launch_token_product_kc(bool f32, const TokenProduct& p, hipStream_t st);
 // dg, dv [T][ldf] from dz = dy W2 and the saved g, v.
 hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const void* w_down_t, const BlockForm& form,
-                           const float* g, const float* v, void* dg, void* dv, hipStream_t st);
+                           const float* g, const float* v, void* dg, void* dv, float* part, hipStream_t st);
 // up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
-                           void* const out[3], hipStream_t st);
+                           void* const out[3], float* part, hipStream_t st);
 // Room for the shares of the sums, for T tokens or fewer and ranks up to rp.
 size_t adapter_share_bytes_most(int T, int rp, int count);
 // v[i] [T][rp] = scale_j A_j x for up to two stacks, and ad.plan for the product of tile `t` that reads them

@@ -32,18 +32,13 @@ namespace {
 template <class E>
 struct EpiTok {
   typename E::T* out;
-  float* part;  // of a split sum
-  int ldo, np;
+  int ldo;
   bool vec;  // rows of whole quads
 
   __device__ __forceinline__ void select(GemmArgs&) const {}
   __device__ __forceinline__ void pair(int, int, f32x4_t, f32x4_t) const {}
-  __device__ __forceinline__ void put(const GemmArgs& g, int split, int m, int n, f32x4_t v) const {
+  __device__ __forceinline__ void put(const GemmArgs& g, int m, int n, f32x4_t v) const {
     if (n >= g.N) return;
-    if (g.splits > 1) {
-      *reinterpret_cast<f32x4_t*>(part + ((size_t)split * g.M + m) * np + n) = v;
-      return;
-    }
     typename E::T* o = out + (size_t)m * ldo + n;
     if (vec) {
       store4<E>(o, v);
@@ -55,34 +50,6 @@ struct EpiTok {
   }
 };
 
-// out[m][n] = sum of the shares, in their order
-template <class E>
-__global__ void __launch_bounds__(kBlock) k_join(int splits, int M, int N, int np, int ldo, const float* part,
-                                                 typename E::T* out) {
-  const int q = np / 4;
-  const size_t total = (size_t)M * q, plane = (size_t)M * np;
-  for (size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x; i < total; i += (size_t)gridDim.x * kBlock) {
-    const int m = (int)(i / q), n = (int)(i - (size_t)m * q) * 4;
-    const float* p = part + (size_t)m * np + n;
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < splits; s0 += 8) {  // 8 loads in flight
-      f32x4_t u[8];
-#pragma unroll
-      for (int s = 0; s < 8; ++s)
-        u[s] = s0 + s < splits ? *reinterpret_cast<const f32x4_t*>(p + (s0 + s) * plane) : f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 8; ++s) v += u[s];
-    }
-    typename E::T* o = out + (size_t)m * ldo + n;
-    if (N % 4 == 0) {
-      store4<E>(o, v);
-    } else {
-      for (int k = 0; k < 4; ++k)
-        if (n + k < N) o[k] = (typename E::T)v[k];
-    }
-  }
-}
-
 template <class E, Lay LB>
 hipError_t product(const TokenProduct& p, hipStream_t st) {
   GemmArgs a{};
@@ -93,24 +60,16 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   a.K = p.k;
   a.products = p.products;
   const Plan plan = token_plan(E::EPC == 4, p.T, p.n, p.k, p.products, p.ad.plan != nullptr);
-  a.splits = plan.splits;
+  a.part = p.part;
   const void *v[2] = {p.v, nullptr}, *b[2] = {p.ab, nullptr};
   if (p.ad.plan) a.lr = low_rank(p.ad, v, b, p.n);
-  const int np = (p.n + 3) / 4 * 4;
-  const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.part, p.ldo, np, p.n % 4 == 0};
-  hipError_t e = with_tile<E>(plan.tile, [&](auto c) {
+  const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.ldo, p.n % 4 == 0};
+  return with_tile<E>(plan.tile, [&](auto c) {
     typedef decltype(c) C;
     if constexpr (adapter_tile<C>())
-      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, 1, st);
-    return launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, 1, st);
+      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, plan, 1, st);
+    return launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, plan, 1, st);
   });
-  if (e == hipSuccess && a.splits > 1) {
-    const int64_t quads = (int64_t)p.T * np / 4;
-    const int grid = (int)(quads / kBlock + 1 < 8 * kCUs ? quads / kBlock + 1 : 8 * kCUs);
-    k_join<E><<<grid, kBlock, 0, st>>>(a.splits, p.T, p.n, np, p.ldo, p.part, static_cast<typename E::T*>(p.out));
-    e = hipGetLastError();
-  }
-  return e;
 }
 
 // ------------------------------------------------------------------ the adapters' first factor
@@ -372,23 +331,28 @@ int tile_rows(Tile t) {
   }
 }
 
-// By an estimate of the time, in us.  The tiles, times the shares that each sum is cut into, spread evenly over
-// the CUs.  A step of a tile takes `step` of a CU that is full, and no less than `lone` where it has the CU for
-// itself (measured at sizes that fill the chip, and at ones that leave CUs empty); a tile's first loads and its
-// stores take 6 us, which `a_cu` tiles of a CU share.  A share writes its fp32 sums, and a second launch reads
-// them.  Few tokens are bound by the weights' bytes, whatever the tile: shares only fill CUs there.
-Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool adapters) {
-  auto tiles = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((n + bn - 1) / bn); };
-  if (M <= 64) {
+// By an estimate of the time, in us.  Tiles run in rounds over the CUs, `a_cu` to a CU.  A step of a tile takes
+// `step` of a CU that is full, and no less than `lone` where it has the CU for itself (measured at sizes that
+// fill the chip, and at ones that leave CUs empty); a round's first loads and stores take 6 us.  The tiles of
+// the last round, where it is not full, may be cut along k in shares that fill it; a share writes its fp32
+// sums, and a second launch reads them (5 us and 4 TB/s).  (4096 tokens, d 2560, d_ff 7168: 840 tiles of the
+// weight gradients are 3 rounds and 72 tiles, in 3 shares each: 449 -> 400 us.)
+//
+// Few tokens are bound by the weights' bytes, whatever the tile: there shares only fill CUs.
+Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapters, bool tokens) {
+  auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((n + bn - 1) / bn) * problems; };
+  if (tokens && M <= 64) {
     const bool few = M <= 16;
-    int64_t s = split ? kCUs * 3 / 2 / tiles(few ? 16 : 64, 64) : 1;
+    const int64_t nt = tiles(few ? 16 : 64, 64);
+    int64_t s = kCUs * 3 / 2 / nt;
     if (s > steps / 8) s = steps / 8;
-    return Plan{few ? Tile::T16 : Tile::T64, (int)(s < 1 ? 1 : s > 32 ? 32 : s)};
+    if (s > 32) s = 32;
+    return Plan{few ? Tile::T16 : Tile::T64, s > 1 ? (int)nt : 0, s > 1 ? (int)s : 1};
   }
   struct Kind {
     Tile t;
     int bm, bn, a_cu;
-    int most;  // tiles of all shares: their fp32 sums stay within share_bytes_most()
+    int most;  // shares of all cut tiles: their sums stay within share_bytes_most()
     double step, lone;
   };
   static const Kind bf16_kinds[] = {{Tile::T256, 256, 256, 1, 512, 1.45, 1.45},
@@ -398,40 +362,45 @@ Plan choose_tile(bool f32, int64_t M, int64_t n, int steps, bool split, bool ada
   static const Kind f32_kinds[] = {{Tile::T64x128, 64, 128, 3, 1024, 0.93, 1.00}, {Tile::T64, 64, 64, 3, 2048, 0.51, 0.60}};
   const Kind* kinds = f32 ? f32_kinds : bf16_kinds;
   const int count = f32 ? 2 : 4;
-  Plan best{Tile::T64, 1};
+  Plan best{Tile::T64, 0, 1};
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Kind& k = kinds[i];
     // the adapters' sums beside T256's need more registers than there are; T128 and T64x128 hold too few
     // steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us in T128, 122 in T128x256)
     if (adapters && (k.t == Tile::T256 || k.t == Tile::T128 || k.t == Tile::T64x128)) continue;
-    const int64_t nt = tiles(k.bm, k.bn);
+    const int64_t nt = tiles(k.bm, k.bn), slots = kCUs * k.a_cu, full = nt / slots;
+    // the tiles of the last round, the same number of each problem's
+    const int64_t last = (nt - full * slots + problems - 1) / problems * problems;
+    const double whole = (double)full * (k.a_cu * k.step * steps + 6.0);
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (s > 1 && (!split || s > steps / 8 || nt * s > k.most)) break;
-      const int64_t on = (nt * s + kCUs - 1) / kCUs, rounds = (on + k.a_cu - 1) / k.a_cu;
+      if (s > 1 && (last == 0 || s > steps / 8 || last * s > k.most)) break;
+      const int64_t on = (last * s + kCUs - 1) / kCUs, rounds = (on + k.a_cu - 1) / k.a_cu;
       const double step = on * k.step > rounds * k.lone ? on * k.step : rounds * k.lone;
-      const double us = step * ((steps + s - 1) / s) + 6.0 * rounds + (s > 1 ? 5.0 + 2e-6 * (double)(M * n) * s : 0.0);
+      const double us = whole + step * ((steps + s - 1) / s) + 6.0 * rounds +
+                        (s > 1 ? 5.0 + 2e-6 * k.bm * k.bn * (double)last * s : 0.0);
       if (us < least) {
         least = us;
-        best = Plan{k.t, s};
+        best = Plan{k.t, s > 1 ? (int)last : 0, s};
       }
     }
   }
   return best;
 }
 
-// Room for the shares of a product of T tokens or fewer: grows with T and n, whatever the plans.
-size_t share_bytes_most(bool f32, int T, int n) {
-  const size_t tiles = f32 ? (size_t)2048 * 64 * 64 * 4 : (size_t)512 * 256 * 256 * 4;
-  const size_t rows = (size_t)32 * T * ((n + 3) / 4 * 4) * 4;
-  return rows < tiles ? rows : tiles;
+size_t share_bytes_most(bool f32, int problems, int M, int64_t n, bool tokens) {
+  const size_t cap = f32 ? (size_t)2048 * 64 * 64 * 4 : (size_t)512 * 256 * 256 * 4;
+  if (tokens && M <= 16) return (size_t)kCUs * 3 / 2 * 16 * 64 * 4;
+  if (tokens && M <= 64) return (size_t)kCUs * 3 / 2 * 64 * 64 * 4;
+  const size_t all = (size_t)32 * problems * ((M + 255) / 256 * 256) * ((n + 255) / 256 * 256) * 4;
+  return all < cap ? all : cap;
 }
 
 Plan token_plan(bool f32, int T, int n, int k, int products, bool adapters) {
-  return choose_tile(f32, T, n, products * ceil_div(k, f32 ? step_k<EF32>() : step_k<EBf16>()), true, adapters);
+  return choose_tile(f32, 1, T, n, products * ceil_div(k, f32 ? step_k<EF32>() : step_k<EBf16>()), adapters, true);
 }
 Plan hidden_plan(bool f32, const BlockShape& s, bool adapters) {
-  return choose_tile(f32, s.T, 2 * (int64_t)s.d_ff, ceil_div(s.d, f32 ? step_k<EF32>() : step_k<EBf16>()), false, adapters);
+  return choose_tile(f32, 1, s.T, 2 * (int64_t)s.d_ff, ceil_div(s.d, f32 ? step_k<EF32>() : step_k<EBf16>()), adapters, true);
 }
 
 hipError_t launch_token_product_ks(bool f32, const TokenProduct& p, hipStream_t st) {

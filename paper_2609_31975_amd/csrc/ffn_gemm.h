@@ -74,7 +74,10 @@ struct GemmArgs {
   int K;         // of one product
   int products;  // 1, or 2: the sum over p[0] and p[1] of both operands
   int ntm, ntn;
-  int splits;    // shares of the steps, one workgroup each
+  // The tiles from the `whole`-th on are cut along k: `shares` workgroups to a tile, which write their fp32
+  // sums to part, [tile][share][16-row piece][16-column piece][thread], for k_join to finish.
+  int whole, shares;
+  float* part;
   LowRank lr;
 };
 
@@ -310,17 +313,26 @@ __device__ __forceinline__ void up_grad(int silu, float v, float& u, float& du) 
 // tiles, and walks it in bands of 8 tile rows, so that the tiles it works on at one time share rows of A
 // and of B.
 struct TileAt {
-  int m, n, split;
+  int m, n, cut, share;  // cut: the place among the tiles that are cut, or -1
 };
-__device__ __forceinline__ TileAt tile_at(const GemmArgs& g) {
-  const int n = g.ntm * g.ntn * g.splits;
-  const int q = n / 8, rem = n % 8, x = blockIdx.x % 8, i = blockIdx.x / 8;
-  int t = x * q + min(x, rem) + i;
-  const int split = t % g.splits;
-  t /= g.splits;
+__device__ __forceinline__ TileAt tile_of(const GemmArgs& g, int t) {
   constexpr int kBand = 8;
   const int band = t / (kBand * g.ntn), rows = min(kBand, g.ntm - band * kBand), u = t - band * kBand * g.ntn;
-  return TileAt{band * kBand + u % rows, u / rows, split};
+  return TileAt{band * kBand + u % rows, u / rows, -1, 0};
+}
+// the x-th eighth of [0, n)
+__device__ __forceinline__ int eighth(int n, int b) {
+  const int q = n / 8, rem = n % 8, x = b % 8;
+  return x * q + min(x, rem) + b / 8;
+}
+__device__ __forceinline__ TileAt tile_at(const GemmArgs& g) {
+  const int b = blockIdx.x;
+  if (b < g.whole) return tile_of(g, eighth(g.whole, b));
+  const int u = eighth((int)gridDim.x - g.whole, b - g.whole), cut = u / g.shares;
+  TileAt at = tile_of(g, g.whole + cut);
+  at.cut = cut;
+  at.share = u - cut * g.shares;
+  return at;
 }
 
 // ------------------------------------------------------------------ the pipeline
@@ -503,6 +515,30 @@ struct AdapterSteps {
   }
 };
 
+// ------------------------------------------------------------------ the end of a tile
+// The sums of this wave's i-th 16 rows: lane l of a 16 x 16 piece holds m = l % 16, n = 4 (l / 16) .. + 3.
+template <class C, bool DUAL, class Epi>
+__device__ __forceinline__ void finish(const GemmArgs& g, const Epi& epi, int m0, int n0, int wm, int wn, int i,
+                                       const f32x4_t (&acc)[C::NT]) {
+  constexpr int G = C::WTN / 2;
+  const int lane = lane_id(), m = m0 + wm * C::WTM + i * 16 + (lane & 15);
+  if (m >= g.M) return;
+  if constexpr (DUAL) {
+#pragma unroll
+    for (int j = 0; j < C::NT / 2; ++j) epi.pair(m, n0 + wn * G + j * 16 + 4 * (lane >> 4), acc[j], acc[j + C::NT / 2]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < C::NT; ++j) epi.put(g, m, n0 + wn * C::WTN + j * 16 + 4 * (lane >> 4), acc[j]);
+  }
+}
+// Where this thread's sums of piece (i, j) lie, of a share of a cut tile.  Several results of one launch
+// (blockIdx.y) follow each other.
+template <class C>
+__device__ __forceinline__ f32x4_t* share_at(const GemmArgs& g, int cut, int share, int i, int j) {
+  const size_t tile = ((size_t)blockIdx.y * (g.ntm * g.ntn - g.whole) + cut) * g.shares + share;
+  return reinterpret_cast<f32x4_t*>(g.part) + ((tile * C::MT + i) * C::NT + j) * C::threads + threadIdx.x;
+}
+
 // ------------------------------------------------------------------ the kernel
 // DUAL: B's tile holds W_gate and W_up rows of the same BN / 2 neurons, a wave's columns being half of
 // either, so that its lanes end with both values of their neurons.  AD: adapters.
@@ -532,8 +568,9 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
   const int64_t b0 = LB == Lay::KC ? (int64_t)n0 * g.b.ld * esz<E>() : (int64_t)n0 * esz<E>();
   const int kt = (g.K + step_k<E>() - 1) / step_k<E>();
 
-  const Split shares(kt * g.products, g.splits);
-  const int it0 = shares.start(at.split), it1 = shares.start(at.split + 1);
+  const int shares = at.cut >= 0 ? g.shares : 1;
+  const Split steps(kt * g.products, shares);
+  const int it0 = steps.start(at.share), it1 = steps.start(at.share + 1);
   // loads [f0, f1) of this wave for step `it`; past the last step they fill the buffer with zeros, which
   // nothing uses, so that every step has the same loads in flight
   constexpr int per_step = decltype(la)::per + decltype(lb)::per;
@@ -569,8 +606,8 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
       plan[i] = g.lr.plan[(size_t)at.m * (1 + 2 * C::BM) + i];
     __syncthreads();
     const Steps ad(g.lr, plan, m0, n0);
-    const Split part(ad.count(), g.splits);
-    const int ad0 = part.start(at.split), ad1 = part.start(at.split + 1);
+    const Split part(ad.count(), shares);
+    const int ad0 = part.start(at.share), ad1 = part.start(at.share + 1);
     const bool whole = g.lr.r % E::EPC == 0;
     pipeline<E, C, LA, LB, per_step>(lds, it0, it1, ra, rb, acc, g.M - m0 - wm * C::WTM, g.M - m0 < C::BM, issue);
     meet();  // the last step has been read
@@ -603,22 +640,46 @@ __global__ void __launch_bounds__(C::threads) k_gemm(GemmArgs g, Epi epi) {
     wait_loads<0>();
   }
 
-  // lane l of a 16 x 16 tile: m = l % 16, n = 4 (l / 16) .. + 3
-  const int lane = lane_id();
+  if (at.cut >= 0) {
+    const int left = g.M - m0 - wm * C::WTM - (lane_id() & 15);  // rows of the result from this lane's first on
 #pragma unroll
-  for (int i = 0; i < C::MT; ++i) {
-    const int m = m0 + wm * C::WTM + i * 16 + (lane & 15);
-    if (m >= g.M) continue;
-    if constexpr (DUAL) {
+    for (int i = 0; i < C::MT; ++i)
+      if (i * 16 < left)
 #pragma unroll
-      for (int j = 0; j < C::NT / 2; ++j)
-        epi.pair(m, n0 + wn * G + j * 16 + 4 * (lane >> 4), acc[i][j], acc[i][j + C::NT / 2]);
-    } else {
+        for (int j = 0; j < C::NT; ++j) *share_at<C>(g, at.cut, at.share, i, j) = acc[i][j];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < C::MT; ++i) finish<C, DUAL>(g, epi, m0, n0, wm, wn, i, acc[i]);
+}
+
+// Adds the shares of the cut tiles up, in their order, and finishes them: a workgroup to a tile and 16-row
+// piece of its waves.
+template <class C, bool DUAL, class Epi>
+__global__ void __launch_bounds__(C::threads) k_join(GemmArgs g, Epi epi) {
+  epi.select(g);
+  const int cut = blockIdx.x, i = blockIdx.z;
+  const TileAt at = tile_of(g, g.whole + cut);
+  const int wave = threadIdx.x / kWave, wm = wave / C::WN, wn = wave % C::WN;
+  const int m0 = at.m * C::BM, n0 = at.n * (DUAL ? C::BN / 2 : C::BN);
+  if (m0 + wm * C::WTM + i * 16 + (lane_id() & 15) >= g.M) return;
+  f32x4_t acc[C::NT];
+#pragma unroll
+  for (int j = 0; j < C::NT; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  constexpr int U = C::NT >= 4 ? 2 : 8 / C::NT;  // shares in flight
+  for (int s0 = 0; s0 < g.shares; s0 += U) {
+    f32x4_t v[U][C::NT];
+#pragma unroll
+    for (int s = 0; s < U; ++s)
 #pragma unroll
       for (int j = 0; j < C::NT; ++j)
-        epi.put(g, at.split, m, n0 + wn * C::WTN + j * 16 + 4 * (lane >> 4), acc[i][j]);
-    }
+        v[s][j] = s0 + s < g.shares ? *share_at<C>(g, cut, s0 + s, i, j) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < U; ++s)
+#pragma unroll
+      for (int j = 0; j < C::NT; ++j) acc[j] += v[s][j];
   }
+  finish<C, DUAL>(g, epi, m0, n0, wm, wn, i, acc);
 }
 
 }  // namespace

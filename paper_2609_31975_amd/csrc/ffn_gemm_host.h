@@ -24,11 +24,19 @@ typedef Config<256, 256, 2, 4, 2> Tile256;
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// plan.whole and plan.shares are of `problems` results at once; each has its own grid row.
 template <class E, class C, Lay LA, Lay LB, bool DUAL, bool AD, class Epi>
-hipError_t launch_gemm(GemmArgs g, const Epi& epi, int problems, hipStream_t st) {
+hipError_t launch_gemm(GemmArgs g, const Epi& epi, const Plan& plan, int problems, hipStream_t st) {
   g.ntm = ceil_div(g.M, C::BM);
   g.ntn = ceil_div(g.N, DUAL ? C::BN / 2 : C::BN);
-  k_gemm<E, C, LA, LB, DUAL, AD, Epi><<<dim3(g.ntm * g.ntn * g.splits, problems), C::threads, 0, st>>>(g, epi);
+  const int tiles = g.ntm * g.ntn, cut = plan.cut / problems;
+  g.whole = tiles - cut;
+  g.shares = plan.shares;
+  const int grid = g.whole + cut * plan.shares;
+  k_gemm<E, C, LA, LB, DUAL, AD, Epi><<<dim3(grid, problems), C::threads, 0, st>>>(g, epi);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || cut == 0) return e;
+  k_join<C, DUAL, Epi><<<dim3(cut, problems, C::MT), C::threads, 0, st>>>(g, epi);
   return hipGetLastError();
 }
 
