@@ -336,7 +336,7 @@ int tile_rows(Tile t) {
 // fill the chip, and at ones that leave CUs empty); a round's first loads and stores take 6 us.  The tiles of
 // the last round, where it is not full, may be cut along k in shares that fill it; a share writes its fp32
 // sums, and a second launch reads them (5 us and 4 TB/s).  (4096 tokens, d 2560, d_ff 7168: 840 tiles of the
-// weight gradients are 3 rounds and 72 tiles, in 3 shares each: 449 -> 400 us.)
+// weight gradients are 3 rounds and 72 tiles, in 3 shares each: 449 -> 400 + 15 us.)
 //
 // Few tokens are bound by the weights' bytes, whatever the tile: there shares only fill CUs.
 Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapters, bool tokens) {
@@ -372,12 +372,15 @@ Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapt
     const int64_t nt = tiles(k.bm, k.bn), slots = kCUs * k.a_cu, full = nt / slots;
     // the tiles of the last round, the same number of each problem's
     const int64_t last = (nt - full * slots + problems - 1) / problems * problems;
+    // tiles at the last row leave empty pieces' products out, but not their loads: a third of a tile at least
+    const int over = M % k.bm, rows = (M + k.bm - 1) / k.bm;
+    const double part = over ? over / (double)k.bm : 1.0, used = (rows - 1 + (part > 0.35 ? part : 0.35)) / rows;
     const double whole = (double)full * (k.a_cu * k.step * steps + 6.0);
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (s > 1 && (last == 0 || s > steps / 8 || last * s > k.most)) break;
       const int64_t on = (last * s + kCUs - 1) / kCUs, rounds = (on + k.a_cu - 1) / k.a_cu;
       const double step = on * k.step > rounds * k.lone ? on * k.step : rounds * k.lone;
-      const double us = whole + step * ((steps + s - 1) / s) + 6.0 * rounds +
+      const double us = used * (whole + step * ((steps + s - 1) / s) + 6.0 * rounds) +
                         (s > 1 ? 5.0 + 2e-6 * k.bm * k.bn * (double)last * s : 0.0);
       if (us < least) {
         least = us;
