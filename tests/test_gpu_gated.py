@@ -103,6 +103,45 @@ def test_large_tiles(T, d, d_ff):
     layer.check(layer.train(1, False), 1, False)
 
 
+@pytest.mark.parametrize("T,d,d_ff", [(1, 4096, 64), (5, 2048, 300), (16, 1032, 33), (33, 2048, 130), (64, 3000, 64),
+                                      (70, 2048, 300), (200, 4096, 65), (2, 72, 3000)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_long_rows_in_few_tiles(dtype, T, d, d_ff):
+    """Sums cut in shares in every product: the hidden layer's, dz's and the tokens' own."""
+    layer = Layer(dtype, T, d, d_ff)
+    layer.check(layer.train(1, True), 1, True)
+
+
+@pytest.mark.parametrize("T,d,d_ff", [(6000, 72, 40), (9000, 136, 16), (4096, 8, 8), (5000, 64, 300)])
+def test_gradients_over_many_tokens_of_small_layers(T, d, d_ff):
+    """Weight gradients of a few tiles, their sums over tokens cut in shares."""
+    for dtype in (BF16, F32):
+        layer = Layer(dtype, T, d, d_ff)
+        layer.check(layer.train(2), 2)
+
+
+def test_one_workspace_for_many_calls():
+    """Allocated for the most tokens, used for others in turn, forward and backward."""
+    ws = ffn.alloc_gated_workspace(1500, 264, 700, BF16)
+    for T in (1500, 1, 64, 65, 17, 300, 1000, 2):
+        layer = Layer(BF16, T, 264, 700)
+        layer.check(layer.train(2, ws=ws), 2, what=f"T={T}")
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    layers = [Layer(BF16, T, 264, 900) for T in (40, 333)]
+    sides = [torch.cuda.Stream() for _ in layers]
+    bufs = [(torch.empty_like(a.x), ffn.alloc_gated_workspace(a.T, 264, 900, BF16)) for a in layers]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, side, (y, ws) in zip(layers, sides, bufs):
+            ffn.ffn_gated_forward(a.x, *a.w, a.t, ffn.options(act=2), y, ws, stream=side)
+    torch.cuda.synchronize()
+    for a, (y, _) in zip(layers, bufs):
+        a.check({"y": y}, 2)
+
+
 def test_paper_size_fp32():
     layer = Layer(F32, 130, 3840, 14231)
     layer.check(layer.train(2, True), 2, True)
