@@ -366,9 +366,10 @@ Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapt
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Kind& k = kinds[i];
-    // the adapters' sums beside T256's need more registers than there are; T128 and T64x128 hold too few
-    // steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us in T128, 122 in T128x256)
-    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128 || k.t == Tile::T64x128)) continue;
+    // the adapters' sums beside T256's need more registers than there are; T128 holds too few steps to load
+    // the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us, 122 in T128x256; fp32 products take so
+    // much longer that it does not show in T64x128)
+    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128)) continue;
     const int64_t nt = tiles(k.bm, k.bn), slots = kCUs * k.a_cu, full = nt / slots;
     // the tiles of the last round, the same number of each problem's
     const int64_t last = (nt - full * slots + problems - 1) / problems * problems;

@@ -56,7 +56,7 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
 // the tiles that choose_tile picks for products with adapters
 template <class C>
 constexpr bool adapter_tile() {
-  return C::S >= 3;
+  return C::S >= 3 || C::BM == 64;
 }
 
 inline LowRank low_rank(const AdapterSet& ad, const void* const v[2], const void* const b[2], int out) {
