@@ -133,7 +133,7 @@ struct Loader {
     if constexpr (E::EPC == 8) return ((k & 3) | (CPR >= 16 ? ((k >> 3) & 1) << 2 : 0)) << 1;
     else return ((k >> 2) & 3) << 2;
   }
-  // row(r): the operand's row that LDS row r holds, or -1
+  // row(r): the row, from r0 on, that LDS row r holds
   template <class RowOf>
   __device__ __forceinline__ void init(int64_t ld, int rows, int r0, RowOf row) {
     const int wave = threadIdx.x / kWave, lane = lane_id();
@@ -143,7 +143,7 @@ struct Loader {
       if constexpr (L == Lay::KC) {
         const int c = (lane & 7) ^ (lane >> 3), rr = row(j * 8 + (lane >> 3));
         kpos[i] = c * E::EPC;
-        off[i] = rr >= 0 && rr + r0 < rows ? (uint32_t)rr * (uint32_t)(ld * esz<E>()) + c * 16 : kOOB;
+        off[i] = rr + r0 < rows ? (uint32_t)rr * (uint32_t)(ld * esz<E>()) + c * 16 : kOOB;
       } else {
         const int s = j * kWave + lane, k = s / CPR, c = (s % CPR) ^ swz(k);
         kpos[i] = k;
