@@ -5,6 +5,9 @@
 namespace ffn {
 namespace {
 
+// dg and dv are rounded once, to the type of the products that read them.  The derivative is taken where g is
+// in fp32, so a neuron is on exactly where the forward call had it on.  8192 tokens, 4096 -> 14336: 1070 us, pipes
+// 43% busy; a tile's epilogue reads 512 KB and writes 256 KB.
 template <class E>
 struct EpiDz {
   BlockForm form;
@@ -33,7 +36,8 @@ struct EpiDz {
   }
 };
 
-// Weight gradient i of a launch: blockIdx.y.
+// Weight gradient i of a launch: blockIdx.y.  All of them in one launch fill more rounds of the CUs (three of 14336 x
+// 4096 over 8192 tokens: 2100 to 2200 us, 1.3 PFLOP/s).
 template <class E>
 struct EpiDw {
   const void *a[3], *b[3];
