@@ -248,15 +248,16 @@ struct Half {
   // between(i): work to issue in front of the products of fragment a[i].  LDS reads and loads into LDS
   // are handed out among the products a few at a time: issued in one piece they fill their queues, and a
   // wave that waits for a queue issues no products either.
-  // RAGGED: only the first `rows` of the 16-row pieces have any rows of the result.
-  template <bool RAGGED, class Between>
+  // RAGGED: only the first `rows` of the 16-row pieces have any rows of the result.  J0, J1: only the products of
+  // fragments b[J0] .. b[J1 - 1].
+  template <bool RAGGED, int J0 = 0, int J1 = C::NT, class Between>
   __device__ __forceinline__ void multiply(f32x4_t (&acc)[C::MT][C::NT], int rows, Between between) const {
 #pragma unroll
     for (int i = 0; i < C::MT; ++i) {
       between(i);
       if (!RAGGED || i < rows) {
 #pragma unroll
-        for (int j = 0; j < C::NT; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
+        for (int j = J0; j < J1; ++j) acc[i][j] = product<E>(b[j], a[i], acc[i][j]);
       }
       issue_barrier();
     }
@@ -408,8 +409,8 @@ __device__ __forceinline__ void pipeline(char* lds, int it0, int it1, const Read
 // ------------------------------------------------------------------ adapters within a product
 // The low-rank part is a product over k = (adapter of the tile, rank), rp to an adapter, in chunks:
 // row m of the A tile holds v[m] in its own adapter's chunks and zero in the others, row n of the B tile
-// B_j[n].  A dual product runs W_gate's adapters, with zeros in W_up's rows of the B tile, then
-// W_up's.  Both images are KC.
+// B_j[n].  A dual product runs W_gate's adapters, into W_gate's sums alone (the zeros in W_up's rows of the B
+// tile would turn an Inf or NaN of v into a NaN of W_up's), then W_up's.  Both images are KC.
 //
 // Rows of whole chunks are loaded into LDS some steps ahead, each lane from an address of its own; odd
 // ranks are read by element and written to LDS, a step at a time.  (As further steps of the main part's
@@ -470,14 +471,24 @@ struct AdapterSteps {
   // goes chunk by chunk, each into sums of its own that only its own tokens take.
   template <class H>
   __device__ __forceinline__ void multiply(const H& h, int it, int kk, int wm, f32x4_t (&acc)[C::MT][C::NT]) const {
+    if constexpr (DUAL) {  // the matrix' half of the wave's columns
+      if (matrix(it) == 0) multiply_columns<0, C::NT / 2>(h, it, kk, wm, acc);
+      else multiply_columns<C::NT / 2, C::NT>(h, it, kk, wm, acc);
+    } else {
+      multiply_columns<0, C::NT>(h, it, kk, wm, acc);
+    }
+  }
+  template <int J0, int J1, class H>
+  __device__ __forceinline__ void multiply_columns(const H& h, int it, int kk, int wm,
+                                                   f32x4_t (&acc)[C::MT][C::NT]) const {
     constexpr uint32_t e = E::EPC == 8 ? 0x7f807f80u : 0x7f800000u, one = E::EPC == 8 ? 0x00800080u : 0x00800000u,
                        top = E::EPC == 8 ? 0x80008000u : 0x80000000u;
     uint32_t odd = 0;  // an exponent of all ones carries into its sign's place
 #pragma unroll
-    for (int j = 0; j < C::NT; ++j)
+    for (int j = J0; j < J1; ++j)
       odd |= ((h.b[j].x & e) + one) | ((h.b[j].y & e) + one) | ((h.b[j].z & e) + one) | ((h.b[j].w & e) + one);
     if (__ballot((odd & top) != 0) == 0) {
-      h.template multiply<false>(acc, C::MT, [](int) {});
+      h.template multiply<false, J0, J1>(acc, C::MT, [](int) {});
       return;
     }
     const int lane = lane_id();
@@ -489,7 +500,7 @@ struct AdapterSteps {
         const bool mine = plan[1 + C::BM + wm * C::WTM + i * 16 + (lane & 15)] == slot;
         const uint4 a = here ? h.a[i] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int j = 0; j < C::NT; ++j) {
+        for (int j = J0; j < J1; ++j) {
           const f32x4_t v = product<E>(here ? h.b[j] : make_uint4(0, 0, 0, 0), a, f32x4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[i][j][k] = mine ? acc[i][j][k] + v[k] : acc[i][j][k];
