@@ -37,6 +37,16 @@ BlockShape shape_of(ffn_dtype_t w, int T, int d, int d_ff) {
   return BlockShape{T, d, d_ff, round_up_to(d, chunk(w)), round_up_to(d_ff, 64)};
 }
 
+// the call's tokens from t0 on, `piece` or fewer, and row t0 of rows of n elements
+BlockShape tokens_of(BlockShape s, int64_t t0, int64_t piece) {
+  s.T = (int)std::min(piece, s.T - t0);
+  return s;
+}
+const void* rows_from(ffn_dtype_t w, const void* p, int64_t t0, int n) {
+  return static_cast<const char*>(p) + t0 * n * (int64_t)esize(w);
+}
+void* rows_from(ffn_dtype_t w, void* p, int64_t t0, int n) { return static_cast<char*>(p) + t0 * n * (int64_t)esize(w); }
+
 struct Carver {
   char* base;
   size_t off = 0;
@@ -235,22 +245,30 @@ int ffn_gated_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const void* x, co
 
   const void* b2[2] = {ad ? ad->gate_b : nullptr, ad ? ad->up_b : nullptr};
   const void* v2[2] = {f.v[0], f.v[1]};
-  if (b2[0] || b2[1]) {
-    const void* a[2] = {b2[0] ? ad->gate_a : ad->up_a, ad->up_a};
-    void* v[2] = {b2[0] ? f.v[0] : f.v[1], f.v[1]};
-    FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, b2[0] && b2[1] ? 2 : 1, a, v, hidden_plan(f32, s, true).tile, stream));
-  }
-  AdapterSet hidden = b2[0] || b2[1] ? set : AdapterSet{};
-  FFN_TRY(launch_block_hidden(f32, s, x, w_gate, w_up, form, hidden, v2, b2, sv.z, sv.g, sv.v, f.part, stream));
   const bool down = ad && ad->down_b;
-  if (down) {
-    const void* a[2] = {ad->down_a, nullptr};
-    void* v[2] = {f.v2, nullptr};
-    FFN_TRY(launch_adapter_v(f32, T, d_ff, s.ldf, sv.z, set, 1, a, v, token_plan(f32, T, d, d_ff, 1, true).tile, stream));
+  const int64_t piece = tokens_a_launch(std::max<int64_t>(d, 2 * (int64_t)d_ff), ad != nullptr);
+  for (int64_t t0 = 0; t0 < T; t0 += piece) {
+    const BlockShape p = tokens_of(s, t0, piece);
+    const void* xp = rows_from(wdt, x, t0, s.dp);
+    void* z = rows_from(wdt, sv.z, t0, s.ldf);
+    float *g = sv.g ? sv.g + t0 * s.ldf : nullptr, *v = sv.v ? sv.v + t0 * s.ldf : nullptr;
+    if (ad) set.ids = ad->ids + t0;
+    if (b2[0] || b2[1]) {
+      const void* a[2] = {b2[0] ? ad->gate_a : ad->up_a, ad->up_a};
+      void* vs[2] = {b2[0] ? f.v[0] : f.v[1], f.v[1]};
+      FFN_TRY(launch_adapter_v(f32, p.T, d, s.dp, xp, set, b2[0] && b2[1] ? 2 : 1, a, vs, hidden_plan(f32, p, true).tile, stream));
+    }
+    const AdapterSet hidden = b2[0] || b2[1] ? set : AdapterSet{};
+    FFN_TRY(launch_block_hidden(f32, p, xp, w_gate, w_up, form, hidden, v2, b2, z, g, v, f.part, stream));
+    if (down) {
+      const void* a[2] = {ad->down_a, nullptr};
+      void* vs[2] = {f.v2, nullptr};
+      FFN_TRY(launch_adapter_v(f32, p.T, d_ff, s.ldf, z, set, 1, a, vs, token_plan(f32, p.T, d, d_ff, 1, true).tile, stream));
+    }
+    const TokenProduct q{{z, nullptr}, {w_down_t, nullptr}, 1, p.T, d, d_ff, s.ldf, s.dp, d, rows_from(wdt, y, t0, d),
+                         f.part, down ? set : AdapterSet{}, f.v2, down ? ad->down_b : nullptr};
+    FFN_TRY(launch_token_product_ks(f32, q, stream));
   }
-  const TokenProduct p{{sv.z, nullptr}, {w_down_t, nullptr}, 1, T, d, d_ff, s.ldf, s.dp, d, y, f.part,
-                       down ? set : AdapterSet{}, f.v2, down ? ad->down_b : nullptr};
-  FFN_TRY(launch_token_product_ks(f32, p, stream));
   return FFN_OK;
 }
 
@@ -321,9 +339,16 @@ int ffn_adapter_forward(ffn_dtype_t wdt, int T, int d, int n_out, const void* x,
   FFN_TRY(padded(f32, s, n_out, &w, a.w, stream));
   const void* aa[2] = {ad->gate_a, nullptr};
   void* v[2] = {a.v, nullptr};
-  FFN_TRY(launch_adapter_v(f32, T, d, s.dp, x, set, 1, aa, v, token_plan(f32, T, n_out, d, 1, true).tile, stream));
-  const TokenProduct p{{x, nullptr}, {w, nullptr}, 1, T, n_out, d, s.dp, s.dp, n_out, y, a.part, set, a.v, ad->gate_b};
-  FFN_TRY(launch_token_product_kc(f32, p, stream));
+  const int64_t piece = tokens_a_launch(n_out, true);
+  for (int64_t t0 = 0; t0 < T; t0 += piece) {
+    const BlockShape p = tokens_of(s, t0, piece);
+    const void* xp = rows_from(wdt, x, t0, s.dp);
+    set.ids = ad->ids + t0;
+    FFN_TRY(launch_adapter_v(f32, p.T, d, s.dp, xp, set, 1, aa, v, token_plan(f32, p.T, n_out, d, 1, true).tile, stream));
+    const TokenProduct q{{xp, nullptr}, {w, nullptr}, 1, p.T, n_out, d, s.dp, s.dp, n_out, rows_from(wdt, y, t0, n_out),
+                         a.part, set, a.v, ad->gate_b};
+    FFN_TRY(launch_token_product_kc(f32, q, stream));
+  }
   return FFN_OK;
 }
 

@@ -39,6 +39,15 @@ size_t share_bytes_most(bool f32, int problems, int M, int64_t n, bool tokens);
 // Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.
 inline size_t plan_ints(int T) { return 2 * ((size_t)T + 256) + T / 16 + 1; }
 
+// Tokens that one launch takes of a product with n columns, a multiple of 256, so that no grid comes to 2^32 work items:
+// the tiles have at most one to 16 results, or, with few columns, 8 to a token, and A x takes 1024 to a token where its
+// rows are no whole chunks.  The forward calls take more tokens in pieces.  The backward call needs none: a save and
+// gradients of so many tokens are larger than the card's memory.
+inline int tokens_a_launch(int64_t n, bool adapters) {
+  const int64_t by_columns = ((int64_t)1 << 35) / n / 256 * 256, most = (int64_t)1 << (adapters ? 21 : 27);
+  return (int)(by_columns < most ? by_columns : most);
+}
+
 // Shapes: rows of dp elements (d rounded up to whole chunks), hidden rows of ldf (d_ff rounded up to 64).
 struct BlockShape {
   int T, d, d_ff, dp, ldf;
@@ -72,6 +81,13 @@ hipError_t launch_block_dz(bool f32, const BlockShape& s, const void* dy, const 
 // up to three weight gradients out[i] [d_ff][d] = a[i]^T b[i], a [T][ldf], b [T][dp]
 hipError_t launch_block_dw(bool f32, const BlockShape& s, int count, const void* const a[3], const void* const b[3],
                            void* const out[3], float* part, hipStream_t st);
+// The launch of A x: tokens of k elements, 16 to a group; tiles: through LDS tiles.  A group's adapters go to `lanes`
+// workgroups, a row to `shares`; blocks: groups x lanes x shares.
+struct AdapterPlan {
+  bool tiles;
+  int lanes, shares, blocks;
+};
+AdapterPlan adapter_plan(bool f32, int T, int k, int rp, int count);
 // Room for the shares of the sums, for T tokens or fewer and ranks up to rp.
 size_t adapter_share_bytes_most(int T, int rp, int count);
 // v[i] [T][rp] = scale_j A_j x for up to two stacks, and ad.plan for the product of tile `t` that reads them

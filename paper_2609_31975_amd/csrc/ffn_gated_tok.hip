@@ -4,27 +4,27 @@
 
 namespace ffn {
 
-// Whether the adapters' first factor goes through LDS tiles (k_adapter_v_tiles): with many tokens, and rows of
-// whole chunks.
-static bool v_tiles(bool f32, int T, int k, int count) {
-  return (T + 15) / 16 * count >= kCUs / 2 && k % (f32 ? 4 : 8) == 0;
-}
-
 // Shares of a row, at most 8 (k_adapter_join), so that a few workgroups come to a CU; a share is at least
 // half a round of loads of k_adapter_v's 16 waves, or 8 steps of k_adapter_v_tiles.
 size_t adapter_share_bytes_most(int T, int rp, int count) {
   const int few = 16 * 3 * kCUs;  // beyond, one share
   return (size_t)8 * count * (T < few ? T : few) * rp * 4;
 }
-static int adapter_shares(bool f32, int T, int k, int rp, int count) {
-  const bool tiles = v_tiles(f32, T, k, count);
+AdapterPlan adapter_plan(bool f32, int T, int k, int rp, int count) {
+  const int groups = ceil_div(T, 16);
+  AdapterPlan p;
+  // through LDS tiles with many tokens, and rows of whole chunks
+  p.tiles = (int64_t)groups * count >= kCUs / 2 && k % (f32 ? 4 : 8) == 0;
+  // most tiles of many tokens hold a prompt's, of one request or of two
+  p.lanes = p.tiles ? 2 : T < 16 ? T : 16;
   const int step = f32 ? 16 : 32;  // k of a product
-  const int steps = (k + step - 1) / step;
-  const int64_t groups = (int64_t)((T + 15) / 16) * count *
-                         (tiles ? (rp + 63) / 64 : (T < 16 ? T : 16) * (int64_t)((rp + 15) / 16));
-  int64_t s = (tiles ? 3 : 2) * kCUs / groups;
-  if (s > steps / (tiles ? 16 : 64)) s = steps / (tiles ? 16 : 64);
-  return (int)(s < 1 ? 1 : s > 8 ? 8 : s);
+  const int steps = ceil_div(k, step);
+  const int64_t all = (int64_t)groups * count * (p.tiles ? ceil_div(rp, 64) : (int64_t)p.lanes * ceil_div(rp, 16));
+  int64_t s = (p.tiles ? 3 : 2) * kCUs / all;
+  if (s > steps / (p.tiles ? 16 : 64)) s = steps / (p.tiles ? 16 : 64);
+  p.shares = (int)(s < 1 ? 1 : s > 8 ? 8 : s);
+  p.blocks = groups * p.lanes * p.shares;
+  return p;
 }
 
 namespace {
@@ -287,22 +287,19 @@ __global__ void __launch_bounds__(kBlock) k_adapter_join(AdapterV p, int blocks)
 
 template <class E>
 hipError_t adapter_v(AdapterV p, hipStream_t st) {
-  const int tiles = ceil_div(p.T, 16), plans = ceil_div(p.T, p.bm);
-  const bool f32 = E::EPC == 4, by_tiles = v_tiles(f32, p.T, p.k, p.count);
-  p.shares = adapter_shares(f32, p.T, p.k, p.rp, p.count);
-  if (by_tiles) {
-    // most tiles hold a prompt's tokens, of one request or of two
-    p.lanes = 2;
-    p.blocks = tiles * p.lanes * p.shares;
+  const int plans = ceil_div(p.T, p.bm);
+  const AdapterPlan plan = adapter_plan(E::EPC == 4, p.T, p.k, p.rp, p.count);
+  p.shares = plan.shares;
+  p.lanes = plan.lanes;
+  p.blocks = plan.blocks;
+  if (plan.tiles) {
     k_adapter_v_tiles<E><<<dim3(p.blocks, ceil_div(p.rp, Tile16::BN), p.count), Tile16::threads, 0, st>>>(p);
   } else {
-    p.lanes = p.T < 16 ? p.T : 16;
-    p.blocks = tiles * p.lanes * p.shares;
     const dim3 grid(p.blocks + (p.shares == 1 ? plans : 0), ceil_div(p.rp, 16), p.count);
     if (p.k % E::EPC == 0) k_adapter_v<E, true><<<grid, kVWaves * kWave, 0, st>>>(p);
     else k_adapter_v<E, false><<<grid, kVWaves * kWave, 0, st>>>(p);
   }
-  if (by_tiles || p.shares > 1) {
+  if (plan.tiles || p.shares > 1) {
     const int blocks = p.shares > 1 ? ceil_div(p.count * p.T * (p.rp / 4), kBlock) : 0;
     k_adapter_join<E><<<blocks + plans, kBlock, 0, st>>>(p, blocks);
   }
@@ -342,7 +339,7 @@ int tile_rows(Tile t) {
 //
 // Few tokens are bound by the weights' bytes, whatever the tile: there shares only fill CUs.
 Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapters, bool tokens) {
-  auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((n + bn - 1) / bn) * problems; };
+  auto tiles = [&](int bm, int bn) { return ((int64_t)M + bm - 1) / bm * ((n + bn - 1) / bn) * problems; };
   if (tokens && M <= 64) {
     const bool few = M <= 16;
     const int64_t nt = tiles(few ? 16 : 64, 64);
@@ -398,7 +395,7 @@ size_t share_bytes_most(bool f32, int problems, int M, int64_t n, bool tokens) {
   const size_t cap = f32 ? (size_t)2048 * 64 * 64 * 4 : (size_t)512 * 256 * 256 * 4;
   if (tokens && M <= 16) return (size_t)kCUs * 3 / 2 * 16 * 64 * 4;
   if (tokens && M <= 64) return (size_t)kCUs * 3 / 2 * 64 * 64 * 4;
-  const size_t all = (size_t)32 * problems * ((M + 255) / 256 * 256) * ((n + 255) / 256 * 256) * 4;
+  const size_t all = (size_t)32 * problems * (((int64_t)M + 255) / 256 * 256) * ((n + 255) / 256 * 256) * 4;
   return all < cap ? all : cap;
 }
 

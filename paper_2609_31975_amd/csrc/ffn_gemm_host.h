@@ -22,7 +22,7 @@ typedef Config<128, 128, 2, 2, 2> Tile128;
 typedef Config<128, 256, 2, 4, 3> Tile128x256;
 typedef Config<256, 256, 2, 4, 2> Tile256;
 
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+inline int ceil_div(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
 
 // plan.whole and plan.shares are of `problems` results at once; each has its own grid row.
 template <class E, class C, Lay LA, Lay LB, bool DUAL, bool AD, class Epi>
