@@ -54,10 +54,7 @@ hipError_t hidden(const BlockShape& s, const void* x, const void* w_gate, const 
   const EpiGated<E> epi{form, s.d_ff, s.ldf, static_cast<typename E::T*>(z), g, v};
   const Plan plan = hidden_plan(E::EPC == 4, s, ad.plan != nullptr);
   return with_tile<E>(plan.tile, [&](auto c) {
-    typedef decltype(c) C;
-    if constexpr (adapter_tile<C>())
-      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, Lay::KC, true, true>(a, epi, plan, 1, st);
-    return launch_gemm<E, C, Lay::KC, Lay::KC, true, false>(a, epi, plan, 1, st);
+    return launch_with_adapters<E, decltype(c), Lay::KC, Lay::KC, true>(a, epi, plan, st);
   });
 }
 

@@ -34,6 +34,7 @@ struct Plan {
 };
 Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapters, bool tokens);
 int tile_rows(Tile t);
+bool takes_adapters(Tile t);  // products with adapters are built for it
 // Room for the shares of a product of M rows or fewer and n columns, whatever its plan.
 size_t share_bytes_most(bool f32, int problems, int M, int64_t n, bool tokens);
 // Entries of the adapters' plan of T tokens, whatever the tile: one or more tiles of tile_rows() rows.

@@ -65,10 +65,7 @@ hipError_t product(const TokenProduct& p, hipStream_t st) {
   if (p.ad.plan) a.lr = low_rank(p.ad, v, b, p.n);
   const EpiTok<E> epi{static_cast<typename E::T*>(p.out), p.ldo, p.n % 4 == 0};
   return with_tile<E>(plan.tile, [&](auto c) {
-    typedef decltype(c) C;
-    if constexpr (adapter_tile<C>())
-      if (a.lr.plan) return launch_gemm<E, C, Lay::KC, LB, false, true>(a, epi, plan, 1, st);
-    return launch_gemm<E, C, Lay::KC, LB, false, false>(a, epi, plan, 1, st);
+    return launch_with_adapters<E, decltype(c), Lay::KC, LB, false>(a, epi, plan, st);
   });
 }
 
@@ -330,6 +327,17 @@ int tile_rows(Tile t) {
   }
 }
 
+bool takes_adapters(Tile t) {
+  switch (t) {
+    case Tile::T16: return adapter_tile<Tile16>();
+    case Tile::T64: return adapter_tile<Tile64>();
+    case Tile::T64x128: return adapter_tile<Tile64x128>();
+    case Tile::T128: return adapter_tile<Tile128>();
+    case Tile::T128x256: return adapter_tile<Tile128x256>();
+    default: return adapter_tile<Tile256>();
+  }
+}
+
 // By an estimate of the time, in us.  Tiles run in rounds over the CUs, `a_cu` to a CU.  A step of a tile takes
 // `step` of a CU that is full, and no less than `lone` where it has the CU for itself (measured at sizes that
 // fill the chip, and at ones that leave CUs empty); a round's first loads and stores take 6 us.  The tiles of
@@ -365,10 +373,7 @@ Plan choose_tile(bool f32, int problems, int M, int64_t n, int steps, bool adapt
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Kind& k = kinds[i];
-    // the adapters' sums beside T256's need more registers than there are; T128 holds too few steps to load
-    // the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us, 122 in T128x256; fp32 products take so
-    // much longer that it does not show in T64x128)
-    if (adapters && (k.t == Tile::T256 || k.t == Tile::T128)) continue;
+    if (adapters && !takes_adapters(k.t)) continue;
     const int64_t nt = tiles(k.bm, k.bn), slots = kCUs * k.a_cu, full = nt / slots;
     // the tiles of the last round, the same number of each problem's
     const int64_t last = (nt - full * slots + problems - 1) / problems * problems;

@@ -24,7 +24,7 @@ typedef Config<256, 256, 2, 4, 2> Tile256;
 
 inline int ceil_div(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
 
-// plan.whole and plan.shares are of `problems` results at once; each has its own grid row.
+// plan.cut counts the tiles of all `problems` results, each of which has its own grid row.
 template <class E, class C, Lay LA, Lay LB, bool DUAL, bool AD, class Epi>
 hipError_t launch_gemm(GemmArgs g, const Epi& epi, const Plan& plan, int problems, hipStream_t st) {
   g.ntm = ceil_div(g.M, C::BM);
@@ -53,7 +53,10 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
   else *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, o);
 }
 
-// the tiles that choose_tile picks for products with adapters
+// The tiles that products with adapters are built for, and so the ones that choose_tile picks for them
+// (takes_adapters): the adapters' sums beside Tile256's need more registers than there are, and Tile128 holds too few
+// steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us, 122 in Tile128x256 at that
+// time; fp32 products take so much longer that it does not show in Tile64x128).
 template <class C>
 constexpr bool adapter_tile() {
   return C::S >= 3 || C::BM == 64;
@@ -63,7 +66,7 @@ inline LowRank low_rank(const AdapterSet& ad, const void* const v[2], const void
   return LowRank{{v[0], v[1]}, {b[0], b[1]}, ad.plan, ad.r, ad.rp, out};
 }
 
-// f(Config{}) for the tile that choose_tile picked
+// f(Config{}) for the tile that choose_tile picked; a tile of the other type is an error
 template <class E, class F>
 hipError_t with_tile(Tile t, F f) {
   switch (t) {
@@ -74,10 +77,20 @@ hipError_t with_tile(Tile t, F f) {
   if constexpr (E::EPC == 8) {
     if (t == Tile::T128) return f(Tile128{});
     if (t == Tile::T128x256) return f(Tile128x256{});
-    return f(Tile256{});
+    if (t == Tile::T256) return f(Tile256{});
   } else {
-    return f(Tile64x128{});
+    if (t == Tile::T64x128) return f(Tile64x128{});
   }
+  return hipErrorInvalidValue;
+}
+
+// The product with adapters, or without where a.lr has none.  A plan for adapters whose tile has none built is an
+// error: the product without them would be a wrong result.
+template <class E, class C, Lay LA, Lay LB, bool DUAL, class Epi>
+hipError_t launch_with_adapters(const GemmArgs& a, const Epi& epi, const Plan& plan, hipStream_t st) {
+  if (!a.lr.plan) return launch_gemm<E, C, LA, LB, DUAL, false>(a, epi, plan, 1, st);
+  if constexpr (adapter_tile<C>()) return launch_gemm<E, C, LA, LB, DUAL, true>(a, epi, plan, 1, st);
+  else return hipErrorInvalidValue;
 }
 
 }  // namespace
