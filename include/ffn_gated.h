@@ -37,9 +37,9 @@
  * order).
  *
  * Special values: a NaN gate value gives A = A' = 0 with FFN_ACT_RELU and FFN_ACT_RSPLUS (it is
- * not above the border) and NaN with FFN_ACT_SILU.  Inf and NaN of a token reach that token's
- * outputs and dx and every weight gradient, and no other token's; those of an adapter's factors reach the
- * tokens of that adapter only.
+ * not above the border) and NaN with FFN_ACT_SILU; SiLU of -Inf is NaN too (-Inf times 0).  Inf and
+ * NaN of a token reach that token's outputs and dx and every weight gradient, and no other token's; those of an
+ * adapter's factors reach the tokens of that adapter only, and g or v only through their own projection.
  */
 #ifndef FFN_GATED_H
 #define FFN_GATED_H

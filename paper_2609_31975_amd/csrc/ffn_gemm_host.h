@@ -11,8 +11,9 @@ namespace {
 //   16, 64      a few tokens: the weights are streamed past them, 2 to 4 workgroups a CU (28672 x 4096 bf16
 //               weights, 1..48 tokens: 36 to 38 us, 6.4 TB/s; 128 columns a tile 38 to 40)
 //   64, 64x128  fp32, any number of tokens: the fp32 products bound it (512 x 28460 x
-//               3840: 123 and 138 TFLOP/s, the card's library product 133), and small tiles waste the least
-//               of odd sizes
+//               3840, k contiguous in both: 123 and 138 TFLOP/s, the card's library product 133; a training
+//               step over 513 tokens, most of whose products read a strided operand by element, 112), and
+//               small tiles waste the least of odd sizes
 //   128, 128x256, 256  bf16, many tokens: 1030, 1150 and 1300 TFLOP/s where the tiles fill the chip
 //               (8192 x 4096 x 14336; the card's library product reaches 1360 to 1480)
 typedef Config<16, 64, 1, 2, 4> Tile16;
@@ -55,8 +56,8 @@ __device__ __forceinline__ void store4(typename E::T* p, f32x4_t x) {
 
 // The tiles that products with adapters are built for, and so the ones that choose_tile picks for them
 // (takes_adapters): the adapters' sums beside Tile256's need more registers than there are, and Tile128 holds too few
-// steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: 159 us, 122 in Tile128x256 at that
-// time; fp32 products take so much longer that it does not show in Tile64x128).
+// steps to load the adapters ahead (3000 tokens, 4096 x 4096, rank 64: the call 173 us, 131 in Tile128x256; fp32
+// products take so much longer that it does not show in Tile64x128).
 template <class C>
 constexpr bool adapter_tile() {
   return C::S >= 3 || C::BM == 64;
