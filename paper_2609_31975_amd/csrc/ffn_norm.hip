@@ -1,0 +1,414 @@
+// include/ffn_norm.h: the norms before and after a block with its gate and residual, and their backward
+// pass.  Both move bytes: a token's row is read once into registers, its one or two means are summed
+// across the threads that hold it, and the outputs are written from the registers.
+#include <math.h>
+
+#include <algorithm>
+
+#include "ffn_norm.h"
+#include "ffn_step_device.h"
+
+namespace ffn {
+namespace {
+
+// Threads to a row (TPR) and elements to a thread (EPT).  A wave or a workgroup holds a row of up to
+// TPR EPT elements; 64 threads take 4 rows to a workgroup and need no barrier.
+constexpr int kMaxNormRow = 16384;
+
+struct NormArgs {
+  int T, d;
+  float alpha, eps;
+  int post, sigmoid, gate_rows;
+  const void *x, *f, *gate, *post_gain, *pre_gain;
+  void *x_out, *n_out;
+  float* rstd;
+};
+
+// The elements of a row that a thread holds: whole 16-byte chunks (VEC), a row's chunks dealt out over its
+// threads, or single elements dealt out the same way.
+template <bool F32, int TPR, int EPT, bool VEC>
+struct Part {
+  static constexpr int E = VEC ? (F32 ? 4 : 8) : 1, N = EPT / E;
+  static __device__ __forceinline__ int at(int t, int i) { return (i * TPR + t) * E; }
+
+  static __device__ __forceinline__ void load(const void* p, int64_t row, int d, int t, float (&v)[EPT], float none = 0.f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = at(t, i);
+      const bool on = e < d;
+      const int64_t o = row * d + (on ? e : 0);
+      if constexpr (VEC) {
+        uint4 c = *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + o * (F32 ? 4 : 2));
+        float u[E];
+        if constexpr (F32) unpack(WF32{}, c, u);
+        else unpack(WBf16{}, c, u);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[i * E + j] = on ? u[j] : none;
+      } else {
+        const float u = F32 ? static_cast<const float*>(p)[o] : bf_to_f(static_cast<const uint16_t*>(p)[o]);
+        v[i] = on ? u : none;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t row, int d, int t, const float (&v)[EPT]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = at(t, i);
+      if (e >= d) continue;
+      const int64_t o = row * d + e;
+      if constexpr (VEC && F32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(p) + o) = make_float4(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]);
+      } else if constexpr (VEC) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = f_to_bf2(v[i * 8 + 2 * j], v[i * 8 + 2 * j + 1]);
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + o) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else if constexpr (F32) {
+        static_cast<float*>(p)[o] = v[i];
+      } else {
+        static_cast<uint16_t*>(p)[o] = f_to_bf(v[i]);
+      }
+    }
+  }
+};
+
+// Sum over the threads of a row.  `room`: TPR / 64 floats of LDS that no earlier sum of the same row used, and none
+// that is still being read: the sums of a row use rooms of their own, and each row's first barrier lies between
+// the last row's reads of a room and this row's writes of it.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* room) {
+  v = wave_sum(v);
+  if constexpr (TPR == 64) return v;
+  if (lane_id() == 0) room[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < TPR / 64; ++i) s += room[i];
+  return s;
+}
+
+template <bool F32, int TPR, int EPT, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) {
+  using P = Part<F32, TPR, EPT, VEC>;
+  constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
+  __shared__ float room[2][2][16];
+  const int t = threadIdx.x % TPR;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    float x[EPT], u[EPT], c[EPT];
+    P::load(a.x, row, a.d, t, x);
+    if (a.f) {
+      P::load(a.f, row, a.d, t, u);
+      if (a.gate_rows) P::load(a.gate, a.gate_rows == 1 ? 0 : row, a.d, t, c);
+      if (a.post) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) s += u[i] * u[i];
+        const float r = 1.f / sqrtf(row_sum<TPR>(s, room[turn][0]) / (float)a.d + a.eps);
+        if (t == 0 && a.rstd) a.rstd[row] = r;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) u[i] *= r;
+        if (a.post_gain) {
+          float w[EPT];
+          P::load(a.post_gain, 0, a.d, t, w);
+#pragma unroll
+          for (int i = 0; i < EPT; ++i) u[i] *= w[i];
+        }
+      }
+      if (a.gate_rows) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) u[i] *= a.sigmoid ? 1.f / (1.f + expf(-c[i])) : c[i];
+      }
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) x[i] = a.alpha * x[i] + u[i];
+    }
+    if (a.x_out) P::store(a.x_out, row, a.d, t, x);
+    if (a.n_out) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) s += x[i] * x[i];
+      const float r = 1.f / sqrtf(row_sum<TPR>(s, room[turn][1]) / (float)a.d + a.eps);
+      if (t == 0 && a.rstd) a.rstd[(int64_t)a.T + row] = r;
+      float w[EPT];
+      if (a.pre_gain) P::load(a.pre_gain, 0, a.d, t, w);
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) x[i] *= a.pre_gain ? r * w[i] : r;
+      P::store(a.n_out, row, a.d, t, x);
+    }
+  }
+}
+
+struct NormBack {
+  int T, d;
+  float alpha;
+  int post, sigmoid, gate_rows;
+  const void *x_out, *f, *gate, *post_gain, *pre_gain;
+  const float* rstd;
+  const void *dn, *dx_out;
+  void *dx, *df, *dgate;   // dgate: rows of T (of one row: summed)
+  float* part[3];          // [groups][d] of dpre_gain, dpost_gain, dgate of one row; null: not wanted
+};
+
+// One group of threads takes every groups-th row and keeps its columns' sums over them in registers.
+template <bool F32, int TPR, int EPT, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_bwd(NormBack a) {
+  using P = Part<F32, TPR, EPT, VEC>;
+  constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
+  __shared__ float room[2][2][16];
+  const int t = threadIdx.x % TPR;
+  const int64_t group = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  float sp[EPT] = {}, so[EPT] = {}, sg[EPT] = {};
+  const bool block_side = a.f && (a.df || a.dgate || a.part[1] || a.part[2]);
+  int turn = 0;
+  for (int64_t row = group; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    float g[EPT], f[EPT], c[EPT];
+    if (a.dx_out) P::load(a.dx_out, row, a.d, t, g);
+    if (block_side) {
+      P::load(a.f, row, a.d, t, f);
+      if (a.gate_rows) P::load(a.gate, a.gate_rows == 1 ? 0 : row, a.d, t, c);
+    }
+    if (a.dn) {
+      float n[EPT], xh[EPT], w[EPT];
+      P::load(a.dn, row, a.d, t, n);
+      P::load(a.x_out, row, a.d, t, xh);
+      if (a.pre_gain) P::load(a.pre_gain, 0, a.d, t, w);
+      const float r = a.rstd[(int64_t)a.T + row];
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        xh[i] *= r;
+        if (a.part[0]) sp[i] += n[i] * xh[i];
+        if (a.pre_gain) n[i] *= w[i];
+        s += n[i] * xh[i];
+      }
+      const float m = row_sum<TPR>(s, room[turn][0]) / (float)a.d;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        const float v = r * (n[i] - xh[i] * m);
+        g[i] = a.dx_out ? g[i] + v : v;
+      }
+    }
+    if (a.dx) {
+      float v[EPT];
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) v[i] = a.alpha * g[i];
+      P::store(a.dx, row, a.d, t, v);
+    }
+    if (!block_side) continue;
+    // du = c G (in g), with dgate = G u c'
+    const float rf = a.post ? a.rstd[row] : 1.f;
+    float w[EPT];
+    if (a.post && a.post_gain) P::load(a.post_gain, 0, a.d, t, w);
+    else {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) w[i] = 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) f[i] *= rf;
+    if (a.gate_rows) {
+      float dg[EPT];
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        float slope = 1.f;
+        if (a.sigmoid) {
+          c[i] = 1.f / (1.f + expf(-c[i]));
+          slope = c[i] * (1.f - c[i]);
+        }
+        dg[i] = g[i] * (f[i] * w[i]) * slope;
+        if (a.part[2]) sg[i] += dg[i];
+        g[i] *= c[i];
+      }
+      if (a.dgate && a.gate_rows != 1) P::store(a.dgate, row, a.d, t, dg);
+    }
+    if (a.post) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        if (a.part[1]) so[i] += g[i] * f[i];
+        g[i] *= w[i];
+        s += g[i] * f[i];
+      }
+      if (a.df) {
+        const float m = row_sum<TPR>(s, room[turn][1]) / (float)a.d;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) g[i] = rf * (g[i] - f[i] * m);
+      }
+    }
+    if (a.df) P::store(a.df, row, a.d, t, g);
+  }
+  auto put = [&](float* p, const float(&v)[EPT]) {
+    if (!p) return;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+      const int e = P::at(t, i / P::E) + i % P::E;
+      if (e < a.d) p[group * a.d + e] = v[i];
+    }
+  };
+  put(a.part[0], sp);
+  put(a.part[1], so);
+  put(a.part[2], sg);
+}
+
+// out[i] [d] = sum over the groups' rows of part[i], in a fixed order: 16 threads to a column take every
+// 16th row each, and one joins them.
+struct NormSums {
+  int groups, d;
+  const float* part[3];
+  void* out[3];
+};
+template <bool F32>
+__global__ __launch_bounds__(1024) void k_norm_sums(NormSums a) {
+  __shared__ float s[16][64];
+  const int c = blockIdx.x * 64 + lane_id(), w = threadIdx.x >> 6;
+  const float* p = a.part[blockIdx.y];
+  float v = 0.f;
+  if (c < a.d)
+    for (int r = w; r < a.groups; r += 16) v += p[(int64_t)r * a.d + c];
+  s[w][lane_id()] = v;
+  __syncthreads();
+  if (w == 0 && c < a.d) {
+    float u = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u += s[i][lane_id()];
+    if constexpr (F32) static_cast<float*>(a.out[blockIdx.y])[c] = u;
+    else static_cast<uint16_t*>(a.out[blockIdx.y])[c] = f_to_bf(u);
+  }
+}
+
+struct NormPlan {
+  int tpr, ept;
+};
+NormPlan norm_plan(int d) {
+  const int tpr = d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
+  return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
+}
+// Rows in flight in the backward call, and so rows of the partial sums.
+int back_groups(int T, int d) {
+  const NormPlan p = norm_plan(d);
+  const int most = p.tpr == 64 ? 2048 : p.tpr == 256 ? 1024 : 512, rows = p.tpr == 64 ? 4 : 1;
+  return std::min(most, ceil_div(T, rows) * rows);
+}
+
+template <bool F32, bool VEC, class F>
+hipError_t with_plan(const NormPlan& p, const F& go) {
+  switch (p.tpr) {
+#define FFN_NORM_CASE(n)                                                              \
+  case n:                                                                             \
+    return p.ept == 8 ? go(std::integral_constant<int, n>{}, std::integral_constant<int, 8>{}) \
+                      : go(std::integral_constant<int, n>{}, std::integral_constant<int, 16>{});
+    FFN_NORM_CASE(64)
+    FFN_NORM_CASE(256)
+    FFN_NORM_CASE(512)
+    FFN_NORM_CASE(1024)
+#undef FFN_NORM_CASE
+  }
+  return hipErrorInvalidValue;
+}
+
+template <bool F32, bool VEC>
+hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
+  return with_plan<F32, VEC>(norm_plan(a.d), [&](auto tpr, auto ept) {
+    constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
+    const int blocks = std::min(ceil_div(a.T, ROWS), 1 << 20);
+    k_norm_fwd<F32, tpr.value, ept.value, VEC><<<blocks, WG, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+template <bool F32, bool VEC>
+hipError_t launch_bwd(const NormBack& a, int groups, hipStream_t st) {
+  return with_plan<F32, VEC>(norm_plan(a.d), [&](auto tpr, auto ept) {
+    constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
+    k_norm_bwd<F32, tpr.value, ept.value, VEC><<<groups / ROWS, WG, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+
+int check_norm_shape(int T, int d) {
+  if (T < 1 || d < 1 || d > kMaxNormRow || (int64_t)T * d >= kMaxElems) return FFN_ERR_SHAPE;
+  return FFN_OK;
+}
+int check_norm_form(const ffn_norm_t* n, int T, bool f) {
+  if (!isfinite(n->alpha) || !isfinite(n->eps) || !(n->eps > 0.f)) return FFN_ERR_OPTION;
+  if ((n->post != 0 && n->post != 1) || (n->gate_sigmoid != 0 && n->gate_sigmoid != 1)) return FFN_ERR_OPTION;
+  if (n->gate_rows != 0 && n->gate_rows != 1 && n->gate_rows != T) return FFN_ERR_OPTION;
+  if ((n->gate_rows != 0) != (n->gate != nullptr) || (n->gate_sigmoid && !n->gate)) return FFN_ERR_OPTION;
+  if (n->post_gain && !n->post) return FFN_ERR_OPTION;
+  if (!f && (n->alpha != 1.f || n->post || n->gate)) return FFN_ERR_OPTION;
+  if (!aligned(n->gate) || !aligned(n->post_gain) || !aligned(n->pre_gain)) return FFN_ERR_ALIGN;
+  return FFN_OK;
+}
+
+}  // namespace
+}  // namespace ffn
+
+using namespace ffn;
+
+extern "C" {
+
+int ffn_norm_forward(ffn_dtype_t dt, int T, int d, const void* x, const void* f, const ffn_norm_t* form, void* x_out,
+                     void* n_out, float* rstd, hipStream_t stream) {
+  if (!x || !form || (!x_out && !n_out)) return FFN_ERR_NULL;
+  if (!known(dt)) return FFN_ERR_DTYPE;
+  if (const int rc = check_norm_shape(T, d)) return rc;
+  if (!aligned(x) || !aligned(f) || !aligned(x_out) || !aligned(n_out) || !aligned(rstd, 4)) return FFN_ERR_ALIGN;
+  if (const int rc = check_norm_form(form, T, f != nullptr)) return rc;
+  if ((!f && x_out) || (!n_out && form->pre_gain)) return FFN_ERR_OPTION;
+  const NormArgs a{T, d, form->alpha, form->eps, form->post, form->gate_sigmoid, form->gate_rows, x, f,
+                   form->gate, form->post_gain, form->pre_gain, x_out, n_out, rstd};
+  const hipError_t e = dt == FFN_F32 ? (d % 4 ? launch_fwd<true, false>(a, stream) : launch_fwd<true, true>(a, stream))
+                                     : (d % 8 ? launch_fwd<false, false>(a, stream) : launch_fwd<false, true>(a, stream));
+  return e == hipSuccess ? FFN_OK : FFN_ERR_HIP;
+}
+
+size_t ffn_norm_workspace_bytes(int T, int d) {
+  if (check_norm_shape(T, d) != FFN_OK) return 0;
+  Carver c{nullptr};
+  for (int i = 0; i < 3; ++i) c.take(sizeof(float) * back_groups(T, d) * (size_t)d);
+  return c.off;
+}
+
+int ffn_norm_backward(ffn_dtype_t dt, int T, int d, const void* x_out, const void* f, const ffn_norm_t* form,
+                      const float* rstd, const void* dn, const void* dx_out, void* dx, void* df, void* dgate,
+                      void* dpost_gain, void* dpre_gain, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!form || !ws || (!dn && !dx_out) || (!dx && !df && !dgate && !dpost_gain && !dpre_gain)) return FFN_ERR_NULL;
+  if (!known(dt)) return FFN_ERR_DTYPE;
+  if (const int rc = check_norm_shape(T, d)) return rc;
+  for (const void* p : {x_out, f, dn, dx_out, (const void*)dx, (const void*)df, (const void*)dgate,
+                        (const void*)dpost_gain, (const void*)dpre_gain, (const void*)ws})
+    if (!aligned(p)) return FFN_ERR_ALIGN;
+  if (!aligned(rstd, 4)) return FFN_ERR_ALIGN;
+  if (const int rc = check_norm_form(form, T, f != nullptr)) return rc;
+  if ((!f && df) || (!form->gate && dgate) || (!form->post && dpost_gain) || (!dn && dpre_gain)) return FFN_ERR_OPTION;
+  if ((dn && !x_out) || ((dn || form->post) && !rstd)) return FFN_ERR_NULL;
+  if (ws_bytes < ffn_norm_workspace_bytes(T, d)) return FFN_ERR_WORKSPACE;
+
+  const int groups = back_groups(T, d);
+  Carver c{static_cast<char*>(ws)};
+  float* room[3];
+  for (float*& p : room) p = static_cast<float*>(c.take(sizeof(float) * groups * (size_t)d));
+  const bool row_gate = dgate && form->gate_rows == 1;
+  NormBack a{T, d, form->alpha, form->post, form->gate_sigmoid, form->gate_rows, x_out, f, form->gate, form->post_gain,
+             form->pre_gain, rstd, dn, dx_out, dx, df, dgate,
+             {dpre_gain ? room[0] : nullptr, dpost_gain ? room[1] : nullptr, row_gate ? room[2] : nullptr}};
+  const bool f32 = dt == FFN_F32;
+  hipError_t e = f32 ? (d % 4 ? launch_bwd<true, false>(a, groups, stream) : launch_bwd<true, true>(a, groups, stream))
+                     : (d % 8 ? launch_bwd<false, false>(a, groups, stream) : launch_bwd<false, true>(a, groups, stream));
+  if (e != hipSuccess) return FFN_ERR_HIP;
+  NormSums s{groups, d, {}, {}};
+  int n = 0;
+  void* outs[3] = {dpre_gain, dpost_gain, row_gate ? dgate : nullptr};
+  for (int i = 0; i < 3; ++i)
+    if (outs[i]) {
+      s.part[n] = a.part[i];
+      s.out[n++] = outs[i];
+    }
+  if (n) {
+    const dim3 grid(ceil_div(d, 64), n);
+    if (f32) k_norm_sums<true><<<grid, 1024, 0, stream>>>(s);
+    else k_norm_sums<false><<<grid, 1024, 0, stream>>>(s);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? FFN_OK : FFN_ERR_HIP;
+}
+
+}  // extern "C"

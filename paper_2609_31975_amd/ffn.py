@@ -15,7 +15,7 @@ import re
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libffn_sparse.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "ffn_sparse.h")
-HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h")]
+HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h", "ffn_norm.h")]
 
 FFN_F32 = 0
 FFN_BF16 = 1
@@ -47,6 +47,13 @@ class AdapterStruct(ctypes.Structure):
     """``ffn_adapters_t``: the adapters of a call's requests (device pointers)."""
     _fields_ = [("n", ctypes.c_int), ("r", ctypes.c_int)] + [
         (f, ctypes.c_void_p) for f in ("ids", "scale", "gate_a", "gate_b", "up_a", "up_b", "down_a", "down_b")]
+
+
+class NormStruct(ctypes.Structure):
+    """``ffn_norm_t``: the norms around a block, its gate and the residual's scale."""
+    _fields_ = [("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("post", ctypes.c_int),
+                ("gate_sigmoid", ctypes.c_int), ("gate_rows", ctypes.c_int), ("gate", ctypes.c_void_p),
+                ("post_gain", ctypes.c_void_p), ("pre_gain", ctypes.c_void_p)]
 
 
 class FFNError(RuntimeError):
@@ -108,6 +115,13 @@ def lib() -> ctypes.CDLL:
                 ("ffn_gated_forward", i, [i, i, i, i, vp, vp, vp, vp, f, op, ap, vp, vp, sz, vp, sz, vp]),
                 ("ffn_gated_backward", i, [i, i, i, i, vp, vp, vp, vp, op, vp, vp, sz, vp, vp, vp, vp, vp, sz, vp]),
                 ("ffn_adapter_forward", i, [i, i, i, i, vp, vp, ap, vp, vp, sz, vp])):
+            getattr(L, name).restype = res
+            getattr(L, name).argtypes = args
+        np_ = ctypes.POINTER(NormStruct)
+        for name, res, args in (
+                ("ffn_norm_forward", i, [i, i, i, vp, vp, np_, vp, vp, vp, vp]),
+                ("ffn_norm_workspace_bytes", sz, [i, i]),
+                ("ffn_norm_backward", i, [i, i, i, vp, vp, np_] + [vp] * 9 + [sz, vp])):
             getattr(L, name).restype = res
             getattr(L, name).argtypes = args
         L.ffn_status_string.restype = ctypes.c_char_p
@@ -639,6 +653,81 @@ def ffn_adapter_forward(x, w, adapters, y, ws, stream=None):
                                           y.data_ptr(), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
     _check("ffn_adapter_forward", rc)
     return y
+
+
+# ---------------------------------------------------------------- the norms before and after a block
+class Norm:
+    """The form of the norms around a block: the ``ffn_norm_t`` and the tensors it points into."""
+
+    def __init__(self, eps, pre_gain=None, post=False, post_gain=None, gate=None, gate_sigmoid=False, alpha=1.0):
+        if gate is not None and gate.dim() != 2:
+            raise ValueError(f"gate must be [1, d] or [T, d], got {tuple(gate.shape)}")
+        self.pre_gain, self.post_gain, self.gate, self.post = pre_gain, post_gain, gate, bool(post)
+        self.struct = NormStruct(float(alpha), float(eps), int(self.post), int(bool(gate_sigmoid)),
+                                 0 if gate is None else gate.shape[0], _dev(gate, "gate"), _dev(post_gain, "post_gain"),
+                                 _dev(pre_gain, "pre_gain"))
+
+    def check(self, x, d, dev):
+        gains = (d,)
+        rows = self.struct.gate_rows
+        if rows not in (0, 1, x.shape[0]):
+            raise ValueError(f"gate has {rows} rows, x has {x.shape[0]}")
+        _check_like(dev, x.dtype, ((self.pre_gain, "pre_gain", gains, True), (self.post_gain, "post_gain", gains, True),
+                                   (self.gate, "gate", (rows, d), True)))
+
+
+def norm(eps, pre_gain=None, post=False, post_gain=None, gate=None, gate_sigmoid=False, alpha=1.0) -> Norm:
+    """The form of ffn_norm_forward: eps of both norms; post: the block's output is normed (times post_gain);
+    gate [1, d] or [T, d], or with gate_sigmoid its logistic function, on it; alpha on the residual; pre_gain of
+    the norm before the next block.  Device tensors of the tokens' dtype, or None."""
+    return Norm(eps, pre_gain, post, post_gain, gate, gate_sigmoid, alpha)
+
+
+def alloc_norm_workspace(T, d, device="cuda"):
+    return _bytes(int(lib().ffn_norm_workspace_bytes(T, d)), "ffn_norm_workspace_bytes", device)
+
+
+def _check_rstd(rstd, T, dev):
+    if rstd is not None and (rstd.dtype is not _torch().float32 or rstd.shape != (2, T) or rstd.get_device() != dev or
+                             not rstd.is_contiguous()):
+        raise ValueError(f"rstd must be a contiguous float32 [2, {T}] tensor on x's device")
+
+
+def ffn_norm_forward(x, f, form, x_out, n_out, rstd=None, stream=None):
+    """x_out = alpha x + gate * post-norm(f) and n_out = pre-norm(x_out), form of ffn.norm(...).  f None: the norm
+    of x alone (x_out None).  rstd: None, or a float32 [2, T] tensor for ffn_norm_backward.  Returns (x_out, n_out)."""
+    T, d, dev, dt = _tokens(x)
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (f, "f", x.shape, True), (x_out, "x_out", x.shape, True),
+                               (n_out, "n_out", x.shape, True)))
+    _check_rstd(rstd, T, dev)
+    form.check(x, d, dev)
+    rc = _function("ffn_norm_forward")(dt, T, d, x.data_ptr(), _p(f), ctypes.byref(form.struct), _p(x_out), _p(n_out),
+                                       _p(rstd), _raw_stream(stream, x))
+    _check("ffn_norm_forward", rc)
+    return x_out, n_out
+
+
+def ffn_norm_backward(x_out, f, form, rstd, dn, dx_out, ws, dx=None, df=None, dgate=None, dpost_gain=None,
+                      dpre_gain=None, stream=None):
+    """Gradients of ffn_norm_forward from dn (of n_out) and dx_out (of x_out), either may be None, written to the
+    tensors given (None: not computed)."""
+    like = next((v for v in (x_out, dx_out, dn) if v is not None), None)
+    if like is None:
+        raise ValueError("x_out, dn or dx_out is required")
+    T, d, dev, dt = _tokens(like)
+    rows, gain = like.shape, (d,)
+    _check_like(dev, like.dtype, ((x_out, "x_out", rows, True), (f, "f", rows, True), (dn, "dn", rows, True),
+                                  (dx_out, "dx_out", rows, True), (dx, "dx", rows, True), (df, "df", rows, True),
+                                  (dgate, "dgate", (form.struct.gate_rows, d), True),
+                                  (dpost_gain, "dpost_gain", gain, True), (dpre_gain, "dpre_gain", gain, True)))
+    _check_rstd(rstd, T, dev)
+    _check_buffers(dev, (ws, "ws"))
+    form.check(like, d, dev)
+    rc = _function("ffn_norm_backward")(dt, T, d, _p(x_out), _p(f), ctypes.byref(form.struct), _p(rstd), _p(dn),
+                                        _p(dx_out), _p(dx), _p(df), _p(dgate), _p(dpost_gain), _p(dpre_gain),
+                                        ws.data_ptr(), _size(ws), _raw_stream(stream, like))
+    _check("ffn_norm_backward", rc)
+    return dx, df, dgate, dpost_gain, dpre_gain
 
 
 def ffn_status_string(code: int) -> str:

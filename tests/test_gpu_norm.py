@@ -1,0 +1,234 @@
+"""The norms before and after a block on the GPU against 64 bits (bounds: norm_ref)."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_31975_amd import ffn
+from tests import norm_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+KINDS = {"plain": dict(), "post": dict(post=True, gains=True), "row": dict(post=True, gains=True, gate="row", alpha=0.5),
+         "token": dict(post=True, gains=True, gate="token", sigmoid=True), "no_post": dict(gate="token", pre=True, gains=True),
+         "no_gains": dict(post=True, gate="row", sigmoid=True), "no_pre": dict(post=True, gains=True, pre=False, gate="row")}
+
+
+def chain(T, d):
+    """The longest chain of additions over the tokens: rows a group takes, groups a thread joins, 16 threads."""
+    groups = min(T + 3, 2048 if d <= 1024 else 1024 if d <= 4096 else 512)
+    return -(-T // max(1, groups - 3)) + 1 + -(-groups // 16) + 16
+
+
+class Layer:
+    def __init__(self, dtype, T, d, post=False, gains=False, gate=None, sigmoid=False, alpha=1.0, pre=True, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed * 1000 + T + 7 * d)
+        rnd = lambda shape, std=1.0, mid=0.0: (torch.randn(shape, generator=gen, device="cuda") * std + mid).to(dtype)
+        self.dtype, self.T, self.d, self.pre = dtype, T, d, pre
+        self.x, self.f = rnd((T, d), 2.0), rnd((T, d), 0.7)
+        self.gate = None if gate is None else rnd((1 if gate == "row" else T, d))
+        self.post_gain = rnd((d,), 0.2, 1.0) if gains and post else None
+        self.pre_gain = rnd((d,), 0.2, 1.0) if gains and pre else None
+        self.dn, self.dxo = rnd((T, d)) if pre else None, rnd((T, d))
+        self.form = ffn.norm(1e-5, self.pre_gain, post, self.post_gain, self.gate, sigmoid, alpha)
+        self.ref = ref.Form(1e-5, self.pre_gain, post, self.post_gain, self.gate, sigmoid, alpha)
+
+    def run(self, stream=None, ws=None, dn="", dxo=""):
+        nan = lambda v: torch.full_like(v, math.nan)
+        dn, dxo = self.dn if dn == "" else dn, self.dxo if dxo == "" else dxo
+        o = {"x_out": nan(self.x), "n_out": nan(self.x) if self.pre else None,
+             "rstd": torch.full((2, self.T), math.nan, dtype=F32, device="cuda")}
+        ffn.ffn_norm_forward(self.x, self.f, self.form, o["x_out"], o["n_out"], o["rstd"], stream)
+        g = {"dx": nan(self.x), "df": nan(self.x)}
+        for name, like, on in (("dgate", self.gate, True), ("dpost_gain", self.x[0], self.form.post),
+                               ("dpre_gain", self.x[0], dn is not None)):
+            if like is not None and on:
+                g[name] = nan(like)
+        ws = torch.full_like(ffn.alloc_norm_workspace(self.T, self.d), 0xFF) if ws is None else ws
+        ffn.ffn_norm_backward(o["x_out"], self.f, self.form, o["rstd"], dn, dxo, ws, **g, stream=stream)
+        return dict(o, **g)
+
+    def check(self, o, dn="", dxo="", what=""):
+        dn, dxo = self.dn if dn == "" else dn, self.dxo if dxo == "" else dxo
+        want = ref.forward(self.x, self.f, self.ref)
+        ref.check(o["x_out"], want["x_out"], want["e_x_out"], self.dtype, what + " x_out")
+        if self.pre:
+            ref.check(o["n_out"], want["n_out"], want["e_n_out"], self.dtype, what + " n_out")
+            ref.check(o["rstd"][1, :, None], want["r"], want["e_r"], F32, what + " r")
+        rf = torch.ones_like(want["rf"])
+        if self.form.post:
+            rf = o["rstd"][0].double()[:, None]
+            ref.check(o["rstd"][0, :, None], want["rf"], want["e_rf"], F32, what + " rf")
+        grads, err = ref.backward(o["x_out"], self.f, self.ref, rf, o["rstd"][1].double()[:, None], dn, dxo,
+                                  chain(self.T, self.d))
+        for name in grads:
+            if name in o:
+                ref.check(o[name], grads[name], err[name], self.dtype, f"{what} {name}")
+
+
+# rows of one element, of a wave, behind each border of threads and elements a row, of narrow loads
+SIZES = [(1, 1), (3, 8), (5, 7), (64, 512), (9, 520), (2, 1024), (3, 1025), (7, 2048), (2, 2056), (4, 4096), (3, 4100), (2, 8192),
+         (3, 8200), (2, 9999), (2, 16384), (1, 16383), (777, 264), (2050, 24), (1030, 1032)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,d", SIZES)
+def test_sizes(dtype, T, d):
+    layer = Layer(dtype, T, d, **KINDS["token"])
+    layer.check(layer.run(), what=f"T={T} d={d}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("T,d", [(1, 96), (37, 1000), (11, 2500), (5, 6001)])
+def test_forms(dtype, kind, T, d):
+    layer = Layer(dtype, T, d, **KINDS[kind])
+    layer.check(layer.run(), what=kind)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradients_of_one_side(dtype):
+    """x' without a gradient of its own, and n without one; a part of the gradients alone gives the same bits."""
+    layer = Layer(dtype, 33, 1536, **KINDS["row"])
+    layer.check(layer.run(dxo=None), dxo=None, what="dn alone")
+    layer.check(layer.run(dn=None), dn=None, what="dx_out alone")
+    o = layer.run()
+    ws = ffn.alloc_norm_workspace(33, 1536)
+    for names in (("dx",), ("df",), ("dgate",), ("dpost_gain",), ("dpre_gain",), ("dgate", "dpre_gain")):
+        g = {n: torch.full_like(o[n], math.nan) for n in names}
+        ffn.ffn_norm_backward(o["x_out"], layer.f, layer.form, o["rstd"], layer.dn, layer.dxo, ws, **g)
+        for n in names:
+            assert torch.equal(g[n], o[n]), n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [40, 1001, 5000])
+def test_norm_alone(dtype, d):
+    """Before a first block: no block's output."""
+    T = 6
+    layer = Layer(dtype, T, d, gains=True)
+    n, rstd = torch.empty_like(layer.x), torch.empty((2, T), dtype=F32, device="cuda")
+    ffn.ffn_norm_forward(layer.x, None, layer.form, None, n, rstd)
+    want = ref.forward(layer.x, None, layer.ref)
+    ref.check(n, want["n_out"], want["e_n_out"], dtype)
+    dx, dg = torch.empty_like(n), torch.empty_like(n[0])
+    ffn.ffn_norm_backward(layer.x, None, layer.form, rstd, layer.dn, None, ffn.alloc_norm_workspace(T, d), dx=dx, dpre_gain=dg)
+    grads, err = ref.backward(layer.x, None, layer.ref, None, rstd[1].double()[:, None], layer.dn, None, chain(T, d))
+    ref.check(dx, grads["dx"], err["dx"], dtype)
+    ref.check(dg, grads["dpre_gain"], err["dpre_gain"], dtype)
+
+
+def test_whole_gradient_f32():
+    """Forward and backward together against torch's differentiation in 64 bits: x' is rounded once in between
+    (2^-24 of each value, which the backward bounds' FACTOR of the same values covers many times)."""
+    layer = Layer(F32, 50, 777, **KINDS["token"])
+    o = layer.run()
+    v = {n: getattr(layer, n).double().requires_grad_() for n in ("x", "f", "gate", "post_gain", "pre_gain")}
+    rms = lambda u: u / torch.sqrt((u * u).mean(1, keepdim=True) + layer.ref.eps)
+    xo = v["x"] + torch.sigmoid(v["gate"]) * rms(v["f"]) * v["post_gain"]
+    ((rms(xo) * v["pre_gain"] * layer.dn.double()).sum() + (xo * layer.dxo.double()).sum()).backward()
+    want = ref.forward(layer.x, layer.f, layer.ref)
+    _, err = ref.backward(want["x_out"], layer.f, layer.ref, want["rf"], want["r"], layer.dn, layer.dxo, chain(50, 777))
+    for name, value in v.items():
+        # r, rf (24 U + FACTOR kappa each, kappa below 2) and x' enter linearly: another 4 FACTOR of the terms' sizes, at most
+        # the errors above times 4
+        ref.check(o["d" + name], value.grad, 4 * err["d" + name] + 4 * ref.FACTOR * value.grad.abs().mean(), F32, name)
+
+
+def test_in_place():
+    layer = Layer(BF16, 40, 1536, **KINDS["token"])
+    want = layer.run()
+    x, dxo = layer.x.clone(), layer.dxo.clone()
+    n, rstd = torch.empty_like(x), torch.empty((2, 40), dtype=F32, device="cuda")
+    ffn.ffn_norm_forward(x, layer.f, layer.form, x, n, rstd)
+    assert torch.equal(x, want["x_out"]) and torch.equal(n, want["n_out"])
+    ffn.ffn_norm_backward(x, layer.f, layer.form, rstd, layer.dn, dxo, ffn.alloc_norm_workspace(40, 1536), dx=dxo)
+    assert torch.equal(dxo, want["dx"])
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("where", ["x", "f", "gate"])
+def test_special_values_stay_in_their_token(bad, where):
+    layer = Layer(BF16, 13, 1000, **KINDS["token"])
+    clean = layer.run()
+    getattr(layer, where)[4, 17] = bad
+    if where == "gate":
+        layer.gate[4, 17] = math.nan if bad == bad else bad  # sigma(+-Inf) is finite
+    got = layer.run()
+    keep = torch.arange(13, device="cuda") != 4
+    for name in ("x_out", "n_out", "dx", "df", "dgate"):
+        assert torch.equal(got[name][keep], clean[name][keep]), name
+    assert not bool(torch.isfinite(got["x_out"][4]).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_zero_and_large_rows(dtype):
+    """A row of zeros norms to zeros; values whose squares are near fp32's largest still norm."""
+    layer = Layer(dtype, 4, 512, post=True, gains=True)
+    layer.x[0], layer.f[0] = 0, 0
+    layer.x[1] *= 1e15
+    layer.f[2] *= 1e15
+    o = layer.run()
+    assert not bool(o["n_out"][0].any()) and not bool(o["x_out"][0].any())
+    layer.check(o)
+
+
+def test_repeats_are_equal():
+    layer = Layer(BF16, 3000, 520, **KINDS["row"])
+    a, b = layer.run(), layer.run()
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+def test_other_stream_and_graphs():
+    """On a side stream; captured and replayed on new inputs with eager work in between, two graphs with one
+    workspace replayed in turn."""
+    layer, other = Layer(BF16, 60, 1032, **KINDS["row"]), Layer(BF16, 60, 1032, **KINDS["row"], seed=3)
+    side = torch.cuda.Stream()
+    want = [layer.run(), other.run()]
+    side.wait_stream(torch.cuda.current_stream())
+    o = layer.run(stream=side)
+    side.synchronize()
+    assert all(torch.equal(o[n], want[0][n]) for n in o)
+    ws = ffn.alloc_norm_workspace(60, 1032)
+    outs, graphs = [], []
+    with torch.cuda.stream(side):  # warm the allocator
+        layer.run(ws=ws), other.run(ws=ws)
+    torch.cuda.synchronize()
+    for one in (layer, other):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(one.run(ws=ws))
+        graphs.append(g)
+    keep = layer.x.clone()
+    for turn in range(4):
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert all(torch.equal(outs[i][n], want[i][n]) for n in want[i]), (turn, i)
+        layer.x.copy_(other.x)
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        changed = layer.run()
+        assert all(torch.equal(outs[0][n], changed[n]) for n in changed)
+        layer.x.copy_(keep)
+
+
+def test_binding_refusals():
+    layer = Layer(BF16, 6, 64, **KINDS["token"])
+    x, n = torch.empty_like(layer.x), torch.empty_like(layer.x)
+
+    def call(x0=layer.x, f=layer.f, form=layer.form, x_out=x, n_out=n, rstd=None):
+        ffn.ffn_norm_forward(x0, f, form, x_out, n_out, rstd)
+
+    call()
+    short = ffn.norm(1e-5, gate=layer.gate[:5])
+    for bad in (dict(x0=layer.x.float()), dict(f=layer.f[:3]), dict(x_out=x.float()), dict(n_out=n.t()), dict(x0=layer.x[0]),
+                dict(rstd=torch.empty(6, device="cuda")), dict(form=short), dict(x0=layer.x.cpu()),
+                dict(form=ffn.norm(1e-5, pre_gain=torch.ones(64, device="cuda")))):
+        with pytest.raises((ValueError, TypeError)):
+            call(**bad)
+    with pytest.raises(ffn.FFNError) as e:
+        call(form=ffn.norm(-1.0))
+    assert e.value.code == -7
