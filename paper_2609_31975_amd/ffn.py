@@ -15,7 +15,8 @@ import re
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libffn_sparse.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "ffn_sparse.h")
-HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h", "ffn_norm.h")]
+HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h", "ffn_norm.h",
+                                                                      "ffn_group_q.h")]
 
 FFN_F32 = 0
 FFN_BF16 = 1
@@ -54,6 +55,12 @@ class NormStruct(ctypes.Structure):
     _fields_ = [("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("post", ctypes.c_int),
                 ("gate_sigmoid", ctypes.c_int), ("gate_rows", ctypes.c_int), ("gate", ctypes.c_void_p),
                 ("post_gain", ctypes.c_void_p), ("pre_gain", ctypes.c_void_p)]
+
+
+class GroupQStruct(ctypes.Structure):
+    """``ffn_group_q_t``: a matrix of 4-bit codes with group scales (device pointers)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
+                ("sdt", ctypes.c_int), ("group", ctypes.c_int)]
 
 
 class FFNError(RuntimeError):
@@ -122,6 +129,13 @@ def lib() -> ctypes.CDLL:
                 ("ffn_norm_forward", i, [i, i, i, vp, vp, np_, vp, vp, vp, vp]),
                 ("ffn_norm_workspace_bytes", sz, [i, i]),
                 ("ffn_norm_backward", i, [i, i, i, vp, vp, np_] + [vp] * 9 + [sz, vp])):
+            getattr(L, name).restype = res
+            getattr(L, name).argtypes = args
+        gp = ctypes.POINTER(GroupQStruct)
+        for name, res, args in (
+                ("ffn_group_q_workspace_bytes", sz, [i, i, i, i]),
+                ("ffn_group_q_forward", i, [i, i, i, i, vp, gp, vp, vp, sz, vp]),
+                ("ffn_group_q_gated_forward", i, [i, i, i, i, vp, gp, gp, f, op, vp, vp, sz, vp])):
             getattr(L, name).restype = res
             getattr(L, name).argtypes = args
         L.ffn_status_string.restype = ctypes.c_char_p
@@ -728,6 +742,70 @@ def ffn_norm_backward(x_out, f, form, rstd, dn, dx_out, ws, dx=None, df=None, dg
                                         ws.data_ptr(), _size(ws), _raw_stream(stream, like))
     _check("ffn_norm_backward", rc)
     return dx, df, dgate, dpost_gain, dpre_gain
+
+
+# ---------------------------------------------------------------- 4-bit weights with group scales
+class GroupQ:
+    """A matrix of 4-bit codes with group scales: the ``ffn_group_q_t`` and the tensors it points into."""
+
+    def __init__(self, codes, scales, offsets=None):
+        torch = _torch()
+        if codes.dim() != 2 or codes.dtype != torch.uint8:
+            raise ValueError(f"codes must be uint8 [n_out, n_in / 2], got {codes.dtype} {tuple(codes.shape)}")
+        self.n_out, self.n_in = codes.shape[0], 2 * codes.shape[1]
+        if scales.dim() != 2 or scales.shape[0] != self.n_out or scales.shape[1] < 1 or self.n_in % scales.shape[1]:
+            raise ValueError(f"scales must be [{self.n_out}, n_in / group], got {tuple(scales.shape)}")
+        self.codes, self.scales, self.offsets = codes, scales, offsets
+        sdt = _type_of(scales.dtype)
+        if offsets is not None and (offsets.dtype != scales.dtype or offsets.shape != scales.shape):
+            raise ValueError(f"offsets must be {scales.dtype} {list(scales.shape)}, got {offsets.dtype} {list(offsets.shape)}")
+        ptrs = [_dev(codes, "codes"), _dev(scales, "scales"), _dev(offsets, "offsets")]
+        if scales.device != codes.device or (offsets is not None and offsets.device != codes.device):
+            raise ValueError("codes, scales and offsets must be on one device")
+        self.struct = GroupQStruct(*ptrs, sdt, self.n_in // scales.shape[1])
+
+
+def group_q(codes, scales, offsets=None) -> GroupQ:
+    """A matrix W = scale code + offset: codes uint8 [n_out, n_in / 2] (two's-complement nibbles, the even element
+    low), scales and offsets (None: zero) float32 or bfloat16 [n_out, n_in / group], a scale for every `group` (a
+    multiple of 32) inputs.  Device tensors."""
+    return GroupQ(codes, scales, offsets)
+
+
+def alloc_group_q_workspace(T, n_in, n_out, gated=False, device="cuda"):
+    return _bytes(int(lib().ffn_group_q_workspace_bytes(T, n_in, n_out, int(bool(gated)))), "ffn_group_q_workspace_bytes",
+                  device)
+
+
+def _group_q_args(x, mats, y):
+    T, n_in, dev, dt = _tokens(x)
+    n_out = mats[0].n_out
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (y, "y", (T, n_out), False)))
+    for w in mats:
+        if (w.n_out, w.n_in) != (n_out, n_in) or w.codes.get_device() != dev:
+            raise ValueError(f"the weights are [{w.n_out}, {w.n_in}] on {w.codes.device}, x is {list(x.shape)} on {x.device}")
+    return dt, T, n_in, n_out
+
+
+def ffn_group_q_forward(x, w, y, ws, stream=None):
+    """y = x W^T of bfloat16 or float32 tokens and 4-bit weights of ffn.group_q(...)."""
+    args = _group_q_args(x, (w,), y)
+    _check_buffers(x.get_device(), (ws, "ws"))
+    rc = _function("ffn_group_q_forward")(*args, x.data_ptr(), ctypes.byref(w.struct), y.data_ptr(), ws.data_ptr(),
+                                          _size(ws), _raw_stream(stream, x))
+    _check("ffn_group_q_forward", rc)
+    return y
+
+
+def ffn_group_q_gated_forward(x, w_gate, w_up, t, opt, z, ws, stream=None):
+    """z = A(x W1^T - t) U(x W3^T): the hidden layer of the gated block with 4-bit weights."""
+    args = _group_q_args(x, (w_gate, w_up), z)
+    _check_buffers(x.get_device(), (ws, "ws"))
+    rc = _function("ffn_group_q_gated_forward")(*args, x.data_ptr(), ctypes.byref(w_gate.struct), ctypes.byref(w_up.struct),
+                                                ctypes.c_float(t), _opt(opt), z.data_ptr(), ws.data_ptr(), _size(ws),
+                                                _raw_stream(stream, x))
+    _check("ffn_group_q_gated_forward", rc)
+    return z
 
 
 def ffn_status_string(code: int) -> str:
