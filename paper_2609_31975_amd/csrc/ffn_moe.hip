@@ -1,0 +1,563 @@
+// include/ffn_moe.h: a mixture-of-experts layer for a decode step's tokens.
+//
+// The chosen experts' three matrices are read once (for up to 64 tokens of an expert) and bound it.  Launches:
+//   1. k_moe_route   logits in 64 bits, a wave to an expert; the last workgroup of 8 tokens chooses for them
+//   2. k_moe_hidden  z = A(x W1^T - t) U(x W3^T), 16 hidden neurons of an expert to a workgroup
+//   3. k_moe_down    z W2 in pieces of neurons, 16-byte columns x 16 lanes of an expert to a workgroup
+//   4. k_moe_join    the pieces and the experts, weighted, in a fixed order
+// The matrix products have tokens as the A operand and weights as the B operand, so that one token costs
+// what 16 do; the weights go from memory to registers and enter as they lie (W1, W3: rows along the summed
+// dimension) or after an exchange of half-words in the lane (W2's rows are neurons: 8 of them, 8 columns each).
+#include <math.h>
+
+#include <algorithm>
+
+#include "ffn_mfma.h"
+#include "ffn_moe.h"
+#include "ffn_step_device.h"
+
+namespace ffn {
+namespace {
+
+constexpr int kMoeTokens = 256, kMoeK = 16, kMoeExperts = 512;
+constexpr int kRouteTokens = 8;  // tokens that choose together
+constexpr int kMoeCounters = kMoeTokens / kRouteTokens;
+
+struct RouteArgs {
+  int T, d, E, k;
+  const void *x, *w;
+  const float* bias;
+  int sigmoid, normalize;
+  float scale;
+  double* logits;  // [T][E]
+  int* arrived;    // one for each kRouteTokens; zero between calls
+  int32_t* ids;
+  float* weights;
+};
+
+struct MoeArgs {
+  int T, d, d_ff, E, k, ldz;
+  int slots;   // T k places (each place's first use of its expert works), or the experts
+  int pieces;  // of the neurons, in k_moe_down
+  const void *x, *w[3];
+  ActForm form;
+  const int32_t* ids;
+  const float* weights;
+  void* z;      // [T k][ldz]
+  float* part;  // [pieces][T k][d]
+  void* y;
+};
+
+// A 16-byte chunk's worth of elements from element i on, `left` of them there: one load, or narrower ones.
+template <bool F32, bool VEC>
+__device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
+  if constexpr (VEC) {
+    return ldb(b, left > 0 ? i * (F32 ? 4u : 2u) : kOOB);
+  } else if constexpr (F32) {
+    return make_uint4(ldb32(b, left > 0 ? i * 4 : kOOB), ldb32(b, left > 1 ? i * 4 + 4 : kOOB),
+                      ldb32(b, left > 2 ? i * 4 + 8 : kOOB), ldb32(b, left > 3 ? i * 4 + 12 : kOOB));
+  } else {
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, left > j ? i * 2 + j * 2 : kOOB, 0, 0);
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+  }
+}
+template <bool F32, bool VEC>
+__device__ __forceinline__ uint4 ld_weight_chunk(const Buf& b, uint32_t i, int left) {
+  if constexpr (VEC) return ldb_nt(b, left > 0 ? i * (F32 ? 4u : 2u) : kOOB);
+  else return ld_chunk<F32, VEC>(b, i, left);
+}
+
+// ------------------------------------------------------------------ the router
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int s = 1; s < kWave; s *= 2) v += __shfl_xor(v, s);
+  return v;
+}
+
+// The choice of one token, by one wave.  A lane has the scores of experts lane, 64 + lane, ...
+__device__ __forceinline__ void choose(const RouteArgs& a, int tok) {
+  constexpr int N = kMoeExperts / kWave;
+  const int lane = lane_id();
+  double l[N], key[N];
+  double top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * kWave + lane;
+    l[i] = e < a.E ? a.logits[(size_t)tok * a.E + e] : -INFINITY;
+    top = l[i] > top ? l[i] : top;
+  }
+  double total = 0.0;
+  if (!a.sigmoid) {
+#pragma unroll
+    for (int s = 1; s < kWave; s *= 2) {
+      const double o = __shfl_xor(top, s);
+      top = o > top ? o : top;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i * kWave < a.E) total += i * kWave + lane < a.E ? exp(l[i] - top) : 0.0;
+    total = wave_sum64(total);
+  }
+  auto score = [&](double v) { return a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - top) / total; };
+  uint32_t open = 0;  // experts of this lane that are not chosen yet
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int e = i * kWave + lane;
+    key[i] = l[i];
+    if (e < a.E) {
+      if (a.bias) key[i] = score(l[i]) + (double)a.bias[e];
+      key[i] = key[i] == key[i] ? key[i] : -INFINITY;
+      open |= 1u << i;
+    }
+  }
+  double sum = 0.0, mine = 0.0;
+  int mine_e = 0;
+  for (int j = 0; j < a.k; ++j) {
+    double best = -INFINITY, bl = 0.0;
+    int be = 1 << 30;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool better = (open >> i & 1) && (key[i] > best || be == 1 << 30);
+      best = better ? key[i] : best;
+      bl = better ? l[i] : bl;
+      be = better ? i * kWave + lane : be;
+    }
+#pragma unroll
+    for (int s = 1; s < kWave; s *= 2) {
+      const double ob = __shfl_xor(best, s), ol = __shfl_xor(bl, s);
+      const int oe = __shfl_xor(be, s);
+      const bool take = ob > best || (ob == best && oe < be);
+      best = take ? ob : best;
+      bl = take ? ol : bl;
+      be = take ? oe : be;
+    }
+    if ((be & (kWave - 1)) == lane) open &= ~(1u << (be >> 6));
+    const double s = score(bl);
+    sum += s;
+    if (lane == j) {
+      mine = s;
+      mine_e = be;
+    }
+  }
+  if (lane < a.k) {
+    a.ids[(size_t)tok * a.k + lane] = mine_e;
+    a.weights[(size_t)tok * a.k + lane] = (float)((double)a.scale * (a.normalize ? mine / sum : mine));
+  }
+}
+
+// A wave takes one expert's logits of NT tokens.
+template <bool F32, bool VEC, int NT>
+__global__ __launch_bounds__(256) void k_moe_route(RouteArgs a) {
+  constexpr int E = F32 ? 4 : 8;
+  __shared__ int s_last;
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), e = blockIdx.x * 4 + wave, t0 = blockIdx.y * kRouteTokens;
+  const int nt = min(a.T - t0, NT);
+  if (e < a.E) {
+    const size_t es = F32 ? 4 : 2;
+    const Buf wb = make_buf(static_cast<const char*>(a.w) + (size_t)e * a.d * es, a.d * (uint32_t)es);
+    const Buf xb = make_buf(static_cast<const char*>(a.x) + (size_t)t0 * a.d * es, nt * a.d * (uint32_t)es);
+    double s[NT] = {};
+    for (int k = lane * E; k < a.d; k += kWave * E) {
+      float w[E], x[E];
+      const uint4 wv = ld_chunk<F32, VEC>(wb, k, a.d - k);
+      uint4 xv[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xv[t] = ld_chunk<F32, VEC>(xb, t * a.d + k, t < nt ? a.d - k : 0);
+      if constexpr (F32) unpack(WF32{}, wv, w);
+      else unpack(WBf16{}, wv, w);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if constexpr (F32) unpack(WF32{}, xv[t], x);
+        else unpack(WBf16{}, xv[t], x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) s[t] = fma((double)w[j], (double)x[j], s[t]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const double v = wave_sum64(s[t]);
+      if (lane == 0 && t < nt) a.logits[(size_t)(t0 + t) * a.E + e] = v;
+    }
+  }
+  // The last workgroup of these tokens has all their logits before it; it leaves the counter at zero.
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s_last = atomicAdd(&a.arrived[blockIdx.y], 1) == (int)gridDim.x - 1;
+    if (s_last) a.arrived[blockIdx.y] = 0;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  for (int t = t0 + wave; t < min(a.T, t0 + kRouteTokens); t += 4) choose(a, t);
+}
+
+// ------------------------------------------------------------------ the experts
+// The expert of a slot, or -1.  With a slot a place, a place whose expert an earlier one names has no work.
+__device__ __forceinline__ int slot_expert(const MoeArgs& a, int slot) {
+  if (a.slots == a.E && a.slots != a.T * a.k) return slot;
+  const int e = uniform(a.ids[slot]);
+  if (e < 0 || e >= a.E) return -1;
+  for (int b = 0; b < slot; b += kWave) {
+    const int at = b + lane_id();
+    if (__ballot(at < slot && a.ids[at] == e)) return -1;
+  }
+  return e;
+}
+// The places of expert e, in order, into list; every wave calls it and gets their number.
+__device__ __forceinline__ int list_places(const MoeArgs& a, int e, uint16_t* list, int* count) {
+  if (threadIdx.x < kWave) {
+    const int n = a.T * a.k;
+    int have = 0;
+    for (int b = 0; b < n; b += 8 * kWave) {
+      int id[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int at = b + j * kWave + lane_id();
+        id[j] = at < n ? a.ids[at] : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint64_t m = __ballot(id[j] == e);
+        if (id[j] == e) list[have + rank_in_mask(m)] = (uint16_t)(b + j * kWave + lane_id());
+        have += __popcll(m);
+      }
+    }
+    if (lane_id() == 0) *count = have;
+  }
+  __syncthreads();
+  return uniform(*count);
+}
+
+// Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.
+template <bool F32, bool VEC, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) {
+  constexpr int E = F32 ? 4 : 8, U = 4, STEP = 4 * E * U;  // elements of a row that a wave takes at once
+  __shared__ uint16_t list[kMoeTokens * kMoeK];
+  __shared__ float red[4][2][4][kWave];
+  __shared__ int count;
+  const int e = slot_expert(a, blockIdx.y);
+  if (e < 0) return;
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int row0 = blockIdx.x * 16, rows = min(16, a.d_ff - row0);
+  const size_t es = F32 ? 4 : 2;
+  Buf wb[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+    wb[m] = make_buf(static_cast<const char*>(a.w[m]) + ((size_t)e * a.d_ff + (rows > 0 ? row0 : 0)) * a.d * es,
+                     rows > 0 ? (uint32_t)rows * a.d * es : 0u);
+  const Buf xb = make_buf(a.x, (uint32_t)a.T * a.d * es);
+
+  struct Batch {
+    uint4 w[U][2];
+  };
+  auto load = [&](int k0, Batch& b) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + (u * 4 + g) * E, left = n < rows ? a.d - k : 0;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) b.w[u][m] = ld_weight_chunk<F32, VEC>(wb[m], (uint32_t)n * a.d + k, left);
+    }
+  };
+  Batch first;
+  load(wave * STEP, first);
+  const int cnt = list_places(a, e, list, &count);
+
+  for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
+    uint32_t xo[NT];  // a token's row: tokens past the last one repeat it, and are not stored
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xo[t] = (uint32_t)(list[min(p0 + t * 16 + n, cnt - 1)] / a.k) * a.d;
+    const int tiles = min(NT, (cnt - p0 + 15) / 16);
+    f32x4_t acc[NT][2] = {};
+    Batch cur = first;
+    if (p0) load(wave * STEP, cur);
+    for (int k0 = wave * STEP; k0 < a.d; k0 += 4 * STEP) {
+      Batch nxt;
+      load(k0 + 4 * STEP, nxt);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (t >= tiles) break;
+        uint4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int k = k0 + (u * 4 + g) * E;
+          x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, a.d - k);
+        }
+        f32x4_t s[2] = {};
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            if constexpr (F32) {
+              s[m] = mfma16f(comp<0>(x[u]), comp<0>(cur.w[u][m]), s[m]);
+              s[m] = mfma16f(comp<1>(x[u]), comp<1>(cur.w[u][m]), s[m]);
+              s[m] = mfma16f(comp<2>(x[u]), comp<2>(cur.w[u][m]), s[m]);
+              s[m] = mfma16f(comp<3>(x[u]), comp<3>(cur.w[u][m]), s[m]);
+            } else {
+              s[m] = mfma16(bf8(x[u]), bf8(cur.w[u][m]), s[m]);
+            }
+          }
+        acc[t][0] += s[0];
+        acc[t][1] += s[1];
+      }
+      cur = nxt;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (t >= tiles) break;
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[wave][m][i][lane] = acc[t][m][i];
+      __syncthreads();
+      const int p = p0 + t * 16 + g * 4 + wave, row = row0 + n;  // thread (wave, lane): result register `wave` of `lane`
+      if (p < cnt) {
+        float h = 0.f, v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          h += red[w][0][wave][lane];
+          v += red[w][1][wave][lane];
+        }
+        // rows up to ldz are zeros for the next product
+        store_as<F32>(a.z, (size_t)list[p] * a.ldz + row, row < a.d_ff ? act_product(a.form, h, v) : 0.f);
+      }
+    }
+  }
+}
+
+// Columns of a workgroup: 16 lanes of 16 bytes.
+template <bool F32>
+constexpr int down_columns() {
+  return F32 ? 64 : 128;
+}
+
+// Four waves take turns at the piece's neurons, 32 at once: a lane has 16 bytes of 8 neurons' rows.
+template <bool F32, bool VEC, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
+  constexpr int E = F32 ? 4 : 8, COLS = down_columns<F32>();
+  __shared__ uint16_t list[kMoeTokens * kMoeK];
+  __shared__ float red[4][E][4][kWave];
+  __shared__ int count;
+  const int e = slot_expert(a, blockIdx.y);
+  if (e < 0) return;
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int col = blockIdx.x * COLS + n * E;
+  // the piece's neurons: whole steps of 32
+  const int steps = a.ldz / 32, s0 = (int)((int64_t)steps * blockIdx.z / a.pieces), s1 = (int)((int64_t)steps * (blockIdx.z + 1) / a.pieces);
+  const size_t es = F32 ? 4 : 2;
+  const Buf zb = make_buf(a.z, (uint32_t)a.T * a.k * a.ldz * es);
+  const char* wbase = static_cast<const char*>(a.w[2]) + (size_t)e * a.d_ff * a.d * es;
+
+  struct Batch {
+    uint4 w[8];
+  };
+  auto load = [&](int s, Batch& b) {
+    const int r0 = min(s, s1 - 1) * 32, rows = s < s1 ? min(32, a.d_ff - r0) : 0;
+    const Buf wb = make_buf(wbase + (size_t)r0 * a.d * es, rows > 0 ? (uint32_t)rows * a.d * es : 0u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      b.w[j] = ld_weight_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
+  };
+  Batch first;
+  load(s0 + wave, first);
+  const int cnt = list_places(a, e, list, &count);
+
+  for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
+    uint32_t zo[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) zo[t] = (uint32_t)list[min(p0 + t * 16 + n, cnt - 1)] * a.ldz;
+    const int tiles = min(NT, (cnt - p0 + 15) / 16);
+    f32x4_t acc[NT][E] = {};
+    Batch cur = first;
+    if (p0) load(s0 + wave, cur);
+    for (int s = s0 + wave; s < s1; s += 4) {
+      Batch nxt;
+      load(s + 4, nxt);
+      uint4 b[E];
+      if constexpr (!F32) {
+        // column 2q (and 2q + 1) of neurons 2p, 2p + 1: the low (high) halves of dword q of both rows
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t lo[4], hi[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const uint4 &r0 = cur.w[2 * p], &r1 = cur.w[2 * p + 1];
+            const uint32_t d0 = q == 0 ? r0.x : q == 1 ? r0.y : q == 2 ? r0.z : r0.w;
+            const uint32_t d1 = q == 0 ? r1.x : q == 1 ? r1.y : q == 2 ? r1.z : r1.w;
+            lo[p] = __builtin_amdgcn_perm(d1, d0, 0x05040100u);
+            hi[p] = __builtin_amdgcn_perm(d1, d0, 0x07060302u);
+          }
+          b[2 * q] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          b[2 * q + 1] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (t >= tiles) break;
+        const uint32_t zi = (zo[t] + s * 32 + g * 8) * (uint32_t)es;
+        const uint4 z0 = ldb(zb, zi);
+        if constexpr (F32) {
+          const uint4 z1 = ldb(zb, zi + 16);
+          const float z[8] = {comp<0>(z0), comp<1>(z0), comp<2>(z0), comp<3>(z0), comp<0>(z1), comp<1>(z1), comp<2>(z1), comp<3>(z1)};
+          f32x4_t sum[E] = {};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            sum[0] = mfma16f(z[j], comp<0>(cur.w[j]), sum[0]);
+            sum[1] = mfma16f(z[j], comp<1>(cur.w[j]), sum[1]);
+            sum[2] = mfma16f(z[j], comp<2>(cur.w[j]), sum[2]);
+            sum[3] = mfma16f(z[j], comp<3>(cur.w[j]), sum[3]);
+          }
+#pragma unroll
+          for (int c = 0; c < E; ++c) acc[t][c] += sum[c];
+        } else {
+#pragma unroll
+          for (int c = 0; c < E; ++c) acc[t][c] = mfma16(bf8(z0), bf8(b[c]), acc[t][c]);
+        }
+      }
+      cur = nxt;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (t >= tiles) break;
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < E; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[wave][c][i][lane] = acc[t][c][i];
+      __syncthreads();
+      // E 16 columns and 16 places; neighbouring threads have neighbouring columns
+      for (int o = threadIdx.x; o < COLS * 16; o += 256) {
+        const int c = o % E, l16 = o / E % 16, tok = o / COLS, p = p0 + t * 16 + tok, at = blockIdx.x * COLS + o % COLS;
+        if (p >= cnt || at >= a.d) continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v += red[w][c][tok & 3][(tok >> 2) * 16 + l16];
+        a.part[((size_t)blockIdx.z * a.T * a.k + list[p]) * a.d + at] = v;
+      }
+    }
+  }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_moe_join(MoeArgs a) {
+  const int t = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= a.d) return;
+  float y = 0.f;
+  for (int j = 0; j < a.k; ++j) {
+    const int p = t * a.k + j, e = a.ids[p];
+    if (e < 0 || e >= a.E) continue;
+    float v = 0.f;
+    for (int s = 0; s < a.pieces; ++s) v += a.part[((size_t)s * a.T * a.k + p) * a.d + c];
+    y += a.weights[p] * v;
+  }
+  store_as<F32>(a.y, (size_t)t * a.d + c, y);
+}
+
+// ------------------------------------------------------------------ host side
+constexpr int kPiecesMost = 8;
+
+int moe_slots(int T, int E, int k) { return std::min(T * k, E); }
+int moe_ldz(int d_ff) { return ceil_div(d_ff, 32) * 32; }
+// Pieces of the neurons: enough workgroups for the card, each with a step of 32 for every wave.
+int moe_pieces(bool f32, int T, int d, int d_ff, int E, int k) {
+  const int64_t blocks = (int64_t)moe_slots(T, E, k) * ceil_div(d, f32 ? 64 : 128);
+  const int64_t want = std::min<int64_t>(ceil_div<int64_t>(1024, blocks), moe_ldz(d_ff) / 128);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, kPiecesMost));
+}
+
+struct MoeWs {
+  int* arrived;
+  double* logits;
+  void* z;
+  float* part;
+};
+// The counters come first, wherever a call's other regions lie.
+size_t moe_layout(bool f32, int T, int d, int d_ff, int E, int k, void* base, MoeWs* out) {
+  Carver c{static_cast<char*>(base)};
+  MoeWs w;
+  w.arrived = static_cast<int*>(c.take(sizeof(int) * kMoeCounters));
+  w.logits = static_cast<double*>(c.take(sizeof(double) * T * E));
+  w.z = c.take((size_t)(f32 ? 4 : 2) * T * k * moe_ldz(d_ff));
+  w.part = static_cast<float*>(c.take(sizeof(float) * kPiecesMost * T * k * (size_t)d));
+  if (out) *out = w;
+  return c.off;
+}
+
+int check_moe_shape(int T, int d, int d_ff, int E, int k) {
+  if (T < 1 || d < 1 || d_ff < 1 || T > kMoeTokens || d > 1 << 20 || d_ff > 1 << 20) return FFN_ERR_SHAPE;
+  if ((int64_t)d_ff * d >= kMaxElems) return FFN_ERR_SHAPE;
+  if (E < 1 || E > kMoeExperts || k < 1 || k > kMoeK || k > E) return FFN_ERR_SHAPE;
+  // z is read through one buffer of less than 2^31 bytes
+  if ((int64_t)T * k * moe_ldz(d_ff) >= kMaxElems / 4) return FFN_ERR_SHAPE;
+  return FFN_OK;
+}
+
+template <bool F32, bool VEC>
+hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
+  const dim3 grid(ceil_div(a.E, 4), ceil_div(a.T, kRouteTokens));
+  if (a.T == 1) k_moe_route<F32, VEC, 1><<<grid, 256, 0, st>>>(a);
+  else k_moe_route<F32, VEC, kRouteTokens><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <bool F32, bool VEC, int NT>
+hipError_t launch_experts(const MoeArgs& a, hipStream_t st) {
+  k_moe_hidden<F32, VEC, NT><<<dim3(a.ldz / 16, a.slots), 256, 0, st>>>(a);
+  if (const hipError_t e = hipGetLastError()) return e;
+  k_moe_down<F32, VEC, NT><<<dim3(ceil_div(a.d, down_columns<F32>()), a.slots, a.pieces), 256, 0, st>>>(a);
+  if (const hipError_t e = hipGetLastError()) return e;
+  k_moe_join<F32><<<dim3(ceil_div(a.d, 256), a.T), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+template <bool F32, bool VEC>
+hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
+  if (r.w)
+    if (const hipError_t e = launch_route<F32, VEC>(r, st)) return e;
+  return a.T <= 16 ? launch_experts<F32, VEC, 1>(a, st) : launch_experts<F32, VEC, 4>(a, st);
+}
+
+}  // namespace
+}  // namespace ffn
+
+using namespace ffn;
+
+extern "C" {
+
+size_t ffn_moe_workspace_bytes(ffn_dtype_t wdt, int T, int d, int d_ff, int experts, int k) {
+  if (!known(wdt) || check_moe_shape(T, d, d_ff, experts, k) != FFN_OK) return 0;
+  return moe_layout(wdt == FFN_F32, T, d, d_ff, experts, k, nullptr, nullptr);
+}
+
+int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t* router, const void* x,
+                    const void* w_gate, const void* w_up, const void* w_down_t, float t, const ffn_options_t* opt,
+                    int32_t* ids, float* weights, void* y, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!router || !x || !w_gate || !w_up || !w_down_t || !ids || !weights || !y || !ws) return FFN_ERR_NULL;
+  if (!known(wdt)) return FFN_ERR_DTYPE;
+  const int E = router->experts, k = router->k;
+  if (const int rc = check_moe_shape(T, d, d_ff, E, k)) return rc;
+  if (!aligned(x) || !aligned(w_gate) || !aligned(w_up) || !aligned(w_down_t) || !aligned(y) || !aligned(ws) ||
+      !aligned(router->w) || !aligned(router->bias, 4) || !aligned(ids, 4) || !aligned(weights, 4))
+    return FFN_ERR_ALIGN;
+  if ((router->sigmoid != 0 && router->sigmoid != 1) || (router->normalize != 0 && router->normalize != 1)) return FFN_ERR_OPTION;
+  if (router->w ? !isfinite(router->scale)
+                : router->bias || router->sigmoid || router->normalize || router->scale != 0.f)
+    return FFN_ERR_OPTION;
+  ActForm form;
+  if (const int rc = check_act(opt, t, &form)) return rc;
+  const bool f32 = wdt == FFN_F32;
+  MoeWs w;
+  if (ws_bytes < moe_layout(f32, T, d, d_ff, E, k, ws, &w)) return FFN_ERR_WORKSPACE;
+
+  const RouteArgs r{T, d, E, k, x, router->w, router->bias, router->sigmoid, router->normalize, router->scale,
+                    w.logits, w.arrived, ids, weights};
+  const MoeArgs a{T, d, d_ff, E, k, moe_ldz(d_ff), moe_slots(T, E, k), moe_pieces(f32, T, d, d_ff, E, k),
+                  x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, w.part, y};
+  const bool vec = d % (f32 ? 4 : 8) == 0;
+  const hipError_t e = f32 ? (vec ? launch_moe<true, true>(r, a, stream) : launch_moe<true, false>(r, a, stream))
+                           : (vec ? launch_moe<false, true>(r, a, stream) : launch_moe<false, false>(r, a, stream));
+  return e == hipSuccess ? FFN_OK : FFN_ERR_HIP;
+}
+
+}  // extern "C"

@@ -16,7 +16,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libffn_sparse.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "ffn_sparse.h")
 HEADERS = [HEADER] + [os.path.join(os.path.dirname(PKG), "include", h) for h in ("ffn_lopa_approx.h", "ffn_gated.h", "ffn_norm.h",
-                                                                      "ffn_group_q.h")]
+                                                                      "ffn_group_q.h", "ffn_moe.h")]
 
 FFN_F32 = 0
 FFN_BF16 = 1
@@ -61,6 +61,12 @@ class GroupQStruct(ctypes.Structure):
     """``ffn_group_q_t``: a matrix of 4-bit codes with group scales (device pointers)."""
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("offsets", ctypes.c_void_p),
                 ("sdt", ctypes.c_int), ("group", ctypes.c_int)]
+
+
+class RouterStruct(ctypes.Structure):
+    """``ffn_router_t``: the router of a mixture-of-experts layer (device pointers)."""
+    _fields_ = [("experts", ctypes.c_int), ("k", ctypes.c_int), ("w", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("sigmoid", ctypes.c_int), ("normalize", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 class FFNError(RuntimeError):
@@ -138,6 +144,10 @@ def lib() -> ctypes.CDLL:
                 ("ffn_group_q_gated_forward", i, [i, i, i, i, vp, gp, gp, f, op, vp, vp, sz, vp])):
             getattr(L, name).restype = res
             getattr(L, name).argtypes = args
+        L.ffn_moe_workspace_bytes.restype = sz
+        L.ffn_moe_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        L.ffn_moe_forward.restype = i
+        L.ffn_moe_forward.argtypes = [i, i, i, i, ctypes.POINTER(RouterStruct), vp, vp, vp, vp, f, op, vp, vp, vp, vp, sz, vp]
         L.ffn_status_string.restype = ctypes.c_char_p
         L.ffn_status_string.argtypes = [i]
         _lib = L
@@ -806,6 +816,56 @@ def ffn_group_q_gated_forward(x, w_gate, w_up, t, opt, z, ws, stream=None):
                                                 _raw_stream(stream, x))
     _check("ffn_group_q_gated_forward", rc)
     return z
+
+
+# ---------------------------------------------------------------- a mixture-of-experts layer
+class Router:
+    """The router of a mixture-of-experts layer: the ``ffn_router_t`` and the tensors it points into."""
+
+    def __init__(self, experts, k, w=None, bias=None, sigmoid=False, normalize=True, scale=1.0):
+        torch = _torch()
+        if w is not None and (w.dim() != 2 or w.shape[0] != experts):
+            raise ValueError(f"w must be [{experts}, d], got {tuple(w.shape)}")
+        if bias is not None and (w is None or bias.dtype != torch.float32 or bias.shape != (experts,)):
+            raise ValueError(f"bias must be float32 [{experts}] beside w, got {bias.dtype} {tuple(bias.shape)}")
+        self.experts, self.k, self.w, self.bias = experts, k, w, bias
+        given = w is None
+        self.struct = RouterStruct(experts, k, _dev(w, "w"), _dev(bias, "bias"), 0 if given else int(bool(sigmoid)),
+                                   0 if given else int(bool(normalize)), 0.0 if given else float(scale))
+
+
+def router(experts, k, w=None, bias=None, sigmoid=False, normalize=True, scale=1.0) -> Router:
+    """A router that chooses k of `experts` experts: w [experts, d] of the tokens' dtype, bias float32 [experts] or None
+    (for the choice alone), logistic scores or a softmax, normalized or not, times scale.  w None: the routing is
+    given with the call."""
+    return Router(experts, k, w, bias, sigmoid, normalize, scale)
+
+
+def alloc_moe_workspace(T, d, d_ff, experts, k, dtype, device="cuda"):
+    """A zero-filled workspace (the header asks for zeros before the first call)."""
+    return _bytes(int(lib().ffn_moe_workspace_bytes(_type_of(dtype), T, d, d_ff, experts, k)), "ffn_moe_workspace_bytes",
+                  device).zero_()
+
+
+def ffn_moe_forward(x, router, w_gate, w_up, w_down_t, t, opt, ids, weights, y, ws, stream=None):
+    """A mixture-of-experts layer of router.k of router.experts gated blocks, stacks w_* [experts, d_ff, d].  ids int32
+    and weights float32 [T, k] are written by the router, or read where ffn.router(...) has no w."""
+    torch = _torch()
+    T, d, dev, wdt = _tokens(x)
+    if w_up.dim() != 3:
+        raise ValueError(f"w_up must be [experts, d_ff, d], got {tuple(w_up.shape)}")
+    E, k, d_ff = router.experts, router.k, w_up.shape[1]
+    w = (E, d_ff, d)
+    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (router.w, "the router's w", (E, d), True), (w_gate, "w_gate", w, False),
+                               (w_up, "w_up", w, False), (w_down_t, "w_down_t", w, False), (y, "y", x.shape, False)))
+    _check_like(dev, torch.int32, ((ids, "ids", (T, k), False),))
+    _check_like(dev, torch.float32, ((weights, "weights", (T, k), False), (router.bias, "the router's bias", (E,), True)))
+    _check_buffers(dev, (ws, "ws"))
+    rc = _function("ffn_moe_forward")(wdt, T, d, d_ff, ctypes.byref(router.struct), x.data_ptr(), w_gate.data_ptr(),
+                                      w_up.data_ptr(), w_down_t.data_ptr(), ctypes.c_float(t), _opt(opt), ids.data_ptr(),
+                                      weights.data_ptr(), y.data_ptr(), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
+    _check("ffn_moe_forward", rc)
+    return y
 
 
 def ffn_status_string(code: int) -> str:
