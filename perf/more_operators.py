@@ -309,11 +309,11 @@ def _kept(s):
         k["ws"] = ffn.alloc_group_q_workspace(T, s["n_in"], s["n_out"], gated=s["op"] == "q4_gated")
         k["opt"] = _options(s)
     else:
-        k["router"] = ffn.router(s["experts"], s["k"], w=s.get("w_router"), bias=s.get("bias"),
+        given = s["router"] == "given"
+        k["router"] = ffn.router(s["experts"], s["k"], w=None if given else s["w_router"], bias=None if given else s["bias"],
                                  sigmoid=s["router"] == "sigmoid", normalize=s["normalize"])
         k["opt"], k["y"] = _options(s), torch.empty_like(x)
         k["ws"] = ffn.alloc_moe_workspace(T, s["d"], s["d_ff"], s["experts"], s["k"], x.dtype)
-        given = s["router"] == "given"
         k["ids"] = s["ids"] if given else torch.empty((T, s["k"]), dtype=torch.int32, device="cuda")
         k["weights"] = s["weights"] if given else torch.empty((T, s["k"]), dtype=torch.float32, device="cuda")
     return k
