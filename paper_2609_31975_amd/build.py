@@ -18,12 +18,13 @@ ROOT = os.path.dirname(PKG)
 SOURCES = [os.path.join(PKG, "csrc", f) for f in ("ffn_api.hip", "ffn_kernels.hip", "ffn_batched.hip",
                                                   "ffn_wide.hip", "ffn_lopa_approx.hip", "ffn_gated_api.hip",
                                                   "ffn_gated_fwd.hip", "ffn_gated_tok.hip", "ffn_gated_bwd.hip",
-                                                  "ffn_norm.hip", "ffn_group_q.hip", "ffn_moe.hip")]
+                                                  "ffn_norm.hip", "ffn_group_q.hip", "ffn_group_q_bf16.hip",
+                                                  "ffn_group_q_f32.hip", "ffn_moe.hip")]
 HEADERS = [os.path.join(ROOT, "include", h) for h in ("ffn_sparse.h", "ffn_lopa_approx.h", "ffn_gated.h",
                                                        "ffn_norm.h", "ffn_group_q.h", "ffn_moe.h")] + \
     [os.path.join(PKG, "csrc", f) for f in ("ffn_internal.h", "ffn_device.h", "ffn_mfma.h", "ffn_gemm.h",
                                                "ffn_gemm_host.h", "ffn_gated_internal.h", "ffn_step_host.h",
-                                               "ffn_step_device.h")]
+                                               "ffn_step_device.h", "ffn_group_q_internal.h", "ffn_group_q_kernels.h")]
 LIB = os.path.join(PKG, "libffn_sparse.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

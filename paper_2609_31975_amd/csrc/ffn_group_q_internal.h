@@ -1,0 +1,64 @@
+// Internal declarations of the products with group scales.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "ffn_step_host.h"
+
+namespace ffn {
+
+constexpr int kWindow = 128;                // codes of a row that four lanes load at once
+constexpr int kGqTokens = 64;               // tokens of a pass
+constexpr int kGqSharesMost = 8;            // of a row's windows
+constexpr size_t kGqLds = 64 * 1024;        // of one token tile's x: two workgroups to a CU
+constexpr int gq_units(bool xf32) { return xf32 ? 2 : 4; }  // 8-column pieces of x that a thread holds while they are on their way
+
+struct GqMatrix {
+  const void *codes, *scales, *offsets;
+};
+struct GqArgs {
+  int T, n_in, n_out;
+  int windows;         // of a row: 128 codes, or 256 (one token)
+  int per_share;       // windows of a workgroup
+  int chunk;           // windows of x in LDS at a time
+  uint32_t div_group;  // q = (n div_group) >> 31 divides a count of 32 codes by group / 32
+  int groups;          // of a row
+  const void* x;
+  GqMatrix w[2];
+  int act, silu_up;
+  float t;
+  void* y;
+  float* part;         // [share][matrix][T][n_out], or null: one share
+  uint4* planes;       // x of two token tiles and more, and the table of its sums (k_group_q_split)
+  float* sums;
+};
+
+// Windows of a wave in a batch, where the next batch's registers fit beside it.
+constexpr int gq_batch(bool gated, int ns) { return (ns > 1 ? 2 : 4) / (gated ? 2 : 1); }
+
+constexpr int gq_batch1(bool gated) { return gated ? 1 : 2; }  // of one token
+
+// Waves that share a row tile's windows with two tiles of tokens and more
+constexpr int kGqWaves = 2;
+
+// Tiles of a pass: nt 16-token tiles (0: one token, windows of 256 codes); wk of the 8 waves share a row tile's windows, u at a time each; whole: a share's x
+// lies in LDS at once.
+struct GqPlan {
+  int nt, wk, u;
+  bool whole;
+  int ns;  // scales of a window
+  int chunk, per_share, shares, blocks;
+};
+// x and its sums in LDS
+inline size_t gq_lds(bool xf32, const GqPlan& p, int T) {
+  const size_t planes = xf32 ? 3 : 1;
+  if (p.nt == 0) return p.chunk * (planes * 4 * kWindow + 32);
+  return planes * T * (p.chunk * 2 * kWindow + 16) + (size_t)p.chunk * p.ns * 64 * p.nt;
+}
+GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out);
+
+// sf32: fp32 scales
+hipError_t launch_group_q_bf16(bool sf32, bool gated, const GqArgs& a, const GqPlan& p, hipStream_t st);
+hipError_t launch_group_q_f32(bool sf32, bool gated, const GqArgs& a, const GqPlan& p, hipStream_t st);
+
+}  // namespace ffn

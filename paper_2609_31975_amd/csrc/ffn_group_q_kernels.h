@@ -1,0 +1,546 @@
+// The kernels of include/ffn_group_q.h: products of a decode step's tokens with 4-bit weights that have a
+// scale (and an offset) for every group of codes along the summed dimension.  Not part of the public ABI.
+//
+// The codes' bytes bound it, and the work that a byte brings: two codes to turn into matrix operands.  So:
+//   - The codes enter the bf16 products unscaled.  Two nibbles of a dword become two bf16 of value 24 + code (16 + u has
+//     u in its top mantissa bits; u = code + 8): 8 operations for 8 codes.  What the 24 add, 24 times the sum of the
+//     same x, is in a table in LDS that the sums start from.  A group's sum is then multiplied by its row's scale.
+//   - One token: dot products on the vector ALUs (k_group_q1).  More: v_mfma_f32_16x16x32_bf16 (k_group_q).
+//   - Tokens are the A operand, weight rows the B operand: a lane's results are of one weight row, whose scale it
+//     holds.
+//   - A lane loads 16 bytes, 32 codes of a row; the four lanes of a row 128 (a window).  Where a window lies in one
+//     group, MFMA f takes dword f of every lane, and x in the same order.  Else the four dwords are transposed between
+//     the lanes (two v_permlane32_swap, two v_permlane16_swap), and each MFMA has 32 codes in a row.
+//   - x lies in LDS, as bf16 in the order of the operands; fp32 x as three bf16 parts, three products.
+#pragma once
+
+#include <algorithm>
+#include <type_traits>
+
+#include "ffn_group_q_internal.h"
+#include "ffn_mfma.h"
+#include "ffn_step_device.h"
+
+namespace ffn {
+namespace {
+
+// The four pairs of a dword, elements (0, 4), (1, 5), (2, 6), (3, 7), as 24 + code: a shift and one three-input operation
+// each (mask, and an exclusive or that sets 16's bits and turns the code's sign bit over).  An instruction takes one constant
+// from the scalar side: `mask` is kMask in a vector register.
+constexpr uint32_t kMask = 0x00780078u;
+__device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t mask) {
+  constexpr uint32_t s = 0x41C041C0u;
+  return make_uint4((w << 3 & mask) ^ s, (w >> 1 & mask) ^ s, (w >> 5 & mask) ^ s, (w >> 9 & mask) ^ s);
+}
+
+// dword f of lane group g <- dword g of lane group f
+__device__ __forceinline__ uint4 transpose4(const uint4& v) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  const u2 a = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(v.x, v.z, false, false));
+  const u2 b = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(v.y, v.w, false, false));
+  const u2 c = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false));
+  const u2 d = __builtin_bit_cast(u2, __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false));
+  return make_uint4(c[0], c[1], d[0], d[1]);
+}
+
+// 8 columns of a token as bf16 in the order of the operands, elements (0, 4), (1, 5), (2, 6), (3, 7), fp32 in three parts; their sum.
+template <bool XF32>
+__device__ __forceinline__ float split_piece(const uint4 (&v)[XF32 ? 2 : 1], uint4 (&d)[XF32 ? 3 : 1]) {
+  float f[8];
+  if constexpr (XF32) {
+    const uint4 lo = v[0], hi = v[1];
+    float r[8] = {comp<0>(lo), comp<0>(hi), comp<1>(lo), comp<1>(hi), comp<2>(lo), comp<2>(hi), comp<3>(lo), comp<3>(hi)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = r[e];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = f_to_bf2(r[2 * e], r[2 * e + 1]);
+        r[2 * e] -= __uint_as_float(w[e] << 16);
+        r[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+      }
+      d[q] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+    unpack(WBf16{}, v[0], f);
+    d[0] = make_uint4(__builtin_amdgcn_perm(v[0].z, v[0].x, 0x05040100u), __builtin_amdgcn_perm(v[0].z, v[0].x, 0x07060302u),
+                      __builtin_amdgcn_perm(v[0].w, v[0].y, 0x05040100u), __builtin_amdgcn_perm(v[0].w, v[0].y, 0x07060302u));
+  }
+  return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+}
+
+// A chunk of windows of x's T rows, on its way into LDS: rows of chunk * 256 + 16 bytes (the 16 spread the rows over the
+// banks), plane after plane, in pieces of 8 columns, of which a thread holds up to gq_units.  Columns past n_in are zero.
+// Behind the planes the table of -24 times the sum of x: SUMS rows for a window, of all tokens of the tiles.
+template <bool XF32, int SUMS, int TOKENS>
+struct XPieces {
+  static constexpr int N = gq_units(XF32), THREADS = 512, SPAN = N * THREADS;
+  uint4 v[N][XF32 ? 2 : 1];
+
+  __device__ __forceinline__ void load(const GqArgs& a, int w0, int from) {
+    const int units = a.chunk * (kWindow / 8);
+    const Buf xb = make_buf(a.x, (uint32_t)a.T * a.n_in * (XF32 ? 4 : 2));
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = from + j * THREADS + (int)threadIdx.x, t = i / units, k = w0 * kWindow + (i - t * units) * 8;
+      const uint32_t o = t < a.T && k < a.n_in ? ((uint32_t)t * a.n_in + k) * (XF32 ? 4 : 2) : kOOB;
+      v[j][0] = ldb(xb, o);
+      if constexpr (XF32) v[j][1] = ldb(xb, o + 16);
+    }
+  }
+  static __device__ __forceinline__ float* table(const GqArgs& a, char* lds) {
+    return reinterpret_cast<float*>(lds + (XF32 ? 3 : 1) * a.T * (a.chunk * 2 * kWindow + 16));
+  }
+  __device__ __forceinline__ void store(const GqArgs& a, char* lds, int from) const {
+    const int units = a.chunk * (kWindow / 8), stride = a.chunk * 2 * kWindow + 16;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = from + j * THREADS + (int)threadIdx.x, t = i / units;
+      uint4 d[XF32 ? 3 : 1];
+      const float sum = group_sum(split_piece<XF32>(v[j], d), 16 / SUMS);  // the pieces of a window lie in 16 neighbouring lanes
+      if (t >= a.T) continue;
+      const int c = i - t * units;
+      if (c % (16 / SUMS) == 0) table(a, lds)[c / (16 / SUMS) * TOKENS + t] = -24.f * sum;
+      char* p = lds + t * stride + c * 16;
+#pragma unroll
+      for (int q = 0; q < (XF32 ? 3 : 1); ++q) *reinterpret_cast<uint4*>(p + q * a.T * stride) = d[q];
+    }
+  }
+};
+
+// Two token tiles and more: what XPieces makes in LDS is made once for all workgroups, in memory: planes [P][T][windows 128] and
+// the table [windows][NS][tokens of the tiles].
+template <bool XF32, int NS>
+__global__ __launch_bounds__(256) void k_group_q_split(GqArgs a, int tokens) {
+  const int pieces = a.windows * (kWindow / 8), i = blockIdx.x * 256 + threadIdx.x, t = i / pieces, c = i - t * pieces;
+  const Buf xb = make_buf(a.x, (uint32_t)a.T * a.n_in * (XF32 ? 4 : 2));
+  const uint32_t o = t < a.T && c * 8 < a.n_in ? ((uint32_t)t * a.n_in + c * 8) * (XF32 ? 4 : 2) : kOOB;
+  uint4 v[XF32 ? 2 : 1], d[XF32 ? 3 : 1];
+  v[0] = ldb(xb, o);
+  if constexpr (XF32) v[1] = ldb(xb, o + 16);
+  const float sum = group_sum(split_piece<XF32>(v, d), 16 / NS);
+  if (t >= a.T) return;
+#pragma unroll
+  for (int q = 0; q < (XF32 ? 3 : 1); ++q) a.planes[((size_t)q * a.T + t) * pieces + c] = d[q];
+  if (c % (16 / NS) == 0) a.sums[(size_t)(c / (16 / NS)) * tokens + t] = -24.f * sum;
+}
+// WK windows of it on their way into LDS, in the same places as XPieces has them.
+template <bool XF32, int NS, int NT, int WK>
+struct XCopy {
+  static constexpr int P = XF32 ? 3 : 1, UNITS = WK * (kWindow / 8), ROWS = P * 16 * NT, N = ROWS * UNITS / 512;
+  static constexpr int SUMS = WK * NS * 16 * NT;  // 512 or fewer
+  uint4 v[N];
+  float sum;
+
+  __device__ __forceinline__ void load(const GqArgs& a, int w0, int) {
+    const int pieces = a.windows * (kWindow / 8);
+    const Buf b = make_buf(a.planes, (uint32_t)(P * a.T * pieces) * 16u), tb = make_buf(a.sums, (uint32_t)a.windows * NS * 64 * NT);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = j * 512 + (int)threadIdx.x, r = i / UNITS, c = w0 * (kWindow / 8) + i % UNITS;
+      v[j] = ldb(b, r < P * a.T && c < pieces ? (uint32_t)(r * pieces + c) * 16u : kOOB);
+    }
+    sum = __builtin_bit_cast(float, ldb32(tb, (int)threadIdx.x < SUMS ? (uint32_t)(w0 * NS * 16 * NT + threadIdx.x) * 4u : kOOB));
+  }
+  static __device__ __forceinline__ float* table(const GqArgs& a, char* lds) {
+    return reinterpret_cast<float*>(lds + P * a.T * (WK * 2 * kWindow + 16));
+  }
+  __device__ __forceinline__ void store(const GqArgs& a, char* lds, int) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = j * 512 + (int)threadIdx.x, r = i / UNITS;
+      if (r < P * a.T) *reinterpret_cast<uint4*>(lds + r * (WK * 2 * kWindow + 16) + i % UNITS * 16) = v[j];
+    }
+    if ((int)threadIdx.x < SUMS) table(a, lds)[threadIdx.x] = sum;
+  }
+};
+
+// 8 waves: WK of them share a row tile's windows, 8 / WK row tiles of 16 to a workgroup.  NT: 16-token
+// tiles.  U: windows of a wave in a batch; the next batch is on its way during a batch's products.  NS: scales of a window, 1,
+// 2 or 4 (groups that are multiples of 128, of 64, of 32).  OFF: there are offsets.  WHOLE: all of a share's x is in LDS at once.
+template <bool XF32, bool SF32, bool GATED, int NS, bool OFF, int NT, int WK, int U, bool WHOLE>
+__global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
+  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK * U, PER = 4 / NS;
+  constexpr bool TR = NS > 1;
+  extern __shared__ __align__(16) char lds[];
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int wk = wave % WK;
+  // rows past the last one repeat it, and are not stored
+  const uint32_t row = min((int)(blockIdx.x * WR + wave / WK) * 16 + n, a.n_out - 1);
+  const int first = blockIdx.y * a.per_share, last = min(a.windows, first + a.per_share);
+  const uint32_t row_bytes = (uint32_t)a.n_in / 2, ss = SF32 ? 4 : 2;
+
+  Buf cb[M], sb[M], ob[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    cb[m] = make_buf(a.w[m].codes, row_bytes * a.n_out);
+    sb[m] = make_buf(a.w[m].scales, (uint32_t)a.n_out * a.groups * ss);
+    ob[m] = make_buf(a.w[m].offsets, a.w[m].offsets ? (uint32_t)a.n_out * a.groups * ss : 0u);
+  }
+  const uint32_t code_at = row * row_bytes + g * 16, scale_at = row * a.groups * ss;
+
+  struct Batch {
+    uint4 codes[U][M];
+    uint32_t sc[U][M][NS], of[OFF ? U : 1][M][NS];
+  };
+  auto raw = [&](const Buf& b, uint32_t i) -> uint32_t {
+    if constexpr (SF32) return (uint32_t)ldb32(b, i);
+    else return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, i, 0, 0);
+  };
+  auto value = [](uint32_t v) { return __uint_as_float(SF32 ? v : v << 16); };
+  // Lines of 128 bytes are read in two halves, by the same wave or its neighbour: through the caches (streamed past them
+  // the same reads came to 5.2 TB/s, through them to 5.6).  Codes behind the row's end, of the next row or zeros behind the
+  // matrix, meet zeros of x; scales behind the share's or the row's end are zeros, never the next row's.
+  auto load = [&](int w_first, Batch& b) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int w = w_first + wk * U + u;
+#pragma unroll
+      for (int m = 0; m < M; ++m) b.codes[u][m] = ldb(cb[m], code_at + w * (kWindow / 2));
+#pragma unroll
+      for (int f = 0; f < NS; ++f) {
+        const uint32_t k32 = w * 4 + f * PER, gi = (uint32_t)((uint64_t)k32 * a.div_group >> 31);
+        const uint32_t at = scale_at + (w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          b.sc[u][m][f] = raw(sb[m], at);
+          if constexpr (OFF) b.of[u][m][f] = raw(ob[m], at);
+        }
+      }
+    }
+  };
+
+  f32x4_t acc[NT][M] = {};
+  const int stride = a.chunk * 2 * kWindow + 16;
+  int xrow[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) xrow[t] = min(t * 16 + n, a.T - 1) * stride;
+  uint32_t mask = kMask;
+  asm("" : "+v"(mask));
+
+  // Where all of x lies in LDS, the workgroups go through it from different places on: with rows of 2^n bytes all of them
+  // would be on the same few memory channels at any time (rows of 4096 bytes: 4.3 TB/s, so 5.25).
+  const int batches = (last - first + UNIT - 1) / UNIT;
+  int turn = WHOLE ? (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)batches) : 0;
+  Batch cur;
+  load(first + turn * UNIT, cur);
+  using Pieces = std::conditional_t<NT == 1, XPieces<XF32, NS, 16>, XCopy<XF32, NS, NT, WK>>;
+  Pieces xp;
+  xp.load(a, first, 0);
+  for (int c0 = first; c0 < last; c0 += a.chunk) {
+    if (c0 != first) __syncthreads();
+    xp.store(a, lds, 0);
+    if constexpr (WHOLE) {
+      for (int i = Pieces::SPAN; i < a.T * a.chunk * (kWindow / 8); i += Pieces::SPAN) {
+        xp.load(a, c0, i);
+        xp.store(a, lds, i);
+      }
+    }
+    __syncthreads();
+    if (!WHOLE && c0 + a.chunk < last) xp.load(a, c0 + a.chunk, 0);
+    for (int b0 = 0; b0 < min(a.chunk, last - c0); b0 += UNIT) {
+      const int here = first + turn * UNIT - c0;  // a window of the chunk
+      turn = turn + 1 == batches ? 0 : turn + 1;
+      Batch nxt;
+      load(first + turn * UNIT, nxt);
+      issue_barrier();
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int w = here + wk * U + u;  // the chunk is a multiple of UNIT
+        uint4 q[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) q[m] = TR ? transpose4(cur.codes[u][m]) : cur.codes[u][m];
+        // The sums of tokens past the last one, and their starts, stay in their own rows, which are not stored.
+        const f32x4_t* tab = reinterpret_cast<const f32x4_t*>(Pieces::table(a, lds)) + w * NS * 4 * NT + g;
+        f32x4_t sum[NT][M], gone[NT];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          bf16x8_t wf[M];
+#pragma unroll
+          for (int m = 0; m < M; ++m) wf[m] = bf8(codes8(f == 0 ? q[m].x : f == 1 ? q[m].y : f == 2 ? q[m].z : q[m].w, mask));
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const char* xr = lds + xrow[t] + w * 2 * kWindow + (TR ? f * 64 + g * 16 : g * 64 + f * 16);
+            bf16x8_t x[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) x[p] = bf8(*reinterpret_cast<const uint4*>(xr + p * a.T * stride));
+            if (f % PER == 0) {
+              gone[t] = tab[f / PER * 4 * NT + t * 4];
+#pragma unroll
+              for (int m = 0; m < M; ++m) sum[t][m] = gone[t];
+            }
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+              for (int m = 0; m < M; ++m) sum[t][m] = mfma16(x[p], wf[m], sum[t][m]);
+            if (f % PER == PER - 1) {
+              const int s = f / PER;
+#pragma unroll
+              for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][m][i] += value(cur.sc[u][m][s]) * sum[t][m][i];
+              if constexpr (OFF) {
+                const f32x4_t sx = gone[t] * (-1.f / 24.f);
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) acc[t][m][i] += value(cur.of[u][m][s]) * sx[i];
+              }
+            }
+          }
+          // operands of one f at a time: more of them in registers spill
+          if constexpr (NT > 1) issue_barrier();
+        }
+      }
+      cur = nxt;
+    }
+  }
+
+  // The WK waves' sums joined in LDS, in their order; one token tile at a time.
+  float* red = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[((wave * M + m) * 4 + i) * 64 + lane] = acc[t][m][i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < WR * 256; e += 512) {
+      const int r = e >> 8, i = e >> 6 & 3, l = e & 63;
+      const int tok = t * 16 + (l >> 4) * 4 + i, o = (blockIdx.x * WR + r) * 16 + (l & 15);
+      if (tok >= a.T || o >= a.n_out) continue;
+      float v[M] = {};
+#pragma unroll
+      for (int k = 0; k < WK; ++k)
+#pragma unroll
+        for (int m = 0; m < M; ++m) v[m] += red[(((r * WK + k) * M + m) * 4 + i) * 64 + l];
+      if (a.part) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) a.part[(((size_t)blockIdx.y * M + m) * a.T + tok) * a.n_out + o] = v[m];
+      } else {
+        store_as<XF32>(a.y, (size_t)tok * a.n_out + o, GATED ? act_product(ActForm{a.act, a.silu_up, a.t}, v[0], v[M - 1]) : v[0]);
+      }
+    }
+  }
+}
+
+// One token.  A load takes 128 bytes of 8 rows (whole lines, streamed past the caches), 32 codes a lane, and those lie in
+// one group whatever it is; a wave takes 16 rows, two loads, of 256 columns (a window here).  A lane's products with its
+// 32 x are 16 v_dot2; 8 lanes share a row.  x in LDS: piece f (8 columns) of a window's 8 lanes side by side.
+template <bool XF32, bool SF32, bool GATED, bool OFF, int WK, int U>
+__global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
+  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK * U, WIN = 2 * kWindow;
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  extern __shared__ __align__(16) char lds[];
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), c = lane & 7, wk = wave % WK;
+  const int row0 = (blockIdx.x * WR + wave / WK) * 16 + (lane >> 3);
+  const int first = blockIdx.y * a.per_share, last = min(a.windows, first + a.per_share);
+  const uint32_t row_bytes = (uint32_t)a.n_in / 2, ss = SF32 ? 4 : 2;
+  uint32_t code_at[2], scale_at[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {  // rows past the last one repeat it, and are not stored
+    const uint32_t row = min(row0 + 8 * s, a.n_out - 1);
+    code_at[s] = row * row_bytes + c * 16;
+    scale_at[s] = row * a.groups * ss;
+  }
+  Buf cb[M], sb[M], ob[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    cb[m] = make_buf(a.w[m].codes, row_bytes * a.n_out);
+    sb[m] = make_buf(a.w[m].scales, (uint32_t)a.n_out * a.groups * ss);
+    ob[m] = make_buf(a.w[m].offsets, a.w[m].offsets ? (uint32_t)a.n_out * a.groups * ss : 0u);
+  }
+  struct Batch {
+    uint4 codes[U][2][M];
+    uint32_t sc[U][2][M], of[OFF ? U : 1][2][M];
+  };
+  auto raw = [&](const Buf& b, uint32_t i) -> uint32_t {
+    if constexpr (SF32) return (uint32_t)ldb32(b, i);
+    else return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, i, 0, 0);
+  };
+  auto value = [](uint32_t v) { return __uint_as_float(SF32 ? v : v << 16); };
+  // codes and scales behind a row's or the share's end: as in k_group_q
+  auto load = [&](int w_first, Batch& b) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int w = w_first + wk * U + u;
+      const uint32_t k32 = w * 8 + c, gi = __umulhi(2 * k32, a.div_group);
+      const uint32_t at = w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          b.codes[u][s][m] = ldb_nt(cb[m], code_at[s] + w * (WIN / 2));
+          b.sc[u][s][m] = raw(sb[m], scale_at[s] + at);
+          if constexpr (OFF) b.of[u][s][m] = raw(ob[m], scale_at[s] + at);
+        }
+    }
+  };
+
+  float acc[2][M] = {};
+  uint32_t mask = kMask;
+  asm("" : "+v"(mask));
+  const int plane = a.chunk * WIN * 2;
+  float* tab = reinterpret_cast<float*>(lds + P * plane);
+  const Buf xb = make_buf(a.x, (uint32_t)a.n_in * (XF32 ? 4 : 2));
+  // the workgroups start at different places of the rows: as in k_group_q
+  const int batches = (last - first + UNIT - 1) / UNIT;
+  int turn = last - first <= a.chunk ? (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)batches) : 0;
+  Batch cur;
+  load(first + turn * UNIT, cur);
+  for (int c0 = first; c0 < last; c0 += a.chunk) {
+    if (c0 != first) __syncthreads();
+    for (int i = threadIdx.x; i < a.chunk * (WIN / 8); i += 512) {
+      const int k = c0 * WIN + i * 8;
+      const uint32_t o = k < a.n_in ? (uint32_t)k * (XF32 ? 4 : 2) : kOOB;
+      char* p = lds + (i >> 5) * (WIN * 2) + (i & 3) * 128 + (i >> 2 & 7) * 16;
+      uint4 v[XF32 ? 2 : 1], d[P];
+      v[0] = ldb(xb, o);
+      if constexpr (XF32) v[1] = ldb(xb, o + 16);
+      const float s = group_sum(split_piece<XF32>(v, d), 4);
+#pragma unroll
+      for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(p + q * plane) = d[q];
+      if ((i & 3) == 0) tab[i >> 2] = -24.f * s;
+    }
+    __syncthreads();
+    for (int b0 = 0; b0 < min(a.chunk, last - c0); b0 += UNIT) {
+      const int here = first + turn * UNIT - c0;  // a window of the chunk
+      turn = turn + 1 == batches ? 0 : turn + 1;
+      Batch nxt;
+      load(first + turn * UNIT, nxt);
+      issue_barrier();
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int w = here + wk * U + u;  // the chunk is a multiple of UNIT
+        const float gone = tab[w * 8 + c];
+        uint4 x[P][4];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) x[p][f] = *reinterpret_cast<const uint4*>(lds + p * plane + w * (WIN * 2) + f * 128 + c * 16);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int m = 0; m < M; ++m) {
+            const uint4 q = cur.codes[u][s][m];
+            const uint4 d[4] = {codes8(q.x, mask), codes8(q.y, mask), codes8(q.z, mask), codes8(q.w, mask)};
+            float sum = gone;
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+              for (int f = 0; f < 4; ++f) {
+                auto dot = [&](uint32_t l, uint32_t r) {
+                  sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, l), __builtin_bit_cast(bf16x2_t, r), sum, false);
+                };
+                dot(d[f].x, x[p][f].x);
+                dot(d[f].y, x[p][f].y);
+                dot(d[f].z, x[p][f].z);
+                dot(d[f].w, x[p][f].w);
+              }
+            acc[s][m] += value(cur.sc[u][s][m]) * sum;
+            if constexpr (OFF) acc[s][m] += value(cur.of[u][s][m]) * (gone * (-1.f / 24.f));
+          }
+      }
+      cur = nxt;
+    }
+  }
+
+  // 8 lanes of a row, then the WK waves, in their order
+  float* red = reinterpret_cast<float*>(lds);
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const float v = group_sum(acc[s][m], 8);
+      if (c == 0) red[(wave * M + m) * 16 + s * 8 + (lane >> 3)] = v;
+    }
+  __syncthreads();
+  const int r = threadIdx.x >> 4, o = (blockIdx.x * WR + r) * 16 + (threadIdx.x & 15);
+  if (r >= WR || o >= a.n_out) return;
+  float v[M] = {};
+#pragma unroll
+  for (int k = 0; k < WK; ++k)
+#pragma unroll
+    for (int m = 0; m < M; ++m) v[m] += red[((r * WK + k) * M + m) * 16 + (threadIdx.x & 15)];
+  if (a.part) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) a.part[((size_t)blockIdx.y * M + m) * a.n_out + o] = v[m];
+  } else {
+    store_as<XF32>(a.y, o, GATED ? act_product(ActForm{a.act, a.silu_up, a.t}, v[0], v[M - 1]) : v[0]);
+  }
+}
+
+template <bool XF32, bool GATED>
+__global__ __launch_bounds__(256) void k_group_q_join(GqArgs a, int shares) {
+  constexpr int M = GATED ? 2 : 1;
+  const size_t count = (size_t)a.T * a.n_out;
+  for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < count; e += (size_t)gridDim.x * 256) {
+    float p[kGqSharesMost][M], v[M] = {};
+#pragma unroll
+    for (int s = 0; s < kGqSharesMost; ++s)
+#pragma unroll
+      for (int m = 0; m < M; ++m) p[s][m] = s < shares ? a.part[((size_t)s * M + m) * count + e] : 0.f;
+#pragma unroll
+    for (int s = 0; s < kGqSharesMost; ++s)
+#pragma unroll
+      for (int m = 0; m < M; ++m) v[m] += p[s][m];
+    store_as<XF32>(a.y, e, GATED ? act_product(ActForm{a.act, a.silu_up, a.t}, v[0], v[M - 1]) : v[0]);
+  }
+}
+
+template <bool XF32, bool SF32, bool GATED, bool OFF>
+hipError_t launch_one(const GqArgs& a, const GqPlan& p, hipStream_t st) {
+  constexpr int U = gq_batch1(GATED);
+  const dim3 grid(p.blocks, p.shares);
+  auto go = [&](auto wk) {
+    k_group_q1<XF32, SF32, GATED, OFF, wk.value, U><<<grid, 512, gq_lds(XF32, p, 1), st>>>(a);
+    return hipGetLastError();
+  };
+  return p.wk == 8 ? go(Int<8>{}) : p.wk == 4 ? go(Int<4>{}) : go(Int<2>{});
+}
+
+template <bool XF32, bool SF32, bool GATED, int NS, bool OFF>
+hipError_t launch_tiles(const GqArgs& a, const GqPlan& p, hipStream_t st) {
+  const size_t lds = std::max<size_t>(gq_lds(XF32, p, a.T), 8 * (GATED ? 2 : 1) * 1024);
+  const dim3 grid(p.blocks, p.shares);
+  auto go = [&](auto nt, auto wk, auto u, auto whole) {
+    k_group_q<XF32, SF32, GATED, NS, OFF, nt.value, wk.value, u.value, whole.value><<<grid, 512, lds, st>>>(a);
+    return hipGetLastError();
+  };
+  constexpr int U = gq_batch(GATED, NS);
+  constexpr Int<0> no;
+  constexpr Int<1> yes;
+  if (p.whole) {
+    if (p.wk == 8) return go(Int<1>{}, Int<8>{}, Int<U>{}, yes);
+    return p.wk == 4 ? go(Int<1>{}, Int<4>{}, Int<U>{}, yes) : go(Int<1>{}, Int<2>{}, Int<U>{}, yes);
+  }
+  if (p.nt == 1) return p.wk == 8 ? go(Int<1>{}, Int<8>{}, Int<1>{}, no) : go(Int<1>{}, Int<4>{}, Int<1>{}, no);
+  k_group_q_split<XF32, NS><<<ceil_div(a.T * a.windows * (kWindow / 8), 256), 256, 0, st>>>(a, 16 * p.nt);
+  if (const hipError_t e = hipGetLastError()) return e;
+  constexpr Int<kGqWaves> w;
+  return p.nt == 2 ? go(Int<2>{}, w, Int<1>{}, no) : p.nt == 3 ? go(Int<3>{}, w, Int<1>{}, no) : go(Int<4>{}, w, Int<1>{}, no);
+}
+
+template <bool XF32, bool GATED>
+hipError_t launch_form(bool sf32, const GqArgs& a, const GqPlan& p, hipStream_t st) {
+  auto by_scales = [&](auto s, auto o) {
+    if (p.nt == 0) return launch_one<XF32, s.value, GATED, o.value>(a, p, st);
+    return p.ns == 1 ? launch_tiles<XF32, s.value, GATED, 1, o.value>(a, p, st)
+           : p.ns == 2 ? launch_tiles<XF32, s.value, GATED, 2, o.value>(a, p, st)
+                       : launch_tiles<XF32, s.value, GATED, 4, o.value>(a, p, st);
+  };
+  const bool off = a.w[0].offsets != nullptr;
+  const hipError_t e = sf32 ? (off ? by_scales(Int<1>{}, Int<1>{}) : by_scales(Int<1>{}, Int<0>{}))
+                            : (off ? by_scales(Int<0>{}, Int<1>{}) : by_scales(Int<0>{}, Int<0>{}));
+  if (e != hipSuccess || p.shares == 1) return e;
+  const size_t blocks = ceil_div<size_t>((size_t)a.T * a.n_out, 256);
+  k_group_q_join<XF32, GATED><<<(int)std::min<size_t>(blocks, 4096), 256, 0, st>>>(a, p.shares);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace ffn

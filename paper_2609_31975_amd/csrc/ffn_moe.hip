@@ -20,6 +20,7 @@ namespace ffn {
 namespace {
 
 constexpr int kMoeTokens = 256, kMoeK = 16, kMoeExperts = 512;
+constexpr int kPiecesMost = 8;   // of an expert's neurons
 constexpr int kRouteTokens = 8;  // tokens that choose together
 constexpr int kMoeCounters = kMoeTokens / kRouteTokens;
 
@@ -63,82 +64,99 @@ __device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
   }
 }
-template <bool F32, bool VEC>
-__device__ __forceinline__ uint4 ld_weight_chunk(const Buf& b, uint32_t i, int left) {
-  if constexpr (VEC) return ldb_nt(b, left > 0 ? i * (F32 ? 4u : 2u) : kOOB);
-  else return ld_chunk<F32, VEC>(b, i, left);
+__device__ __forceinline__ uint4 ldb_nt(const Buf& b, uint32_t off, uint32_t uniform_off) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b.r, off, uniform_off, 2));
 }
-
 // ------------------------------------------------------------------ the router
+template <int CTRL>
+__device__ __forceinline__ double dpp_move64(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double lane64(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)u, lane), hi = __builtin_amdgcn_readlane((int)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// every lane's v joined, as group_sum joins floats
+template <class F>
+__device__ __forceinline__ double wave_join64(double v, const F& f) {
+  v = f(v, dpp_move64<kDppXor1>(v));
+  v = f(v, dpp_move64<kDppXor2>(v));
+  v = f(v, dpp_move64<kDppHalfMirror>(v));
+  v = f(v, dpp_move64<kDppMirror>(v));
+  return f(f(lane64(v, 0), lane64(v, 16)), f(lane64(v, 32), lane64(v, 48)));
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int s = 1; s < kWave; s *= 2) v += __shfl_xor(v, s);
-  return v;
+  return wave_join64(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double wave_max64(double v) {
+  return wave_join64(v, [](double a, double b) { return b > a ? b : a; });
 }
 
-// The choice of one token, by one wave.  A lane has the scores of experts lane, 64 + lane, ...
+// The choice of one token, by one wave.  A lane has the scores of experts lane, 64 + lane, ... (N of them).
+template <int N>
 __device__ __forceinline__ void choose(const RouteArgs& a, int tok) {
-  constexpr int N = kMoeExperts / kWave;
   const int lane = lane_id();
-  double l[N], key[N];
-  double top = -INFINITY;
+  double score[N], key[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = i * kWave + lane;
-    l[i] = e < a.E ? a.logits[(size_t)tok * a.E + e] : -INFINITY;
-    top = l[i] > top ? l[i] : top;
+    score[i] = e < a.E ? a.logits[(size_t)tok * a.E + e] : -INFINITY;
+    key[i] = score[i];
   }
-  double total = 0.0;
-  if (!a.sigmoid) {
+  if (a.sigmoid) {
 #pragma unroll
-    for (int s = 1; s < kWave; s *= 2) {
-      const double o = __shfl_xor(top, s);
-      top = o > top ? o : top;
+    for (int i = 0; i < N; ++i) score[i] = 1.0 / (1.0 + exp(-score[i]));
+  } else {
+    double top = -INFINITY, total = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = score[i] > top ? score[i] : top;
+    top = wave_max64(top);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      score[i] = exp(score[i] - top);
+      total += i * kWave + lane < a.E ? score[i] : 0.0;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i * kWave < a.E) total += i * kWave + lane < a.E ? exp(l[i] - top) : 0.0;
     total = wave_sum64(total);
+#pragma unroll
+    for (int i = 0; i < N; ++i) score[i] /= total;
   }
-  auto score = [&](double v) { return a.sigmoid ? 1.0 / (1.0 + exp(-v)) : exp(v - top) / total; };
   uint32_t open = 0;  // experts of this lane that are not chosen yet
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int e = i * kWave + lane;
-    key[i] = l[i];
-    if (e < a.E) {
-      if (a.bias) key[i] = score(l[i]) + (double)a.bias[e];
-      key[i] = key[i] == key[i] ? key[i] : -INFINITY;
-      open |= 1u << i;
-    }
+    if (e >= a.E) continue;
+    if (a.bias) key[i] = score[i] + (double)a.bias[e];
+    key[i] = key[i] == key[i] ? key[i] : -INFINITY;
+    open |= 1u << i;
   }
   double sum = 0.0, mine = 0.0;
   int mine_e = 0;
   for (int j = 0; j < a.k; ++j) {
-    double best = -INFINITY, bl = 0.0;
-    int be = 1 << 30;
+    double best = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const bool better = (open >> i & 1) && (key[i] > best || be == 1 << 30);
-      best = better ? key[i] : best;
-      bl = better ? l[i] : bl;
-      be = better ? i * kWave + lane : be;
-    }
+    for (int i = 0; i < N; ++i) best = (open >> i & 1) && key[i] > best ? key[i] : best;
+    best = wave_max64(best);
+    // the lowest of the open experts that have it
+    int at = -1, from = 0;
 #pragma unroll
-    for (int s = 1; s < kWave; s *= 2) {
-      const double ob = __shfl_xor(best, s), ol = __shfl_xor(bl, s);
-      const int oe = __shfl_xor(be, s);
-      const bool take = ob > best || (ob == best && oe < be);
-      best = take ? ob : best;
-      bl = take ? ol : bl;
-      be = take ? oe : be;
+    for (int i = N - 1; i >= 0; --i) {
+      const uint64_t m = __ballot((open >> i & 1) && key[i] == best);
+      at = m ? i : at;
+      from = m ? __builtin_ctzll(m) : from;
     }
-    if ((be & (kWave - 1)) == lane) open &= ~(1u << (be >> 6));
-    const double s = score(bl);
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i == at) s = lane64(score[i], from);
+    if (lane == from) open &= ~(1u << at);
     sum += s;
     if (lane == j) {
       mine = s;
-      mine_e = be;
+      mine_e = at * kWave + from;
     }
   }
   if (lane < a.k) {
@@ -158,21 +176,30 @@ __global__ __launch_bounds__(256) void k_moe_route(RouteArgs a) {
     const size_t es = F32 ? 4 : 2;
     const Buf wb = make_buf(static_cast<const char*>(a.w) + (size_t)e * a.d * es, a.d * (uint32_t)es);
     const Buf xb = make_buf(static_cast<const char*>(a.x) + (size_t)t0 * a.d * es, nt * a.d * (uint32_t)es);
+    // U chunks' loads at once; the same order of additions whatever NT
+    constexpr int U = VEC ? (NT == 1 ? 4 : 2) : 1;
     double s[NT] = {};
-    for (int k = lane * E; k < a.d; k += kWave * E) {
-      float w[E], x[E];
-      const uint4 wv = ld_chunk<F32, VEC>(wb, k, a.d - k);
-      uint4 xv[NT];
+    for (int k0 = lane * E; k0 < a.d; k0 += U * kWave * E) {
+      uint4 wv[U], xv[U][NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) xv[t] = ld_chunk<F32, VEC>(xb, t * a.d + k, t < nt ? a.d - k : 0);
-      if constexpr (F32) unpack(WF32{}, wv, w);
-      else unpack(WBf16{}, wv, w);
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * kWave * E;
+        wv[u] = ld_chunk<F32, VEC>(wb, k, a.d - k);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if constexpr (F32) unpack(WF32{}, xv[t], x);
-        else unpack(WBf16{}, xv[t], x);
+        for (int t = 0; t < NT; ++t) xv[u][t] = ld_chunk<F32, VEC>(xb, t * a.d + k, t < nt ? a.d - k : 0);
+      }
 #pragma unroll
-        for (int j = 0; j < E; ++j) s[t] = fma((double)w[j], (double)x[j], s[t]);
+      for (int u = 0; u < U; ++u) {
+        float w[E], x[E];
+        if constexpr (F32) unpack(WF32{}, wv[u], w);
+        else unpack(WBf16{}, wv[u], w);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if constexpr (F32) unpack(WF32{}, xv[u][t], x);
+          else unpack(WBf16{}, xv[u][t], x);
+#pragma unroll
+          for (int j = 0; j < E; ++j) s[t] = fma((double)w[j], (double)x[j], s[t]);
+        }
       }
     }
 #pragma unroll
@@ -191,7 +218,11 @@ __global__ __launch_bounds__(256) void k_moe_route(RouteArgs a) {
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  for (int t = t0 + wave; t < min(a.T, t0 + kRouteTokens); t += 4) choose(a, t);
+  for (int t = t0 + wave; t < min(a.T, t0 + kRouteTokens); t += 4) {
+    if (a.E <= kWave) choose<1>(a, t);
+    else if (a.E <= 2 * kWave) choose<2>(a, t);
+    else choose<kMoeExperts / kWave>(a, t);
+  }
 }
 
 // ------------------------------------------------------------------ the experts
@@ -233,7 +264,7 @@ __device__ __forceinline__ int list_places(const MoeArgs& a, int e, uint16_t* li
 
 // Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.
 template <bool F32, bool VEC, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) {
+__global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a) {
   constexpr int E = F32 ? 4 : 8, U = 4, STEP = 4 * E * U;  // elements of a row that a wave takes at once
   __shared__ uint16_t list[kMoeTokens * kMoeK];
   __shared__ float red[4][2][4][kWave];
@@ -247,22 +278,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) 
 #pragma unroll
   for (int m = 0; m < 2; ++m)
     wb[m] = make_buf(static_cast<const char*>(a.w[m]) + ((size_t)e * a.d_ff + (rows > 0 ? row0 : 0)) * a.d * es,
-                     rows > 0 ? (uint32_t)rows * a.d * es : 0u);
+                     rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
   const Buf xb = make_buf(a.x, (uint32_t)a.T * a.d * es);
 
-  struct Batch {
-    uint4 w[U][2];
-  };
-  auto load = [&](int k0, Batch& b) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + (u * 4 + g) * E, left = n < rows ? a.d - k : 0;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) b.w[u][m] = ld_weight_chunk<F32, VEC>(wb[m], (uint32_t)n * a.d + k, left);
-    }
-  };
-  Batch first;
-  load(wave * STEP, first);
   const int cnt = list_places(a, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
@@ -271,11 +289,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) 
     for (int t = 0; t < NT; ++t) xo[t] = (uint32_t)(list[min(p0 + t * 16 + n, cnt - 1)] / a.k) * a.d;
     const int tiles = min(NT, (cnt - p0 + 15) / 16);
     f32x4_t acc[NT][2] = {};
-    Batch cur = first;
-    if (p0) load(wave * STEP, cur);
-    for (int k0 = wave * STEP; k0 < a.d; k0 += 4 * STEP) {
-      Batch nxt;
-      load(k0 + 4 * STEP, nxt);
+    // Rows' lines of 128 bytes come in two halves: through the caches (16 rows of 64 bytes a load: streamed past them 5.2
+    // TB/s, through them 5.6).  One step: 8 loads of weights and the tokens' in flight, and three or more other waves of the SIMD at theirs.  The
+    // last step of a row that is no whole steps (tail) loads zeros behind it; rows behind the last are behind the buffer.
+    auto step = [&](int k0, auto tail) {
+      uint4 w[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + (u * 4 + g) * E, left = tail.value ? a.d - k : E;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) w[u][m] = ld_chunk<F32, VEC>(wb[m], (uint32_t)n * a.d + k, VEC || n < rows ? left : 0);
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         if (t >= tiles) break;
@@ -283,7 +307,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int k = k0 + (u * 4 + g) * E;
-          x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, a.d - k);
+          x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, tail.value ? a.d - k : E);
         }
         f32x4_t s[2] = {};
 #pragma unroll
@@ -291,18 +315,27 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_hidden(MoeArgs a) 
 #pragma unroll
           for (int m = 0; m < 2; ++m) {
             if constexpr (F32) {
-              s[m] = mfma16f(comp<0>(x[u]), comp<0>(cur.w[u][m]), s[m]);
-              s[m] = mfma16f(comp<1>(x[u]), comp<1>(cur.w[u][m]), s[m]);
-              s[m] = mfma16f(comp<2>(x[u]), comp<2>(cur.w[u][m]), s[m]);
-              s[m] = mfma16f(comp<3>(x[u]), comp<3>(cur.w[u][m]), s[m]);
+              s[m] = mfma16f(comp<0>(x[u]), comp<0>(w[u][m]), s[m]);
+              s[m] = mfma16f(comp<1>(x[u]), comp<1>(w[u][m]), s[m]);
+              s[m] = mfma16f(comp<2>(x[u]), comp<2>(w[u][m]), s[m]);
+              s[m] = mfma16f(comp<3>(x[u]), comp<3>(w[u][m]), s[m]);
             } else {
-              s[m] = mfma16(bf8(x[u]), bf8(cur.w[u][m]), s[m]);
+              s[m] = mfma16(bf8(x[u]), bf8(w[u][m]), s[m]);
             }
           }
         acc[t][0] += s[0];
         acc[t][1] += s[1];
       }
-      cur = nxt;
+    };
+    // The workgroups go through the rows from different places on: with rows of 2^n bytes all of them would be on the
+    // same few memory channels at any time (rows of 4096 bytes: 4.3 TB/s, so 5.25).
+    const int turns = (a.d + 4 * STEP - 1) / (4 * STEP);
+    int turn = (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)turns);
+    for (int i = 0; i < turns; ++i) {
+      const int k0 = (turn * 4 + wave) * STEP;
+      turn = turn + 1 == turns ? 0 : turn + 1;
+      if (k0 + STEP <= a.d) step(k0, Int<0>{});
+      else if (k0 < a.d) step(k0, Int<1>{});
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -336,7 +369,7 @@ constexpr int down_columns() {
 
 // Four waves take turns at the piece's neurons, 32 at once: a lane has 16 bytes of 8 neurons' rows.
 template <bool F32, bool VEC, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
   constexpr int E = F32 ? 4 : 8, COLS = down_columns<F32>();
   __shared__ uint16_t list[kMoeTokens * kMoeK];
   __shared__ float red[4][E][4][kWave];
@@ -349,20 +382,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   const int steps = a.ldz / 32, s0 = (int)((int64_t)steps * blockIdx.z / a.pieces), s1 = (int)((int64_t)steps * (blockIdx.z + 1) / a.pieces);
   const size_t es = F32 ? 4 : 2;
   const Buf zb = make_buf(a.z, (uint32_t)a.T * a.k * a.ldz * es);
+  const uint32_t vo = col < a.d ? (uint32_t)((g * 8 * (size_t)a.d + col) * es) : kOOB;
   const char* wbase = static_cast<const char*>(a.w[2]) + (size_t)e * a.d_ff * a.d * es;
 
-  struct Batch {
-    uint4 w[8];
-  };
-  auto load = [&](int s, Batch& b) {
-    const int r0 = min(s, s1 - 1) * 32, rows = s < s1 ? min(32, a.d_ff - r0) : 0;
-    const Buf wb = make_buf(wbase + (size_t)r0 * a.d * es, rows > 0 ? (uint32_t)rows * a.d * es : 0u);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      b.w[j] = ld_weight_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
-  };
-  Batch first;
-  load(s0 + wave, first);
   const int cnt = list_places(a, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
@@ -371,11 +393,16 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
     for (int t = 0; t < NT; ++t) zo[t] = (uint32_t)list[min(p0 + t * 16 + n, cnt - 1)] * a.ldz;
     const int tiles = min(NT, (cnt - p0 + 15) / 16);
     f32x4_t acc[NT][E] = {};
-    Batch cur = first;
-    if (p0) load(s0 + wave, cur);
     for (int s = s0 + wave; s < s1; s += 4) {
-      Batch nxt;
-      load(s + 4, nxt);
+      // rows behind the last are behind the buffer
+      const int rows = min(32, a.d_ff - s * 32);
+      const Buf wb = make_buf(wbase + (size_t)s * 32 * a.d * es, rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
+      uint4 w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (VEC) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
+        else w[j] = ld_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
+      }
       uint4 b[E];
       if constexpr (!F32) {
         // column 2q (and 2q + 1) of neurons 2p, 2p + 1: the low (high) halves of dword q of both rows
@@ -384,7 +411,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
           uint32_t lo[4], hi[4];
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            const uint4 &r0 = cur.w[2 * p], &r1 = cur.w[2 * p + 1];
+            const uint4 &r0 = w[2 * p], &r1 = w[2 * p + 1];
             const uint32_t d0 = q == 0 ? r0.x : q == 1 ? r0.y : q == 2 ? r0.z : r0.w;
             const uint32_t d1 = q == 0 ? r1.x : q == 1 ? r1.y : q == 2 ? r1.z : r1.w;
             lo[p] = __builtin_amdgcn_perm(d1, d0, 0x05040100u);
@@ -405,10 +432,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
           f32x4_t sum[E] = {};
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            sum[0] = mfma16f(z[j], comp<0>(cur.w[j]), sum[0]);
-            sum[1] = mfma16f(z[j], comp<1>(cur.w[j]), sum[1]);
-            sum[2] = mfma16f(z[j], comp<2>(cur.w[j]), sum[2]);
-            sum[3] = mfma16f(z[j], comp<3>(cur.w[j]), sum[3]);
+            sum[0] = mfma16f(z[j], comp<0>(w[j]), sum[0]);
+            sum[1] = mfma16f(z[j], comp<1>(w[j]), sum[1]);
+            sum[2] = mfma16f(z[j], comp<2>(w[j]), sum[2]);
+            sum[3] = mfma16f(z[j], comp<3>(w[j]), sum[3]);
           }
 #pragma unroll
           for (int c = 0; c < E; ++c) acc[t][c] += sum[c];
@@ -417,7 +444,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
           for (int c = 0; c < E; ++c) acc[t][c] = mfma16(bf8(z0), bf8(b[c]), acc[t][c]);
         }
       }
-      cur = nxt;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -441,24 +467,30 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   }
 }
 
+// 64 columns of a token to a workgroup; four waves take turns at its places' pieces.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_moe_join(MoeArgs a) {
-  const int t = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.d) return;
+  __shared__ float red[4][kWave];
+  const int t = blockIdx.y, wave = uniform(threadIdx.x >> 6), lane = lane_id(), c = blockIdx.x * kWave + lane;
+  const size_t rows = (size_t)a.T * a.k;
   float y = 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    const int p = t * a.k + j, e = a.ids[p];
-    if (e < 0 || e >= a.E) continue;
-    float v = 0.f;
-    for (int s = 0; s < a.pieces; ++s) v += a.part[((size_t)s * a.T * a.k + p) * a.d + c];
-    y += a.weights[p] * v;
+  for (int j = wave; j < a.k; j += 4) {
+    const int p = t * a.k + j, e = uniform(a.ids[p]);
+    if (e < 0 || e >= a.E || c >= a.d) continue;
+    const float w = a.weights[p];
+    float v[kPiecesMost];
+#pragma unroll
+    for (int s = 0; s < kPiecesMost; ++s) v[s] = s < a.pieces ? a.part[(s * rows + p) * a.d + c] : 0.f;
+#pragma unroll
+    for (int s = 1; s < kPiecesMost; ++s) v[0] += v[s];
+    y += w * v[0];
   }
-  store_as<F32>(a.y, (size_t)t * a.d + c, y);
+  red[wave][lane] = y;
+  __syncthreads();
+  if (wave == 0 && c < a.d) store_as<F32>(a.y, (size_t)t * a.d + c, (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]));
 }
 
 // ------------------------------------------------------------------ host side
-constexpr int kPiecesMost = 8;
-
 int moe_slots(int T, int E, int k) { return std::min(T * k, E); }
 int moe_ldz(int d_ff) { return ceil_div(d_ff, 32) * 32; }
 // Pieces of the neurons: enough workgroups for the card, each with a step of 32 for every wave.
@@ -508,14 +540,18 @@ hipError_t launch_experts(const MoeArgs& a, hipStream_t st) {
   if (const hipError_t e = hipGetLastError()) return e;
   k_moe_down<F32, VEC, NT><<<dim3(ceil_div(a.d, down_columns<F32>()), a.slots, a.pieces), 256, 0, st>>>(a);
   if (const hipError_t e = hipGetLastError()) return e;
-  k_moe_join<F32><<<dim3(ceil_div(a.d, 256), a.T), 256, 0, st>>>(a);
+  k_moe_join<F32><<<dim3(ceil_div(a.d, kWave), a.T), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 template <bool F32, bool VEC>
 hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
   if (r.w)
     if (const hipError_t e = launch_route<F32, VEC>(r, st)) return e;
-  return a.T <= 16 ? launch_experts<F32, VEC, 1>(a, st) : launch_experts<F32, VEC, 4>(a, st);
+  // An expert of more tokens than the tiles hold reads its weights again.  With every choice as likely, that is one in
+  // two hundred experts of a mean of 8 tokens and 16 a pass, and fewer with 20 and 32.
+  const int tokens = a.T * a.k;
+  if (a.T <= 16 || tokens <= 8 * a.E) return launch_experts<F32, VEC, 1>(a, st);
+  return a.T <= 32 || tokens <= 20 * a.E ? launch_experts<F32, VEC, 2>(a, st) : launch_experts<F32, VEC, 4>(a, st);
 }
 
 }  // namespace
