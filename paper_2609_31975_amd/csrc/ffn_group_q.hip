@@ -29,7 +29,7 @@ GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out) {
     // Few tokens: all workgroups at once on the card, two to a CU, rather than rounds of them.
     const int tiles = ceil_div(n_out, 16);
     p.wk = tiles <= 512 ? 8 : tiles <= 1024 ? 4 : 2;
-    p.u = p.nt ? gq_batch(gated, p.ns) : gq_batch1(gated);
+    p.u = p.nt ? gq_batch(gated, p.ns) : 1;
     p.whole = share();
     if (p.whole) return p;
     if (!p.nt) {

@@ -34,9 +34,8 @@ struct GqArgs {
 };
 
 // Windows of a wave in a batch, where the next batch's registers fit beside it.
-constexpr int gq_batch(bool gated, int ns) { return (ns > 1 ? 2 : 4) / (gated ? 2 : 1); }
+constexpr int gq_batch(bool gated, int ns) { return gated || ns > 1 ? 1 : 2; }
 
-constexpr int gq_batch1(bool gated) { return gated ? 1 : 2; }  // of one token
 
 // Waves that share a row tile's windows with two tiles of tokens and more
 constexpr int kGqWaves = 2;

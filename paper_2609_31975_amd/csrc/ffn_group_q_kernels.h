@@ -224,8 +224,8 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
   // would be on the same few memory channels at any time (rows of 4096 bytes: 4.3 TB/s, so 5.25).
   const int batches = (last - first + UNIT - 1) / UNIT;
   int turn = WHOLE ? (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)batches) : 0;
-  Batch cur;
-  load(first + turn * UNIT, cur);
+  Batch even, odd;
+  load(first + turn * UNIT, even);
   using Pieces = std::conditional_t<NT == 1, XPieces<XF32, NS, 16>, XCopy<XF32, NS, NT, WK>>;
   Pieces xp;
   xp.load(a, first, 0);
@@ -240,10 +240,9 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
     }
     __syncthreads();
     if (!WHOLE && c0 + a.chunk < last) xp.load(a, c0 + a.chunk, 0);
-    for (int b0 = 0; b0 < min(a.chunk, last - c0); b0 += UNIT) {
+    auto products = [&](const Batch& cur, Batch& nxt) {
       const int here = first + turn * UNIT - c0;  // a window of the chunk
       turn = turn + 1 == batches ? 0 : turn + 1;
-      Batch nxt;
       load(first + turn * UNIT, nxt);
       issue_barrier();
 #pragma unroll
@@ -291,10 +290,21 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
             }
           }
           // operands of one f at a time: more of them in registers spill
-          if constexpr (NT > 1) issue_barrier();
+          if constexpr (NT > 1 || (GATED && NS == 4)) issue_barrier();
         }
       }
-      cur = nxt;
+    };
+    // two batches that take turns: a copy of one to the other would wait for it
+    int left = (min(a.chunk, last - c0) + UNIT - 1) / UNIT;
+    if constexpr (NT == 1) {
+      for (; left >= 2; left -= 2) {
+        products(even, odd);
+        products(odd, even);
+      }
+    }
+    if (left) {  // all there is of a chunk with more than one token tile
+      products(even, odd);
+      even = odd;
     }
   }
 
@@ -330,9 +340,9 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
 // One token.  A load takes 128 bytes of 8 rows (whole lines, streamed past the caches), 32 codes a lane, and those lie in
 // one group whatever it is; a wave takes 16 rows, two loads, of 256 columns (a window here).  A lane's products with its
 // 32 x are 16 v_dot2; 8 lanes share a row.  x in LDS: piece f (8 columns) of a window's 8 lanes side by side.
-template <bool XF32, bool SF32, bool GATED, bool OFF, int WK, int U>
+template <bool XF32, bool SF32, bool GATED, bool OFF, int WK>
 __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
-  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK * U, WIN = 2 * kWindow;
+  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK, WIN = 2 * kWindow;
   typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
   extern __shared__ __align__(16) char lds[];
   const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), c = lane & 7, wk = wave % WK;
@@ -354,8 +364,8 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
     ob[m] = make_buf(a.w[m].offsets, a.w[m].offsets ? (uint32_t)a.n_out * a.groups * ss : 0u);
   }
   struct Batch {
-    uint4 codes[U][2][M];
-    uint32_t sc[U][2][M], of[OFF ? U : 1][2][M];
+    uint4 codes[2][M];
+    uint32_t sc[2][M], of[2][M];
   };
   auto raw = [&](const Buf& b, uint32_t i) -> uint32_t {
     if constexpr (SF32) return (uint32_t)ldb32(b, i);
@@ -364,20 +374,17 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
   auto value = [](uint32_t v) { return __uint_as_float(SF32 ? v : v << 16); };
   // codes and scales behind a row's or the share's end: as in k_group_q
   auto load = [&](int w_first, Batch& b) {
+    const int w = w_first + wk;
+    const uint32_t k32 = w * 8 + c, gi = __umulhi(2 * k32, a.div_group);
+    const uint32_t at = w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int w = w_first + wk * U + u;
-      const uint32_t k32 = w * 8 + c, gi = __umulhi(2 * k32, a.div_group);
-      const uint32_t at = w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB;
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-          b.codes[u][s][m] = ldb_nt(cb[m], code_at[s] + w * (WIN / 2));
-          b.sc[u][s][m] = raw(sb[m], scale_at[s] + at);
-          if constexpr (OFF) b.of[u][s][m] = raw(ob[m], scale_at[s] + at);
-        }
-    }
+      for (int m = 0; m < M; ++m) {
+        b.codes[s][m] = ldb_nt(cb[m], code_at[s] + w * (WIN / 2));
+        b.sc[s][m] = raw(sb[m], scale_at[s] + at);
+        if constexpr (OFF) b.of[s][m] = raw(ob[m], scale_at[s] + at);
+      }
   };
 
   float acc[2][M] = {};
@@ -389,8 +396,8 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
   // the workgroups start at different places of the rows: as in k_group_q
   const int batches = (last - first + UNIT - 1) / UNIT;
   int turn = last - first <= a.chunk ? (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)batches) : 0;
-  Batch cur;
-  load(first + turn * UNIT, cur);
+  Batch even, odd;
+  load(first + turn * UNIT, even);
   for (int c0 = first; c0 < last; c0 += a.chunk) {
     if (c0 != first) __syncthreads();
     for (int i = threadIdx.x; i < a.chunk * (WIN / 8); i += 512) {
@@ -406,45 +413,50 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
       if ((i & 3) == 0) tab[i >> 2] = -24.f * s;
     }
     __syncthreads();
-    for (int b0 = 0; b0 < min(a.chunk, last - c0); b0 += UNIT) {
+    auto products = [&](const Batch& cur, Batch& nxt) {
       const int here = first + turn * UNIT - c0;  // a window of the chunk
       turn = turn + 1 == batches ? 0 : turn + 1;
-      Batch nxt;
       load(first + turn * UNIT, nxt);
       issue_barrier();
+      const int w = here + wk;  // the chunk is a multiple of WK
+      const float gone = tab[w * 8 + c];
+      uint4 x[P][4];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int w = here + wk * U + u;  // the chunk is a multiple of UNIT
-        const float gone = tab[w * 8 + c];
-        uint4 x[P][4];
+      for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int f = 0; f < 4; ++f) x[p][f] = *reinterpret_cast<const uint4*>(lds + p * plane + w * (WIN * 2) + f * 128 + c * 16);
 #pragma unroll
-          for (int f = 0; f < 4; ++f) x[p][f] = *reinterpret_cast<const uint4*>(lds + p * plane + w * (WIN * 2) + f * 128 + c * 16);
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int m = 0; m < M; ++m) {
+          const uint4 q = cur.codes[s][m];
+          const uint4 d[4] = {codes8(q.x, mask), codes8(q.y, mask), codes8(q.z, mask), codes8(q.w, mask)};
+          float sum = gone;
 #pragma unroll
-          for (int m = 0; m < M; ++m) {
-            const uint4 q = cur.codes[u][s][m];
-            const uint4 d[4] = {codes8(q.x, mask), codes8(q.y, mask), codes8(q.z, mask), codes8(q.w, mask)};
-            float sum = gone;
+          for (int p = P - 1; p >= 0; --p)
 #pragma unroll
-            for (int p = P - 1; p >= 0; --p)
-#pragma unroll
-              for (int f = 0; f < 4; ++f) {
-                auto dot = [&](uint32_t l, uint32_t r) {
-                  sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, l), __builtin_bit_cast(bf16x2_t, r), sum, false);
-                };
-                dot(d[f].x, x[p][f].x);
-                dot(d[f].y, x[p][f].y);
-                dot(d[f].z, x[p][f].z);
-                dot(d[f].w, x[p][f].w);
-              }
-            acc[s][m] += value(cur.sc[u][s][m]) * sum;
-            if constexpr (OFF) acc[s][m] += value(cur.of[u][s][m]) * (gone * (-1.f / 24.f));
-          }
-      }
-      cur = nxt;
+            for (int f = 0; f < 4; ++f) {
+              auto dot = [&](uint32_t l, uint32_t r) {
+                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, l), __builtin_bit_cast(bf16x2_t, r), sum, false);
+              };
+              dot(d[f].x, x[p][f].x);
+              dot(d[f].y, x[p][f].y);
+              dot(d[f].z, x[p][f].z);
+              dot(d[f].w, x[p][f].w);
+            }
+          acc[s][m] += value(cur.sc[s][m]) * sum;
+          if constexpr (OFF) acc[s][m] += value(cur.of[s][m]) * (gone * (-1.f / 24.f));
+        }
+    };
+    // two batches that take turns: a copy of one to the other would wait for it
+    int left = (min(a.chunk, last - c0) + UNIT - 1) / UNIT;
+    for (; left >= 2; left -= 2) {
+      products(even, odd);
+      products(odd, even);
+    }
+    if (left) {
+      products(even, odd);
+      even = odd;
     }
   }
 
@@ -494,10 +506,9 @@ __global__ __launch_bounds__(256) void k_group_q_join(GqArgs a, int shares) {
 
 template <bool XF32, bool SF32, bool GATED, bool OFF>
 hipError_t launch_one(const GqArgs& a, const GqPlan& p, hipStream_t st) {
-  constexpr int U = gq_batch1(GATED);
   const dim3 grid(p.blocks, p.shares);
   auto go = [&](auto wk) {
-    k_group_q1<XF32, SF32, GATED, OFF, wk.value, U><<<grid, 512, gq_lds(XF32, p, 1), st>>>(a);
+    k_group_q1<XF32, SF32, GATED, OFF, wk.value><<<grid, 512, gq_lds(XF32, p, 1), st>>>(a);
     return hipGetLastError();
   };
   return p.wk == 8 ? go(Int<8>{}) : p.wk == 4 ? go(Int<4>{}) : go(Int<2>{});
