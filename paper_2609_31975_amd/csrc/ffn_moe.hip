@@ -1,7 +1,9 @@
 // include/ffn_moe.h: a mixture-of-experts layer for a decode step's tokens.
 //
 // The chosen experts' three matrices are read once (for up to 64 tokens of an expert) and bound it.  Launches:
-//   1. k_moe_route   logits in 64 bits, a wave to an expert; the last workgroup of 8 tokens chooses for them
+//   1. k_moe_logits  the router's products in 64 bits, a wave to an expert
+//      k_moe_choose  the choice, a wave to a token; up to 4 tokens' is made by every workgroup of k_moe_hidden instead (a
+//                    launch less)
 //   2. k_moe_hidden  z = A(x W1^T - t) U(x W3^T), 16 hidden neurons of an expert to a workgroup
 //   3. k_moe_down    z W2 in pieces of neurons, 16-byte columns x 16 lanes of an expert to a workgroup
 //   4. k_moe_join    the pieces and the experts, weighted, in a fixed order
@@ -21,8 +23,8 @@ namespace {
 
 constexpr int kMoeTokens = 256, kMoeK = 16, kMoeExperts = 512;
 constexpr int kPiecesMost = 8;   // of an expert's neurons
-constexpr int kRouteTokens = 8;  // tokens that choose together
-constexpr int kMoeCounters = kMoeTokens / kRouteTokens;
+constexpr int kRouteTokens = 8;  // tokens of a wave that computes logits
+constexpr int kChooseTokens = 4; // tokens that k_moe_hidden chooses for itself: a wave each
 
 struct RouteArgs {
   int T, d, E, k;
@@ -31,7 +33,6 @@ struct RouteArgs {
   int sigmoid, normalize;
   float scale;
   double* logits;  // [T][E]
-  int* arrived;    // one for each kRouteTokens; zero between calls
   int32_t* ids;
   float* weights;
 };
@@ -50,10 +51,11 @@ struct MoeArgs {
 };
 
 // A 16-byte chunk's worth of elements from element i on, `left` of them there: one load, or narrower ones.
-template <bool F32, bool VEC>
+template <bool F32, bool VEC, bool STREAM = false>
 __device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
   if constexpr (VEC) {
-    return ldb(b, left > 0 ? i * (F32 ? 4u : 2u) : kOOB);
+    const uint32_t o = left > 0 ? i * (F32 ? 4u : 2u) : kOOB;
+    return STREAM ? ldb_nt(b, o) : ldb(b, o);
   } else if constexpr (F32) {
     return make_uint4(ldb32(b, left > 0 ? i * 4 : kOOB), ldb32(b, left > 1 ? i * 4 + 4 : kOOB),
                       ldb32(b, left > 2 ? i * 4 + 8 : kOOB), ldb32(b, left > 3 ? i * 4 + 12 : kOOB));
@@ -96,9 +98,14 @@ __device__ __forceinline__ double wave_max64(double v) {
   return wave_join64(v, [](double a, double b) { return b > a ? b : a; });
 }
 
-// The choice of one token, by one wave.  A lane has the scores of experts lane, 64 + lane, ... (N of them).
+// The choice of one token, by one wave: k of lanes 0 ... k - 1.  A lane has the scores of experts lane, 64 + lane, ...
+// (N of them).
+struct Chosen {
+  int id;
+  float weight;
+};
 template <int N>
-__device__ __forceinline__ void choose(const RouteArgs& a, int tok) {
+__device__ __forceinline__ Chosen choose_of(const RouteArgs& a, int tok) {
   const int lane = lane_id();
   double score[N], key[N];
 #pragma unroll
@@ -159,20 +166,29 @@ __device__ __forceinline__ void choose(const RouteArgs& a, int tok) {
       mine_e = at * kWave + from;
     }
   }
-  if (lane < a.k) {
-    a.ids[(size_t)tok * a.k + lane] = mine_e;
-    a.weights[(size_t)tok * a.k + lane] = (float)((double)a.scale * (a.normalize ? mine / sum : mine));
+  return Chosen{mine_e, (float)((double)a.scale * (a.normalize ? mine / sum : mine))};
+}
+__device__ __forceinline__ Chosen choose(const RouteArgs& a, int tok) {
+  if (a.E <= kWave) return choose_of<1>(a, tok);
+  if (a.E <= 2 * kWave) return choose_of<2>(a, tok);
+  return choose_of<kMoeExperts / kWave>(a, tok);
+}
+__device__ __forceinline__ void put_choice(const RouteArgs& a, int tok, const Chosen& c) {
+  if (lane_id() < a.k) {
+    a.ids[(size_t)tok * a.k + lane_id()] = c.id;
+    a.weights[(size_t)tok * a.k + lane_id()] = c.weight;
   }
 }
+__global__ __launch_bounds__(64) void k_moe_choose(RouteArgs a) { put_choice(a, blockIdx.x, choose(a, blockIdx.x)); }
 
 // A wave takes one expert's logits of NT tokens.
 template <bool F32, bool VEC, int NT>
-__global__ __launch_bounds__(256) void k_moe_route(RouteArgs a) {
+__global__ __launch_bounds__(256) void k_moe_logits(RouteArgs a) {
   constexpr int E = F32 ? 4 : 8;
-  __shared__ int s_last;
-  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), e = blockIdx.x * 4 + wave, t0 = blockIdx.y * kRouteTokens;
+  const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), e = blockIdx.x * 4 + wave, t0 = blockIdx.y * NT;
   const int nt = min(a.T - t0, NT);
-  if (e < a.E) {
+  if (e >= a.E) return;
+  {
     const size_t es = F32 ? 4 : 2;
     const Buf wb = make_buf(static_cast<const char*>(a.w) + (size_t)e * a.d * es, a.d * (uint32_t)es);
     const Buf xb = make_buf(static_cast<const char*>(a.x) + (size_t)t0 * a.d * es, nt * a.d * (uint32_t)es);
@@ -208,37 +224,22 @@ __global__ __launch_bounds__(256) void k_moe_route(RouteArgs a) {
       if (lane == 0 && t < nt) a.logits[(size_t)(t0 + t) * a.E + e] = v;
     }
   }
-  // The last workgroup of these tokens has all their logits before it; it leaves the counter at zero.
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s_last = atomicAdd(&a.arrived[blockIdx.y], 1) == (int)gridDim.x - 1;
-    if (s_last) a.arrived[blockIdx.y] = 0;
-  }
-  __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  for (int t = t0 + wave; t < min(a.T, t0 + kRouteTokens); t += 4) {
-    if (a.E <= kWave) choose<1>(a, t);
-    else if (a.E <= 2 * kWave) choose<2>(a, t);
-    else choose<kMoeExperts / kWave>(a, t);
-  }
 }
 
 // ------------------------------------------------------------------ the experts
 // The expert of a slot, or -1.  With a slot a place, a place whose expert an earlier one names has no work.
-__device__ __forceinline__ int slot_expert(const MoeArgs& a, int slot) {
+__device__ __forceinline__ int slot_expert(const MoeArgs& a, const int32_t* ids, int slot) {
   if (a.slots == a.E && a.slots != a.T * a.k) return slot;
-  const int e = uniform(a.ids[slot]);
+  const int e = uniform(ids[slot]);
   if (e < 0 || e >= a.E) return -1;
   for (int b = 0; b < slot; b += kWave) {
     const int at = b + lane_id();
-    if (__ballot(at < slot && a.ids[at] == e)) return -1;
+    if (__ballot(at < slot && ids[at] == e)) return -1;
   }
   return e;
 }
 // The places of expert e, in order, into list; every wave calls it and gets their number.
-__device__ __forceinline__ int list_places(const MoeArgs& a, int e, uint16_t* list, int* count) {
+__device__ __forceinline__ int list_places(const MoeArgs& a, const int32_t* ids, int e, uint16_t* list, int* count) {
   if (threadIdx.x < kWave) {
     const int n = a.T * a.k;
     int have = 0;
@@ -247,7 +248,7 @@ __device__ __forceinline__ int list_places(const MoeArgs& a, int e, uint16_t* li
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int at = b + j * kWave + lane_id();
-        id[j] = at < n ? a.ids[at] : -1;
+        id[j] = at < n ? ids[at] : -1;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -262,16 +263,41 @@ __device__ __forceinline__ int list_places(const MoeArgs& a, int e, uint16_t* li
   return uniform(*count);
 }
 
-// Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.
-template <bool F32, bool VEC, int NT>
-__global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a) {
+// Lanes 8 apart exchange halves: a keeps its own in lanes n < 8 and gets b's of lane n - 8 in the others; b the other way round.
+__device__ __forceinline__ void exchange8(uint4& a, uint4& b) {
+  auto one = [](uint32_t& x, uint32_t& y) {  // 0x128: row_ror:8, written in the upper or the lower 8 lanes of each 16
+    const uint32_t u = __builtin_amdgcn_update_dpp((int)x, (int)y, 0x128, 0xF, 0xC, false);
+    y = __builtin_amdgcn_update_dpp((int)y, (int)x, 0x128, 0xF, 0x3, false);
+    x = u;
+  };
+  one(a.x, b.x);
+  one(a.y, b.y);
+  one(a.z, b.z);
+  one(a.w, b.w);
+}
+
+// Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.  CHOOSE: the
+// tokens' choice is made here, from the logits.
+template <bool F32, bool VEC, int NT, bool CHOOSE>
+__global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) {
   constexpr int E = F32 ? 4 : 8, U = 4, STEP = 4 * E * U;  // elements of a row that a wave takes at once
-  __shared__ uint16_t list[kMoeTokens * kMoeK];
+  __shared__ uint16_t list[CHOOSE ? kChooseTokens * kMoeK : kMoeTokens * kMoeK];
   __shared__ float red[4][2][4][kWave];
+  __shared__ int32_t chosen[CHOOSE ? kChooseTokens * kMoeK : 1];
   __shared__ int count;
-  const int e = slot_expert(a, blockIdx.y);
-  if (e < 0) return;
   const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int32_t* ids = a.ids;
+  if constexpr (CHOOSE) {
+    if (wave < a.T) {
+      const Chosen c = choose(route, wave);
+      if (lane < a.k) chosen[wave * a.k + lane] = c.id;
+      if (blockIdx.x == 0 && blockIdx.y == 0) put_choice(route, wave, c);
+    }
+    __syncthreads();
+    ids = chosen;
+  }
+  const int e = slot_expert(a, ids, blockIdx.y);
+  if (e < 0) return;
   const int row0 = blockIdx.x * 16, rows = min(16, a.d_ff - row0);
   const size_t es = F32 ? 4 : 2;
   Buf wb[2];
@@ -280,8 +306,7 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a) {
     wb[m] = make_buf(static_cast<const char*>(a.w[m]) + ((size_t)e * a.d_ff + (rows > 0 ? row0 : 0)) * a.d * es,
                      rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
   const Buf xb = make_buf(a.x, (uint32_t)a.T * a.d * es);
-
-  const int cnt = list_places(a, e, list, &count);
+  const int cnt = list_places(a, ids, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
     uint32_t xo[NT];  // a token's row: tokens past the last one repeat it, and are not stored
@@ -289,16 +314,24 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a) {
     for (int t = 0; t < NT; ++t) xo[t] = (uint32_t)(list[min(p0 + t * 16 + n, cnt - 1)] / a.k) * a.d;
     const int tiles = min(NT, (cnt - p0 + 15) / 16);
     f32x4_t acc[NT][2] = {};
-    // Rows' lines of 128 bytes come in two halves: through the caches (16 rows of 64 bytes a load: streamed past them 5.2
-    // TB/s, through them 5.6).  One step: 8 loads of weights and the tokens' in flight, and three or more other waves of the SIMD at theirs.  The
-    // last step of a row that is no whole steps (tail) loads zeros behind it; rows behind the last are behind the buffer.
+    // One step: 8 loads of weights and the tokens' in flight, and three or more other waves of the SIMD at theirs.  A load
+    // takes whole lines, 128 bytes of 8 rows, streamed past the caches (7.0 TB/s over 1.9 GB; 16 rows of 64 bytes, as the
+    // operands have them, 6.3 through the caches and less past them): lane (n, g) has chunk g + 4 (n / 8) of row n % 8, and
+    // of row n % 8 + 8 in a second load.  The operands' lanes (n, g) want row n's chunks g and 4 + g: lanes 8 apart exchange
+    // halves.  The last step of a row that is no whole steps (tail) loads zeros behind it; rows behind the last are behind
+    // the buffer.
     auto step = [&](int k0, auto tail) {
       uint4 w[U][2];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = k0 + (u * 4 + g) * E, left = tail.value ? a.d - k : E;
+      for (int q = 0; q < U; q += 2) {
+        const int k = k0 + (q * 4 + g + (n >> 3) * 4) * E, left = tail.value ? a.d - k : E;
 #pragma unroll
-        for (int m = 0; m < 2; ++m) w[u][m] = ld_chunk<F32, VEC>(wb[m], (uint32_t)n * a.d + k, VEC || n < rows ? left : 0);
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = (n & 7) + 8 * h;
+            w[q + h][m] = ld_chunk<F32, VEC, true>(wb[m], (uint32_t)r * a.d + k, VEC || r < rows ? left : 0);
+          }
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -308,6 +341,12 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a) {
         for (int u = 0; u < U; ++u) {
           const int k = k0 + (u * 4 + g) * E;
           x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, tail.value ? a.d - k : E);
+        }
+        if (t == 0) {
+#pragma unroll
+          for (int q = 0; q < U; q += 2)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) exchange8(w[q][m], w[q + 1][m]);
         }
         f32x4_t s[2] = {};
 #pragma unroll
@@ -374,7 +413,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
   __shared__ uint16_t list[kMoeTokens * kMoeK];
   __shared__ float red[4][E][4][kWave];
   __shared__ int count;
-  const int e = slot_expert(a, blockIdx.y);
+  const int e = slot_expert(a, a.ids, blockIdx.y);
   if (e < 0) return;
   const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int col = blockIdx.x * COLS + n * E;
@@ -385,7 +424,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
   const uint32_t vo = col < a.d ? (uint32_t)((g * 8 * (size_t)a.d + col) * es) : kOOB;
   const char* wbase = static_cast<const char*>(a.w[2]) + (size_t)e * a.d_ff * a.d * es;
 
-  const int cnt = list_places(a, e, list, &count);
+  const int cnt = list_places(a, a.ids, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
     uint32_t zo[NT];
@@ -501,16 +540,13 @@ int moe_pieces(bool f32, int T, int d, int d_ff, int E, int k) {
 }
 
 struct MoeWs {
-  int* arrived;
   double* logits;
   void* z;
   float* part;
 };
-// The counters come first, wherever a call's other regions lie.
 size_t moe_layout(bool f32, int T, int d, int d_ff, int E, int k, void* base, MoeWs* out) {
   Carver c{static_cast<char*>(base)};
   MoeWs w;
-  w.arrived = static_cast<int*>(c.take(sizeof(int) * kMoeCounters));
   w.logits = static_cast<double*>(c.take(sizeof(double) * T * E));
   w.z = c.take((size_t)(f32 ? 4 : 2) * T * k * moe_ldz(d_ff));
   w.part = static_cast<float*>(c.take(sizeof(float) * kPiecesMost * T * k * (size_t)d));
@@ -527,31 +563,38 @@ int check_moe_shape(int T, int d, int d_ff, int E, int k) {
   return FFN_OK;
 }
 
-template <bool F32, bool VEC>
-hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
-  const dim3 grid(ceil_div(a.E, 4), ceil_div(a.T, kRouteTokens));
-  if (a.T == 1) k_moe_route<F32, VEC, 1><<<grid, 256, 0, st>>>(a);
-  else k_moe_route<F32, VEC, kRouteTokens><<<grid, 256, 0, st>>>(a);
+template <bool F32, bool VEC, int NT, bool CHOOSE>
+hipError_t launch_hidden(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
+  k_moe_hidden<F32, VEC, NT, CHOOSE><<<dim3(a.ldz / 16, a.slots), 256, 0, st>>>(a, r);
   return hipGetLastError();
 }
 template <bool F32, bool VEC, int NT>
-hipError_t launch_experts(const MoeArgs& a, hipStream_t st) {
-  k_moe_hidden<F32, VEC, NT><<<dim3(a.ldz / 16, a.slots), 256, 0, st>>>(a);
-  if (const hipError_t e = hipGetLastError()) return e;
+hipError_t launch_experts(const RouteArgs& r, const MoeArgs& a, bool choose, hipStream_t st) {
+  hipError_t e;
+  if constexpr (NT == 1) e = choose ? launch_hidden<F32, VEC, 1, true>(r, a, st) : launch_hidden<F32, VEC, 1, false>(r, a, st);
+  else e = launch_hidden<F32, VEC, NT, false>(r, a, st);
+  if (e != hipSuccess) return e;
   k_moe_down<F32, VEC, NT><<<dim3(ceil_div(a.d, down_columns<F32>()), a.slots, a.pieces), 256, 0, st>>>(a);
-  if (const hipError_t e = hipGetLastError()) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   k_moe_join<F32><<<dim3(ceil_div(a.d, kWave), a.T), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 template <bool F32, bool VEC>
 hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
-  if (r.w)
-    if (const hipError_t e = launch_route<F32, VEC>(r, st)) return e;
+  const bool choose = r.w && a.T <= kChooseTokens;
+  if (r.w) {
+    // Waves of one token while there are few of them: 8 tokens of a wave save its expert's row 7 times, one after the
+    // other (8 experts, 16 tokens of 4096: 10.9 us, so MEAS).
+    if (a.T * a.E <= 4096) k_moe_logits<F32, VEC, 1><<<dim3(ceil_div(a.E, 4), a.T), 256, 0, st>>>(r);
+    else k_moe_logits<F32, VEC, kRouteTokens><<<dim3(ceil_div(a.E, 4), ceil_div(a.T, kRouteTokens)), 256, 0, st>>>(r);
+    if (!choose) k_moe_choose<<<a.T, kWave, 0, st>>>(r);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
   // An expert of more tokens than the tiles hold reads its weights again.  With every choice as likely, that is one in
   // two hundred experts of a mean of 8 tokens and 16 a pass, and fewer with 20 and 32.
   const int tokens = a.T * a.k;
-  if (a.T <= 16 || tokens <= 8 * a.E) return launch_experts<F32, VEC, 1>(a, st);
-  return a.T <= 32 || tokens <= 20 * a.E ? launch_experts<F32, VEC, 2>(a, st) : launch_experts<F32, VEC, 4>(a, st);
+  if (a.T <= 16 || tokens <= 8 * a.E) return launch_experts<F32, VEC, 1>(r, a, choose, st);
+  return a.T <= 32 || tokens <= 20 * a.E ? launch_experts<F32, VEC, 2>(r, a, false, st) : launch_experts<F32, VEC, 4>(r, a, false, st);
 }
 
 }  // namespace
@@ -587,7 +630,7 @@ int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t*
   if (ws_bytes < moe_layout(f32, T, d, d_ff, E, k, ws, &w)) return FFN_ERR_WORKSPACE;
 
   const RouteArgs r{T, d, E, k, x, router->w, router->bias, router->sigmoid, router->normalize, router->scale,
-                    w.logits, w.arrived, ids, weights};
+                    w.logits, ids, weights};
   const MoeArgs a{T, d, d_ff, E, k, moe_ldz(d_ff), moe_slots(T, E, k), moe_pieces(f32, T, d, d_ff, E, k),
                   x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, w.part, y};
   const bool vec = d % (f32 ? 4 : 8) == 0;
