@@ -50,12 +50,13 @@ struct MoeArgs {
   void* y;
 };
 
-// A 16-byte chunk's worth of elements from element i on, `left` of them there: one load, or narrower ones.
-template <bool F32, bool VEC, bool STREAM = false>
+// A 16-byte chunk's worth of elements from element i on, `left` of them there: one load, or narrower ones.  VEC: 2, rows are
+// whole lines of 128 bytes (weights are streamed past the caches); 1, whole chunks; 0, neither.
+template <bool F32, int VEC, bool WEIGHTS = false>
 __device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
   if constexpr (VEC) {
     const uint32_t o = left > 0 ? i * (F32 ? 4u : 2u) : kOOB;
-    return STREAM ? ldb_nt(b, o) : ldb(b, o);
+    return WEIGHTS && VEC == 2 ? ldb_nt(b, o) : ldb(b, o);
   } else if constexpr (F32) {
     return make_uint4(ldb32(b, left > 0 ? i * 4 : kOOB), ldb32(b, left > 1 ? i * 4 + 4 : kOOB),
                       ldb32(b, left > 2 ? i * 4 + 8 : kOOB), ldb32(b, left > 3 ? i * 4 + 12 : kOOB));
@@ -182,7 +183,7 @@ __device__ __forceinline__ void put_choice(const RouteArgs& a, int tok, const Ch
 __global__ __launch_bounds__(64) void k_moe_choose(RouteArgs a) { put_choice(a, blockIdx.x, choose(a, blockIdx.x)); }
 
 // A wave takes one expert's logits of NT tokens.
-template <bool F32, bool VEC, int NT>
+template <bool F32, int VEC, int NT>
 __global__ __launch_bounds__(256) void k_moe_logits(RouteArgs a) {
   constexpr int E = F32 ? 4 : 8;
   const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), e = blockIdx.x * 4 + wave, t0 = blockIdx.y * NT;
@@ -278,7 +279,7 @@ __device__ __forceinline__ void exchange8(uint4& a, uint4& b) {
 
 // Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.  CHOOSE: the
 // tokens' choice is made here, from the logits.
-template <bool F32, bool VEC, int NT, bool CHOOSE>
+template <bool F32, int VEC, int NT, bool CHOOSE>
 __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) {
   constexpr int E = F32 ? 4 : 8, U = 4, STEP = 4 * E * U;  // elements of a row that a wave takes at once
   __shared__ uint16_t list[CHOOSE ? kChooseTokens * kMoeK : kMoeTokens * kMoeK];
@@ -306,6 +307,30 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) 
     wb[m] = make_buf(static_cast<const char*>(a.w[m]) + ((size_t)e * a.d_ff + (rows > 0 ? row0 : 0)) * a.d * es,
                      rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
   const Buf xb = make_buf(a.x, (uint32_t)a.T * a.d * es);
+  // A load takes whole lines, 128 bytes of 8 rows, streamed past the caches where the rows are whole lines (7.0 TB/s over 1.9
+  // GB; 16 rows of 64 bytes, as the operands have them, 6.3 through the caches and less past them): lane (n, g) has chunk
+  // g + 4 (n / 8) of row n % 8, and of row n % 8 + 8 in a second load.  The operands' lanes (n, g) want row n's chunks g and
+  // 4 + g: lanes 8 apart exchange halves.  Columns behind a row's end are zeros; rows behind the last are behind the buffer.
+  uint4 w[U][2];
+  auto load = [&](int k0) {
+    if (k0 >= a.d) return;
+    const bool tail = k0 + STEP > a.d;
+#pragma unroll
+    for (int q = 0; q < U; q += 2) {
+      const int k = k0 + (q * 4 + g + (n >> 3) * 4) * E, left = tail ? a.d - k : E;
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = (n & 7) + 8 * h;
+          w[q + h][m] = ld_chunk<F32, VEC, true>(wb[m], (uint32_t)r * a.d + k, VEC || r < rows ? left : 0);
+        }
+    }
+  };
+  // The workgroups go through the rows from different places on: with rows of 2^n bytes all of them would be on the
+  // same few memory channels at any time (rows of 4096 bytes: 4.3 TB/s, so 5.25).
+  const int turns = (a.d + 4 * STEP - 1) / (4 * STEP), start = (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)turns);
+  load((start * 4 + wave) * STEP);
   const int cnt = list_places(a, ids, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
@@ -314,67 +339,48 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) 
     for (int t = 0; t < NT; ++t) xo[t] = (uint32_t)(list[min(p0 + t * 16 + n, cnt - 1)] / a.k) * a.d;
     const int tiles = min(NT, (cnt - p0 + 15) / 16);
     f32x4_t acc[NT][2] = {};
-    // One step: 8 loads of weights and the tokens' in flight, and three or more other waves of the SIMD at theirs.  A load
-    // takes whole lines, 128 bytes of 8 rows, streamed past the caches (7.0 TB/s over 1.9 GB; 16 rows of 64 bytes, as the
-    // operands have them, 6.3 through the caches and less past them): lane (n, g) has chunk g + 4 (n / 8) of row n % 8, and
-    // of row n % 8 + 8 in a second load.  The operands' lanes (n, g) want row n's chunks g and 4 + g: lanes 8 apart exchange
-    // halves.  The last step of a row that is no whole steps (tail) loads zeros behind it; rows behind the last are behind
-    // the buffer.
-    auto step = [&](int k0, auto tail) {
-      uint4 w[U][2];
-#pragma unroll
-      for (int q = 0; q < U; q += 2) {
-        const int k = k0 + (q * 4 + g + (n >> 3) * 4) * E, left = tail.value ? a.d - k : E;
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = (n & 7) + 8 * h;
-            w[q + h][m] = ld_chunk<F32, VEC, true>(wb[m], (uint32_t)r * a.d + k, VEC || r < rows ? left : 0);
-          }
-      }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (t >= tiles) break;
-        uint4 x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int k = k0 + (u * 4 + g) * E;
-          x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, tail.value ? a.d - k : E);
-        }
-        if (t == 0) {
-#pragma unroll
-          for (int q = 0; q < U; q += 2)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) exchange8(w[q][m], w[q + 1][m]);
-        }
-        f32x4_t s[2] = {};
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            if constexpr (F32) {
-              s[m] = mfma16f(comp<0>(x[u]), comp<0>(w[u][m]), s[m]);
-              s[m] = mfma16f(comp<1>(x[u]), comp<1>(w[u][m]), s[m]);
-              s[m] = mfma16f(comp<2>(x[u]), comp<2>(w[u][m]), s[m]);
-              s[m] = mfma16f(comp<3>(x[u]), comp<3>(w[u][m]), s[m]);
-            } else {
-              s[m] = mfma16(bf8(x[u]), bf8(w[u][m]), s[m]);
-            }
-          }
-        acc[t][0] += s[0];
-        acc[t][1] += s[1];
-      }
-    };
-    // The workgroups go through the rows from different places on: with rows of 2^n bytes all of them would be on the
-    // same few memory channels at any time (rows of 4096 bytes: 4.3 TB/s, so 5.25).
-    const int turns = (a.d + 4 * STEP - 1) / (4 * STEP);
-    int turn = (int)((blockIdx.x * 5 + (blockIdx.x >> 3)) % (uint32_t)turns);
+    int turn = start;
+    if (p0) load((start * 4 + wave) * STEP);
     for (int i = 0; i < turns; ++i) {
       const int k0 = (turn * 4 + wave) * STEP;
       turn = turn + 1 == turns ? 0 : turn + 1;
-      if (k0 + STEP <= a.d) step(k0, Int<0>{});
-      else if (k0 < a.d) step(k0, Int<1>{});
+      // 8 loads of weights in flight, and three or more other waves of the SIMD at theirs
+      if (k0 < a.d) {
+        const bool tail = k0 + STEP > a.d;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (t >= tiles) break;
+          uint4 x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int k = k0 + (u * 4 + g) * E;
+            x[u] = ld_chunk<F32, VEC>(xb, xo[t] + k, tail ? a.d - k : E);
+          }
+          if (t == 0) {
+#pragma unroll
+            for (int q = 0; q < U; q += 2)
+#pragma unroll
+              for (int m = 0; m < 2; ++m) exchange8(w[q][m], w[q + 1][m]);
+          }
+          f32x4_t s[2] = {};
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              if constexpr (F32) {
+                s[m] = mfma16f(comp<0>(x[u]), comp<0>(w[u][m]), s[m]);
+                s[m] = mfma16f(comp<1>(x[u]), comp<1>(w[u][m]), s[m]);
+                s[m] = mfma16f(comp<2>(x[u]), comp<2>(w[u][m]), s[m]);
+                s[m] = mfma16f(comp<3>(x[u]), comp<3>(w[u][m]), s[m]);
+              } else {
+                s[m] = mfma16(bf8(x[u]), bf8(w[u][m]), s[m]);
+              }
+            }
+          acc[t][0] += s[0];
+          acc[t][1] += s[1];
+        }
+      }
+      if (i + 1 < turns) load((turn * 4 + wave) * STEP);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -407,11 +413,11 @@ constexpr int down_columns() {
 }
 
 // Four waves take turns at the piece's neurons, 32 at once: a lane has 16 bytes of 8 neurons' rows.
-template <bool F32, bool VEC, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
+template <bool F32, int VEC, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   constexpr int E = F32 ? 4 : 8, COLS = down_columns<F32>();
   __shared__ uint16_t list[kMoeTokens * kMoeK];
-  __shared__ float red[4][E][4][kWave];
+  __shared__ float red[4][4][4][kWave];
   __shared__ int count;
   const int e = slot_expert(a, a.ids, blockIdx.y);
   if (e < 0) return;
@@ -424,6 +430,19 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
   const uint32_t vo = col < a.d ? (uint32_t)((g * 8 * (size_t)a.d + col) * es) : kOOB;
   const char* wbase = static_cast<const char*>(a.w[2]) + (size_t)e * a.d_ff * a.d * es;
 
+  uint4 w[8];
+  auto load = [&](int s) {
+    if (s >= s1) return;
+    // rows behind the last are behind the buffer
+    const int rows = min(32, a.d_ff - s * 32);
+    const Buf wb = make_buf(wbase + (size_t)s * 32 * a.d * es, rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (VEC != 0) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
+      else w[j] = ld_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
+    }
+  };
+  load(s0 + wave);
   const int cnt = list_places(a, a.ids, e, list, &count);
 
   for (int p0 = 0; p0 < cnt; p0 += 16 * NT) {
@@ -432,16 +451,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
     for (int t = 0; t < NT; ++t) zo[t] = (uint32_t)list[min(p0 + t * 16 + n, cnt - 1)] * a.ldz;
     const int tiles = min(NT, (cnt - p0 + 15) / 16);
     f32x4_t acc[NT][E] = {};
+    if (p0) load(s0 + wave);
     for (int s = s0 + wave; s < s1; s += 4) {
-      // rows behind the last are behind the buffer
-      const int rows = min(32, a.d_ff - s * 32);
-      const Buf wb = make_buf(wbase + (size_t)s * 32 * a.d * es, rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
-      uint4 w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (VEC) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
-        else w[j] = ld_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
-      }
       uint4 b[E];
       if constexpr (!F32) {
         // column 2q (and 2q + 1) of neurons 2p, 2p + 1: the low (high) halves of dword q of both rows
@@ -483,24 +494,30 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_moe_down(MoeArgs a) {
           for (int c = 0; c < E; ++c) acc[t][c] = mfma16(bf8(z0), bf8(b[c]), acc[t][c]);
         }
       }
+      load(s + 4);
     }
+    // The waves' sums joined, four of a lane's columns at a time; neighbouring threads have neighbouring columns
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       if (t >= tiles) break;
-      __syncthreads();
 #pragma unroll
-      for (int c = 0; c < E; ++c)
+      for (int h = 0; h < E / 4; ++h) {
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[wave][c][i][lane] = acc[t][c][i];
-      __syncthreads();
-      // E 16 columns and 16 places; neighbouring threads have neighbouring columns
-      for (int o = threadIdx.x; o < COLS * 16; o += 256) {
-        const int c = o % E, l16 = o / E % 16, tok = o / COLS, p = p0 + t * 16 + tok, at = blockIdx.x * COLS + o % COLS;
-        if (p >= cnt || at >= a.d) continue;
-        float v = 0.f;
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) v += red[w][c][tok & 3][(tok >> 2) * 16 + l16];
-        a.part[((size_t)blockIdx.z * a.T * a.k + list[p]) * a.d + at] = v;
+          for (int i = 0; i < 4; ++i) red[wave][c][i][lane] = acc[t][h * 4 + c][i];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = threadIdx.x & 3, l16 = threadIdx.x >> 2 & 15, tok = j * 4 + wave;
+          const int p = p0 + t * 16 + tok, at = blockIdx.x * COLS + l16 * E + h * 4 + c;
+          if (p >= cnt || at >= a.d) continue;
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v += red[w][c][tok & 3][(tok >> 2) * 16 + l16];
+          a.part[((size_t)blockIdx.z * a.T * a.k + list[p]) * a.d + at] = v;
+        }
       }
     }
   }
@@ -563,12 +580,12 @@ int check_moe_shape(int T, int d, int d_ff, int E, int k) {
   return FFN_OK;
 }
 
-template <bool F32, bool VEC, int NT, bool CHOOSE>
+template <bool F32, int VEC, int NT, bool CHOOSE>
 hipError_t launch_hidden(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
   k_moe_hidden<F32, VEC, NT, CHOOSE><<<dim3(a.ldz / 16, a.slots), 256, 0, st>>>(a, r);
   return hipGetLastError();
 }
-template <bool F32, bool VEC, int NT>
+template <bool F32, int VEC, int NT>
 hipError_t launch_experts(const RouteArgs& r, const MoeArgs& a, bool choose, hipStream_t st) {
   hipError_t e;
   if constexpr (NT == 1) e = choose ? launch_hidden<F32, VEC, 1, true>(r, a, st) : launch_hidden<F32, VEC, 1, false>(r, a, st);
@@ -579,7 +596,7 @@ hipError_t launch_experts(const RouteArgs& r, const MoeArgs& a, bool choose, hip
   k_moe_join<F32><<<dim3(ceil_div(a.d, kWave), a.T), 256, 0, st>>>(a);
   return hipGetLastError();
 }
-template <bool F32, bool VEC>
+template <bool F32, int VEC>
 hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
   const bool choose = r.w && a.T <= kChooseTokens;
   if (r.w) {
@@ -633,9 +650,12 @@ int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t*
                     w.logits, ids, weights};
   const MoeArgs a{T, d, d_ff, E, k, moe_ldz(d_ff), moe_slots(T, E, k), moe_pieces(f32, T, d, d_ff, E, k),
                   x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, w.part, y};
-  const bool vec = d % (f32 ? 4 : 8) == 0;
-  const hipError_t e = f32 ? (vec ? launch_moe<true, true>(r, a, stream) : launch_moe<true, false>(r, a, stream))
-                           : (vec ? launch_moe<false, true>(r, a, stream) : launch_moe<false, false>(r, a, stream));
+  // rows of whole lines, of whole chunks, of neither
+  const int vec = d % (f32 ? 32 : 64) == 0 ? 2 : d % (f32 ? 4 : 8) == 0 ? 1 : 0;
+  auto go = [&](auto f) {
+    return vec == 2 ? launch_moe<f.value, 2>(r, a, stream) : vec ? launch_moe<f.value, 1>(r, a, stream) : launch_moe<f.value, 0>(r, a, stream);
+  };
+  const hipError_t e = f32 ? go(Int<1>{}) : go(Int<0>{});
   return e == hipSuccess ? FFN_OK : FFN_ERR_HIP;
 }
 

@@ -31,22 +31,24 @@ struct Part {
   static constexpr int E = VEC ? (F32 ? 4 : 8) : 1, N = EPT / E;
   static __device__ __forceinline__ int at(int t, int i) { return (i * TPR + t) * E; }
 
-  static __device__ __forceinline__ void load(const void* p, int64_t row, int d, int t, float (&v)[EPT], float none = 0.f) {
+  template <bool STREAM = false>
+  static __device__ __forceinline__ void load(const void* p, int64_t row, int d, int t, float (&v)[EPT]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int e = at(t, i);
       const bool on = e < d;
       const int64_t o = row * d + (on ? e : 0);
       if constexpr (VEC) {
-        uint4 c = *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + o * (F32 ? 4 : 2));
+        const uint4* at = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + o * (F32 ? 4 : 2));
+        const uint4 c = STREAM ? ld_weights(at) : *at;
         float u[E];
         if constexpr (F32) unpack(WF32{}, c, u);
         else unpack(WBf16{}, c, u);
 #pragma unroll
-        for (int j = 0; j < E; ++j) v[i * E + j] = on ? u[j] : none;
+        for (int j = 0; j < E; ++j) v[i * E + j] = on ? u[j] : 0.f;
       } else {
         const float u = F32 ? static_cast<const float*>(p)[o] : bf_to_f(static_cast<const uint16_t*>(p)[o]);
-        v[i] = on ? u : none;
+        v[i] = on ? u : 0.f;
       }
     }
   }
@@ -87,7 +89,8 @@ __device__ __forceinline__ float row_sum(float v, float* room) {
   return s;
 }
 
-template <bool F32, int TPR, int EPT, bool VEC>
+// STREAM: rows are read past the caches.
+template <bool F32, int TPR, int EPT, bool VEC, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) {
   using P = Part<F32, TPR, EPT, VEC>;
   constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
@@ -96,10 +99,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
     float x[EPT], u[EPT], c[EPT];
-    P::load(a.x, row, a.d, t, x);
+    P::template load<STREAM>(a.x, row, a.d, t, x);
     if (a.f) {
-      P::load(a.f, row, a.d, t, u);
-      if (a.gate_rows) P::load(a.gate, a.gate_rows == 1 ? 0 : row, a.d, t, c);
+      P::template load<STREAM>(a.f, row, a.d, t, u);
+      if (a.gate_rows) P::template load<STREAM>(a.gate, a.gate_rows == 1 ? 0 : row, a.d, t, c);
       if (a.post) {
         float s = 0.f;
 #pragma unroll
@@ -251,6 +254,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_bwd(NormBack a) 
 
 // out[i] [d] = sum over the groups' rows of part[i], in a fixed order: 16 threads to a column take every
 // 16th row each, and one joins them.
+constexpr int kSumLoads = 8;
 struct NormSums {
   int groups, d;
   const float* part[3];
@@ -262,8 +266,18 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormSums a) {
   const int c = blockIdx.x * 64 + lane_id(), w = threadIdx.x >> 6;
   const float* p = a.part[blockIdx.y];
   float v = 0.f;
-  if (c < a.d)
-    for (int r = w; r < a.groups; r += 16) v += p[(int64_t)r * a.d + c];
+  if (c < a.d) {
+    for (int r0 = w; r0 < a.groups; r0 += 16 * kSumLoads) {  // so many loads in flight
+      float u[kSumLoads];
+#pragma unroll
+      for (int i = 0; i < kSumLoads; ++i) {
+        const int r = r0 + 16 * i;
+        u[i] = r < a.groups ? p[(int64_t)r * a.d + c] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < kSumLoads; ++i) v += u[i];
+    }
+  }
   s[w][lane_id()] = v;
   __syncthreads();
   if (w == 0 && c < a.d) {
@@ -278,13 +292,19 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormSums a) {
 struct NormPlan {
   int tpr, ept;
 };
-NormPlan norm_plan(int d) {
+NormPlan forward_plan(int d) {
   const int tpr = d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
   return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
 }
-// Rows in flight in the backward call, and so rows of the partial sums.
+// The backward call holds six rows and up to three sums: 8 elements to a thread leave room for twice the waves (8192 x 8192
+// bf16: 282 us with 16, so MEASB).
+NormPlan backward_plan(int d) {
+  const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
+  return NormPlan{tpr, d <= 8192 ? 8 : 16};
+}
+// Rows in flight in the backward call, and so rows of the partial sums: what the card holds at once.
 int back_groups(int T, int d) {
-  const NormPlan p = norm_plan(d);
+  const NormPlan p = backward_plan(d);
   const int most = p.tpr == 64 ? 2048 : p.tpr == 256 ? 1024 : 512, rows = p.tpr == 64 ? 4 : 1;
   return std::min(most, ceil_div(T, rows) * rows);
 }
@@ -307,16 +327,20 @@ hipError_t with_plan(const NormPlan& p, const F& go) {
 
 template <bool F32, bool VEC>
 hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
-  return with_plan<F32, VEC>(norm_plan(a.d), [&](auto tpr, auto ept) {
+  // Rows that no backward call reads again, or too many to find them in a cache then, are streamed (4096 x 4096 bf16: 39.6
+  // us through the caches, 36.7 past them; 513 x 3840 fp32, forward and backward: 3 us more past them).
+  const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) > (int64_t)128 << 20;
+  return with_plan<F32, VEC>(forward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     const int blocks = std::min(ceil_div(a.T, ROWS), 1 << 20);
-    k_norm_fwd<F32, tpr.value, ept.value, VEC><<<blocks, WG, 0, st>>>(a);
+    if (stream) k_norm_fwd<F32, tpr.value, ept.value, VEC, true><<<blocks, WG, 0, st>>>(a);
+    else k_norm_fwd<F32, tpr.value, ept.value, VEC, false><<<blocks, WG, 0, st>>>(a);
     return hipGetLastError();
   });
 }
 template <bool F32, bool VEC>
 hipError_t launch_bwd(const NormBack& a, int groups, hipStream_t st) {
-  return with_plan<F32, VEC>(norm_plan(a.d), [&](auto tpr, auto ept) {
+  return with_plan<F32, VEC>(backward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     k_norm_bwd<F32, tpr.value, ept.value, VEC><<<groups / ROWS, WG, 0, st>>>(a);
     return hipGetLastError();
