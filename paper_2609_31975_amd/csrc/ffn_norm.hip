@@ -154,7 +154,7 @@ struct NormBack {
 
 // One group of threads takes every groups-th row and keeps its columns' sums over them in registers.
 template <bool F32, int TPR, int EPT, bool VEC>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_bwd(NormBack a) {
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_norm_bwd(NormBack a) {
   using P = Part<F32, TPR, EPT, VEC>;
   constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
   __shared__ float room[2][2][16];
@@ -329,7 +329,7 @@ template <bool F32, bool VEC>
 hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
   // Rows that no backward call reads again, or too many to find them in a cache then, are streamed (4096 x 4096 bf16: 39.6
   // us through the caches, 36.7 past them; 513 x 3840 fp32, forward and backward: 3 us more past them).
-  const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) > (int64_t)128 << 20;
+  const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) >= (int64_t)64 << 20;
   return with_plan<F32, VEC>(forward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     const int blocks = std::min(ceil_div(a.T, ROWS), 1 << 20);

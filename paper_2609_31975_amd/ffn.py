@@ -253,7 +253,7 @@ def _well_formed(x, y, ws, mats, wdtype) -> bool:
 def _raw_stream(stream, x):
     """The stream as _stream gives it, as an integer."""
     if stream is None:
-        return _torch().cuda.current_stream(x.get_device()).cuda_stream
+        return _torch()._C._cuda_getCurrentRawStream(x.get_device())
     return _stream(stream, x.device).value
 
 
@@ -606,6 +606,14 @@ def _check_like(dev, dtype, tensors):
             raise ValueError(f"{name} must be {dtype} {list(shape)}, got {w.dtype} {list(w.shape)}")
 
 
+def _all_like(dev, dtype, shape, tensors) -> bool:
+    """_check_like of tensors that all have one shape (None: left out), without its words."""
+    for w in tensors:
+        if w is not None and (w.dtype is not dtype or w.shape != shape or w.get_device() != dev or not w.is_contiguous()):
+            return False
+    return True
+
+
 def _check_buffers(dev, *buffers):
     for b, name in buffers:
         if b is not None and (b.get_device() != dev or not b.is_contiguous()):
@@ -690,14 +698,22 @@ class Norm:
         self.struct = NormStruct(float(alpha), float(eps), int(self.post), int(bool(gate_sigmoid)),
                                  0 if gate is None else gate.shape[0], _dev(gate, "gate"), _dev(post_gain, "post_gain"),
                                  _dev(pre_gain, "pre_gain"))
+        self.ref, self.rows = ctypes.byref(self.struct), self.struct.gate_rows
+        given = [(v, n) for v, n in ((pre_gain, "pre_gain"), (post_gain, "post_gain"), (gate, "gate")) if v is not None]
+        # what the tensors are, for one comparison a call
+        self.like = None
+        if given:
+            v = given[0][0]
+            self.like = (v.shape[-1], v.get_device(), v.dtype)
+            _check_like(*self.like[1:], [(w, n, (self.rows, self.like[0]) if w is gate else (self.like[0],), False)
+                                         for w, n in given])
 
     def check(self, x, d, dev):
-        gains = (d,)
-        rows = self.struct.gate_rows
-        if rows not in (0, 1, x.shape[0]):
-            raise ValueError(f"gate has {rows} rows, x has {x.shape[0]}")
-        _check_like(dev, x.dtype, ((self.pre_gain, "pre_gain", gains, True), (self.post_gain, "post_gain", gains, True),
-                                   (self.gate, "gate", (rows, d), True)))
+        if self.rows > 1 and self.rows != x.shape[0]:
+            raise ValueError(f"gate has {self.rows} rows, x has {x.shape[0]}")
+        if self.like is not None and self.like != (d, dev, x.dtype):
+            raise ValueError(f"the form's tensors are {self.like[2]} of {self.like[0]} columns on device {self.like[1]}, x is "
+                             f"{x.dtype} of {d} on device {dev}")
 
 
 def norm(eps, pre_gain=None, post=False, post_gain=None, gate=None, gate_sigmoid=False, alpha=1.0) -> Norm:
@@ -721,12 +737,13 @@ def ffn_norm_forward(x, f, form, x_out, n_out, rstd=None, stream=None):
     """x_out = alpha x + gate * post-norm(f) and n_out = pre-norm(x_out), form of ffn.norm(...).  f None: the norm
     of x alone (x_out None).  rstd: None, or a float32 [2, T] tensor for ffn_norm_backward.  Returns (x_out, n_out)."""
     T, d, dev, dt = _tokens(x)
-    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (f, "f", x.shape, True), (x_out, "x_out", x.shape, True),
-                               (n_out, "n_out", x.shape, True)))
+    if not _all_like(dev, x.dtype, x.shape, (x, f, x_out, n_out)):
+        _check_like(dev, x.dtype, ((x, "x", x.shape, False), (f, "f", x.shape, True), (x_out, "x_out", x.shape, True),
+                                   (n_out, "n_out", x.shape, True)))
     _check_rstd(rstd, T, dev)
     form.check(x, d, dev)
-    rc = _function("ffn_norm_forward")(dt, T, d, x.data_ptr(), _p(f), ctypes.byref(form.struct), _p(x_out), _p(n_out),
-                                       _p(rstd), _raw_stream(stream, x))
+    rc = _function("ffn_norm_forward")(dt, T, d, x.data_ptr(), _p(f), form.ref, _p(x_out), _p(n_out), _p(rstd),
+                                       _raw_stream(stream, x))
     _check("ffn_norm_forward", rc)
     return x_out, n_out
 
@@ -740,14 +757,17 @@ def ffn_norm_backward(x_out, f, form, rstd, dn, dx_out, ws, dx=None, df=None, dg
         raise ValueError("x_out, dn or dx_out is required")
     T, d, dev, dt = _tokens(like)
     rows, gain = like.shape, (d,)
-    _check_like(dev, like.dtype, ((x_out, "x_out", rows, True), (f, "f", rows, True), (dn, "dn", rows, True),
-                                  (dx_out, "dx_out", rows, True), (dx, "dx", rows, True), (df, "df", rows, True),
-                                  (dgate, "dgate", (form.struct.gate_rows, d), True),
-                                  (dpost_gain, "dpost_gain", gain, True), (dpre_gain, "dpre_gain", gain, True)))
+    if not (_all_like(dev, like.dtype, rows, (x_out, f, dn, dx_out, dx, df)) and
+            _all_like(dev, like.dtype, gain, (dpost_gain, dpre_gain)) and
+            _all_like(dev, like.dtype, (form.rows, d), (dgate,))):
+        _check_like(dev, like.dtype, ((x_out, "x_out", rows, True), (f, "f", rows, True), (dn, "dn", rows, True),
+                                      (dx_out, "dx_out", rows, True), (dx, "dx", rows, True), (df, "df", rows, True),
+                                      (dgate, "dgate", (form.rows, d), True), (dpost_gain, "dpost_gain", gain, True),
+                                      (dpre_gain, "dpre_gain", gain, True)))
     _check_rstd(rstd, T, dev)
     _check_buffers(dev, (ws, "ws"))
     form.check(like, d, dev)
-    rc = _function("ffn_norm_backward")(dt, T, d, _p(x_out), _p(f), ctypes.byref(form.struct), _p(rstd), _p(dn),
+    rc = _function("ffn_norm_backward")(dt, T, d, _p(x_out), _p(f), form.ref, _p(rstd), _p(dn),
                                         _p(dx_out), _p(dx), _p(df), _p(dgate), _p(dpost_gain), _p(dpre_gain),
                                         ws.data_ptr(), _size(ws), _raw_stream(stream, like))
     _check("ffn_norm_backward", rc)
@@ -773,6 +793,7 @@ class GroupQ:
         if scales.device != codes.device or (offsets is not None and offsets.device != codes.device):
             raise ValueError("codes, scales and offsets must be on one device")
         self.struct = GroupQStruct(*ptrs, sdt, self.n_in // scales.shape[1])
+        self.ref, self.dev = ctypes.byref(self.struct), codes.get_device()
 
 
 def group_q(codes, scales, offsets=None) -> GroupQ:
@@ -790,9 +811,10 @@ def alloc_group_q_workspace(T, n_in, n_out, gated=False, device="cuda"):
 def _group_q_args(x, mats, y):
     T, n_in, dev, dt = _tokens(x)
     n_out = mats[0].n_out
-    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (y, "y", (T, n_out), False)))
+    if y is None or not (_all_like(dev, x.dtype, x.shape, (x,)) and _all_like(dev, x.dtype, (T, n_out), (y,))):
+        _check_like(dev, x.dtype, ((x, "x", x.shape, False), (y, "y", (T, n_out), False)))
     for w in mats:
-        if (w.n_out, w.n_in) != (n_out, n_in) or w.codes.get_device() != dev:
+        if w.n_out != n_out or w.n_in != n_in or w.dev != dev:
             raise ValueError(f"the weights are [{w.n_out}, {w.n_in}] on {w.codes.device}, x is {list(x.shape)} on {x.device}")
     return dt, T, n_in, n_out
 
@@ -801,7 +823,7 @@ def ffn_group_q_forward(x, w, y, ws, stream=None):
     """y = x W^T of bfloat16 or float32 tokens and 4-bit weights of ffn.group_q(...)."""
     args = _group_q_args(x, (w,), y)
     _check_buffers(x.get_device(), (ws, "ws"))
-    rc = _function("ffn_group_q_forward")(*args, x.data_ptr(), ctypes.byref(w.struct), y.data_ptr(), ws.data_ptr(),
+    rc = _function("ffn_group_q_forward")(*args, x.data_ptr(), w.ref, y.data_ptr(), ws.data_ptr(),
                                           _size(ws), _raw_stream(stream, x))
     _check("ffn_group_q_forward", rc)
     return y
@@ -811,7 +833,7 @@ def ffn_group_q_gated_forward(x, w_gate, w_up, t, opt, z, ws, stream=None):
     """z = A(x W1^T - t) U(x W3^T): the hidden layer of the gated block with 4-bit weights."""
     args = _group_q_args(x, (w_gate, w_up), z)
     _check_buffers(x.get_device(), (ws, "ws"))
-    rc = _function("ffn_group_q_gated_forward")(*args, x.data_ptr(), ctypes.byref(w_gate.struct), ctypes.byref(w_up.struct),
+    rc = _function("ffn_group_q_gated_forward")(*args, x.data_ptr(), w_gate.ref, w_up.ref,
                                                 ctypes.c_float(t), _opt(opt), z.data_ptr(), ws.data_ptr(), _size(ws),
                                                 _raw_stream(stream, x))
     _check("ffn_group_q_gated_forward", rc)
@@ -832,6 +854,7 @@ class Router:
         given = w is None
         self.struct = RouterStruct(experts, k, _dev(w, "w"), _dev(bias, "bias"), 0 if given else int(bool(sigmoid)),
                                    0 if given else int(bool(normalize)), 0.0 if given else float(scale))
+        self.ref = ctypes.byref(self.struct)
 
 
 def router(experts, k, w=None, bias=None, sigmoid=False, normalize=True, scale=1.0) -> Router:
@@ -856,12 +879,15 @@ def ffn_moe_forward(x, router, w_gate, w_up, w_down_t, t, opt, ids, weights, y, 
         raise ValueError(f"w_up must be [experts, d_ff, d], got {tuple(w_up.shape)}")
     E, k, d_ff = router.experts, router.k, w_up.shape[1]
     w = (E, d_ff, d)
-    _check_like(dev, x.dtype, ((x, "x", x.shape, False), (router.w, "the router's w", (E, d), True), (w_gate, "w_gate", w, False),
-                               (w_up, "w_up", w, False), (w_down_t, "w_down_t", w, False), (y, "y", x.shape, False)))
+    if w_gate is None or w_down_t is None or y is None or not (
+            _all_like(dev, x.dtype, x.shape, (x, y)) and _all_like(dev, x.dtype, w, (w_gate, w_up, w_down_t)) and
+            _all_like(dev, x.dtype, (E, d), (router.w,))):
+        _check_like(dev, x.dtype, ((x, "x", x.shape, False), (router.w, "the router's w", (E, d), True), (w_gate, "w_gate", w, False),
+                                   (w_up, "w_up", w, False), (w_down_t, "w_down_t", w, False), (y, "y", x.shape, False)))
     _check_like(dev, torch.int32, ((ids, "ids", (T, k), False),))
     _check_like(dev, torch.float32, ((weights, "weights", (T, k), False), (router.bias, "the router's bias", (E,), True)))
     _check_buffers(dev, (ws, "ws"))
-    rc = _function("ffn_moe_forward")(wdt, T, d, d_ff, ctypes.byref(router.struct), x.data_ptr(), w_gate.data_ptr(),
+    rc = _function("ffn_moe_forward")(wdt, T, d, d_ff, router.ref, x.data_ptr(), w_gate.data_ptr(),
                                       w_up.data_ptr(), w_down_t.data_ptr(), ctypes.c_float(t), _opt(opt), ids.data_ptr(),
                                       weights.data_ptr(), y.data_ptr(), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
     _check("ffn_moe_forward", rc)
