@@ -73,11 +73,11 @@ struct GqWs {
   size_t bytes;
 };
 GqWs gq_layout(int T, int n_in, int n_out, bool gated, void* base) {
-  const size_t tokens = std::min(T, kGqTokens), columns = (size_t)ceil_div(n_in, kWindow) * kWindow;
+  const size_t tokens = std::min(T, kGqTokens), columns = (size_t)ceil_div(n_in, kGqWaves * kWindow) * kGqWaves * kWindow;
   Carver c{static_cast<char*>(base)};
   GqWs w;
   w.part = static_cast<float*>(c.take(sizeof(float) * kGqSharesMost * (gated ? 2 : 1) * tokens * n_out));
-  w.planes = static_cast<uint4*>(c.take(3 * 2 * tokens * columns));
+  w.planes = static_cast<uint4*>(c.take(3 * 2 * ceil_div<size_t>(tokens, 16) * 16 * columns));
   w.sums = static_cast<float*>(c.take(sizeof(float) * columns / 32 * kGqTokens));
   w.bytes = c.off;
   return w;
@@ -115,6 +115,7 @@ int gq_call(ffn_dtype_t xdt, int T, int n_in, int n_out, const void* x, const ff
     a.chunk = p.chunk;
     a.div_group = (uint32_t)(((uint64_t)1 << 31) / (w->group / 32) + 1);
     a.groups = n_in / w->group;
+    a.packed = p.ns > 1 && w->group * p.ns == kWindow && n_in % kWindow == 0;
     a.x = static_cast<const char*>(x) + (size_t)t0 * n_in * xs;
     a.w[0] = GqMatrix{w->codes, w->scales, w->offsets};
     if (w2) a.w[1] = GqMatrix{w2->codes, w2->scales, w2->offsets};

@@ -23,6 +23,7 @@ struct GqArgs {
   int chunk;           // windows of x in LDS at a time
   uint32_t div_group;  // q = (n div_group) >> 31 divides a count of 32 codes by group / 32
   int groups;          // of a row
+  bool packed;         // a window's scales lie side by side, whole dwords of them
   const void* x;
   GqMatrix w[2];
   int act, silu_up;
@@ -40,6 +41,11 @@ constexpr int gq_batch(bool gated, int ns) { return gated || ns > 1 ? 1 : 2; }
 // Waves that share a row tile's windows with two tiles of tokens and more
 constexpr int kGqWaves = 2;
 
+// x of kGqWaves windows of nt token tiles in LDS, with their sums; two of them where the CU has room (160 KB), so that one is
+// filled while the other is read.
+constexpr size_t gq_buffer(bool xf32, int nt) { return (size_t)kGqWaves * nt * ((xf32 ? 3 : 1) * 4096 + 4 * 64); }
+constexpr int gq_buffers(bool xf32, int nt) { return 2 * gq_buffer(xf32, nt) <= 160 * 1024 ? 2 : 1; }
+
 // Tiles of a pass: nt 16-token tiles (0: one token, windows of 256 codes); wk of the 8 waves share a row tile's windows, u at a time each; whole: a share's x
 // lies in LDS at once.
 struct GqPlan {
@@ -52,7 +58,8 @@ struct GqPlan {
 inline size_t gq_lds(bool xf32, const GqPlan& p, int T) {
   const size_t planes = xf32 ? 3 : 1;
   if (p.nt == 0) return p.chunk * (planes * 4 * kWindow + 32);
-  return planes * T * (p.chunk * 2 * kWindow + 16) + (size_t)p.chunk * p.ns * 64 * p.nt;
+  const size_t sums = (size_t)p.chunk * p.ns * 64 * p.nt;
+  return p.nt > 1 ? gq_buffers(xf32, p.nt) * gq_buffer(xf32, p.nt) : planes * T * (p.chunk * 2 * kWindow + 16) + sums;
 }
 GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out);
 

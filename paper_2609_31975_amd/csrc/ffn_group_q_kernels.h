@@ -28,6 +28,8 @@ namespace {
 // each (mask, and an exclusive or that sets 16's bits and turns the code's sign bit over).  An instruction takes one constant
 // from the scalar side: `mask` is kMask in a vector register.
 constexpr uint32_t kMask = 0x00780078u;
+// all vector memory operations of this wave, the ones into LDS among them
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t mask) {
   constexpr uint32_t s = 0x41C041C0u;
   return make_uint4((w << 3 & mask) ^ s, (w >> 1 & mask) ^ s, (w >> 5 & mask) ^ s, (w >> 9 & mask) ^ s);
@@ -110,50 +112,41 @@ struct XPieces {
   }
 };
 
-// Two token tiles and more: what XPieces makes in LDS is made once for all workgroups, in memory: planes [P][T][windows 128] and
-// the table [windows][NS][tokens of the tiles].
-template <bool XF32, int NS>
-__global__ __launch_bounds__(256) void k_group_q_split(GqArgs a, int tokens) {
-  const int pieces = a.windows * (kWindow / 8), i = blockIdx.x * 256 + threadIdx.x, t = i / pieces, c = i - t * pieces;
+// Two token tiles and more: x is taken apart once for all workgroups, in memory, into whole operands: for window w, MFMA f, part
+// p and token tile t the 64 lanes' 16 bytes at ((4 w + f) P + p) NT + t, so that a chunk is one piece of memory and LDS reads
+// have no bank conflicts; and the table [windows][NS][tokens].  Tokens past the last one are left as they are in there: a token's
+// operands reach its own results alone.
+template <bool XF32, int NS, int NT>
+__global__ __launch_bounds__(256) void k_group_q_split(GqArgs a, int windows) {
+  constexpr int P = XF32 ? 3 : 1;
+  const int pieces = windows * (kWindow / 8), i = blockIdx.x * 256 + threadIdx.x, t = i / pieces, c = i - t * pieces;
   const Buf xb = make_buf(a.x, (uint32_t)a.T * a.n_in * (XF32 ? 4 : 2));
   const uint32_t o = t < a.T && c * 8 < a.n_in ? ((uint32_t)t * a.n_in + c * 8) * (XF32 ? 4 : 2) : kOOB;
-  uint4 v[XF32 ? 2 : 1], d[XF32 ? 3 : 1];
+  uint4 v[XF32 ? 2 : 1], d[P];
   v[0] = ldb(xb, o);
   if constexpr (XF32) v[1] = ldb(xb, o + 16);
   const float sum = group_sum(split_piece<XF32>(v, d), 16 / NS);
   if (t >= a.T) return;
+  const int w = c / 16, f = NS > 1 ? c % 16 / 4 : c % 4, g = NS > 1 ? c % 4 : c % 16 / 4;
 #pragma unroll
-  for (int q = 0; q < (XF32 ? 3 : 1); ++q) a.planes[((size_t)q * a.T + t) * pieces + c] = d[q];
-  if (c % (16 / NS) == 0) a.sums[(size_t)(c / (16 / NS)) * tokens + t] = -24.f * sum;
+  for (int p = 0; p < P; ++p) a.planes[(((size_t)(w * 4 + f) * P + p) * NT + t / 16) * 64 + g * 16 + t % 16] = d[p];
+  if (c % (16 / NS) == 0) a.sums[(size_t)(c / (16 / NS)) * (16 * NT) + t] = -24.f * sum;
 }
-// WK windows of it on their way into LDS, in the same places as XPieces has them.
+// WK windows of it, straight into LDS.
 template <bool XF32, int NS, int NT, int WK>
 struct XCopy {
-  static constexpr int P = XF32 ? 3 : 1, UNITS = WK * (kWindow / 8), ROWS = P * 16 * NT, N = ROWS * UNITS / 512;
-  static constexpr int SUMS = WK * NS * 16 * NT;  // 512 or fewer
-  uint4 v[N];
-  float sum;
-
-  __device__ __forceinline__ void load(const GqArgs& a, int w0, int) {
-    const int pieces = a.windows * (kWindow / 8);
-    const Buf b = make_buf(a.planes, (uint32_t)(P * a.T * pieces) * 16u), tb = make_buf(a.sums, (uint32_t)a.windows * NS * 64 * NT);
+  static constexpr int P = XF32 ? 3 : 1, BYTES = WK * 4 * P * NT * 1024, SUMS = WK * NS * 16 * NT;  // 512 sums or fewer
+  static __device__ __forceinline__ float* table(const GqArgs&, char* lds) { return reinterpret_cast<float*>(lds + BYTES); }
+  static __device__ __forceinline__ void copy(const GqArgs& a, char* lds, int w0) {
+    const char* from = reinterpret_cast<const char*>(a.planes) + (size_t)w0 * (BYTES / WK);
+    const int wave = uniform(threadIdx.x >> 6);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = j * 512 + (int)threadIdx.x, r = i / UNITS, c = w0 * (kWindow / 8) + i % UNITS;
-      v[j] = ldb(b, r < P * a.T && c < pieces ? (uint32_t)(r * pieces + c) * 16u : kOOB);
+    for (int j = 0; j < BYTES / 8192; ++j) {  // 8 waves, 1 KB each
+      const int at = (j * 8 + wave) * 1024;
+      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(const_cast<char*>(from) + at + lane_id() * 16),
+                                       (__attribute__((address_space(3))) void*)(lds + at), 16, 0, 0);
     }
-    sum = __builtin_bit_cast(float, ldb32(tb, (int)threadIdx.x < SUMS ? (uint32_t)(w0 * NS * 16 * NT + threadIdx.x) * 4u : kOOB));
-  }
-  static __device__ __forceinline__ float* table(const GqArgs& a, char* lds) {
-    return reinterpret_cast<float*>(lds + P * a.T * (WK * 2 * kWindow + 16));
-  }
-  __device__ __forceinline__ void store(const GqArgs& a, char* lds, int) const {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = j * 512 + (int)threadIdx.x, r = i / UNITS;
-      if (r < P * a.T) *reinterpret_cast<uint4*>(lds + r * (WK * 2 * kWindow + 16) + i % UNITS * 16) = v[j];
-    }
-    if ((int)threadIdx.x < SUMS) table(a, lds)[threadIdx.x] = sum;
+    if ((int)threadIdx.x < SUMS) table(a, lds)[threadIdx.x] = a.sums[(size_t)w0 * NS * 16 * NT + threadIdx.x];
   }
 };
 
@@ -181,15 +174,50 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
   }
   const uint32_t code_at = row * row_bytes + g * 16, scale_at = row * a.groups * ss;
 
+  // A window's scales: NS floats, or with bf16 ones NS / 2 dwords of two (one of one).
+  constexpr int SD = SF32 ? NS : (NS + 1) / 2;
+  struct Scales {
+    uint32_t v[SD];
+    __device__ __forceinline__ float at(int f) const {
+      if constexpr (SF32) return __uint_as_float(v[f]);
+      else return __uint_as_float(f & 1 ? v[f >> 1] & 0xffff0000u : v[f >> 1] << 16);
+    }
+  };
   struct Batch {
     uint4 codes[U][M];
-    uint32_t sc[U][M][NS], of[OFF ? U : 1][M][NS];
+    Scales sc[U][M], of[OFF ? U : 1][M];
   };
-  auto raw = [&](const Buf& b, uint32_t i) -> uint32_t {
-    if constexpr (SF32) return (uint32_t)ldb32(b, i);
-    else return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, i, 0, 0);
+  auto load_scales = [&](const Buf& b, int w, Scales& s) {
+    if (NS > 1 && a.packed) {
+      // one load: a gather of 16 rows' scales costs what one of their codes does (two a group with offsets; groups of 64,
+      // 48 fp32 tokens of 4096 -> 14336 twice: 77 us, so 67)
+      const uint32_t at = scale_at + (w < last ? w * NS * ss : kOOB);
+      if constexpr (SD == 1) {
+        s.v[0] = (uint32_t)ldb32(b, at);
+      } else if constexpr (SD == 2) {
+        typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+        const u2 v = __builtin_bit_cast(u2, __builtin_amdgcn_raw_buffer_load_b64(b.r, at, 0, 0));
+        s.v[0] = v[0];
+        s.v[1] = v[1];
+      } else {
+        const uint4 v = ldb(b, at);
+        s.v[0] = v.x;
+        s.v[1] = v.y;
+        s.v[SD - 2] = v.z;
+        s.v[SD - 1] = v.w;
+      }
+      return;
+    }
+    uint32_t raw[NS];
+#pragma unroll
+    for (int f = 0; f < NS; ++f) {
+      const uint32_t k32 = w * 4 + f * PER, gi = (uint32_t)((uint64_t)k32 * a.div_group >> 31);
+      const uint32_t at = scale_at + (w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB);
+      raw[f] = SF32 ? (uint32_t)ldb32(b, at) : (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, at, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < SD; ++i) s.v[i] = SF32 ? raw[i] : NS == 1 ? raw[0] : raw[2 * i] | raw[(2 * i + 1) % NS] << 16;
   };
-  auto value = [](uint32_t v) { return __uint_as_float(SF32 ? v : v << 16); };
   // Lines of 128 bytes are read in two halves, by the same wave or its neighbour: through the caches (streamed past them
   // the same reads came to 5.2 TB/s, through them to 5.6).  Codes behind the row's end, of the next row or zeros behind the
   // matrix, meet zeros of x; scales behind the share's or the row's end are zeros, never the next row's.
@@ -198,16 +226,10 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
     for (int u = 0; u < U; ++u) {
       const int w = w_first + wk * U + u;
 #pragma unroll
-      for (int m = 0; m < M; ++m) b.codes[u][m] = ldb(cb[m], code_at + w * (kWindow / 2));
-#pragma unroll
-      for (int f = 0; f < NS; ++f) {
-        const uint32_t k32 = w * 4 + f * PER, gi = (uint32_t)((uint64_t)k32 * a.div_group >> 31);
-        const uint32_t at = scale_at + (w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB);
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-          b.sc[u][m][f] = raw(sb[m], at);
-          if constexpr (OFF) b.of[u][m][f] = raw(ob[m], at);
-        }
+      for (int m = 0; m < M; ++m) {
+        b.codes[u][m] = ldb(cb[m], code_at + w * (kWindow / 2));
+        load_scales(sb[m], w, b.sc[u][m]);
+        if constexpr (OFF) load_scales(ob[m], w, b.of[u][m]);
       }
     }
   };
@@ -227,19 +249,36 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
   Batch even, odd;
   load(first + turn * UNIT, even);
   using Pieces = std::conditional_t<NT == 1, XPieces<XF32, NS, 16>, XCopy<XF32, NS, NT, WK>>;
-  Pieces xp;
-  xp.load(a, first, 0);
+  std::conditional_t<NT == 1, Pieces, int> xp;
+  if constexpr (NT == 1) xp.load(a, first, 0);
+  constexpr int BUFFERS = NT > 1 ? gq_buffers(XF32, NT) : 1;
+  char* buf = lds;
+  if constexpr (BUFFERS == 2) Pieces::copy(a, buf, first);
   for (int c0 = first; c0 < last; c0 += a.chunk) {
-    if (c0 != first) __syncthreads();
-    xp.store(a, lds, 0);
-    if constexpr (WHOLE) {
-      for (int i = Pieces::SPAN; i < a.T * a.chunk * (kWindow / 8); i += Pieces::SPAN) {
-        xp.load(a, c0, i);
-        xp.store(a, lds, i);
+    if constexpr (BUFFERS == 2) {
+      // this chunk is here; the next one goes where the last one was, which all waves have left
+      wait_loads();
+      __syncthreads();
+      char* other = lds + (buf == lds ? gq_buffer(XF32, NT) : 0);
+      if (c0 + a.chunk < last) Pieces::copy(a, other, c0 + a.chunk);
+    } else {
+      if (c0 != first) __syncthreads();
+      if constexpr (NT == 1) {
+        xp.store(a, buf, 0);
+        if constexpr (WHOLE) {
+          for (int i = Pieces::SPAN; i < a.T * a.chunk * (kWindow / 8); i += Pieces::SPAN) {
+            xp.load(a, c0, i);
+            xp.store(a, buf, i);
+          }
+        }
+      } else {
+        Pieces::copy(a, buf, c0);
+        wait_loads();
       }
+      __syncthreads();
+      if constexpr (NT == 1 && !WHOLE)
+        if (c0 + a.chunk < last) xp.load(a, c0 + a.chunk, 0);
     }
-    __syncthreads();
-    if (!WHOLE && c0 + a.chunk < last) xp.load(a, c0 + a.chunk, 0);
     auto products = [&](const Batch& cur, Batch& nxt) {
       const int here = first + turn * UNIT - c0;  // a window of the chunk
       turn = turn + 1 == batches ? 0 : turn + 1;
@@ -252,45 +291,59 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
 #pragma unroll
         for (int m = 0; m < M; ++m) q[m] = TR ? transpose4(cur.codes[u][m]) : cur.codes[u][m];
         // The sums of tokens past the last one, and their starts, stay in their own rows, which are not stored.
-        const f32x4_t* tab = reinterpret_cast<const f32x4_t*>(Pieces::table(a, lds)) + w * NS * 4 * NT + g;
-        f32x4_t sum[NT][M], gone[NT];
+        const f32x4_t* tab = reinterpret_cast<const f32x4_t*>(Pieces::table(a, buf)) + w * NS * 4 * NT + g;
+        f32x4_t sum[NT][M], starts[2][NT];
+        // x of an MFMA f and what its sums start from; with more than one token tile the next f's are on their way during its products
+        bf16x8_t x[2][NT][P];
+        auto load_x = [&](int f) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            if (f % PER == 0) starts[f / PER & 1][t] = tab[f / PER * 4 * NT + t * 4];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+              const char* at = NT == 1 ? buf + xrow[t] + w * 2 * kWindow + (TR ? f * 64 + g * 16 : g * 64 + f * 16) + p * a.T * stride
+                                       : buf + ((w * 4 + f) * P * NT + p * NT + t) * 1024 + lane * 16;
+              x[f & 1][t][p] = bf8(*reinterpret_cast<const uint4*>(at));
+            }
+          }
+        };
+        load_x(0);
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
+          if (f < 3) load_x(f + 1);
+          if constexpr (NT > 1) issue_barrier();
           bf16x8_t wf[M];
 #pragma unroll
           for (int m = 0; m < M; ++m) wf[m] = bf8(codes8(f == 0 ? q[m].x : f == 1 ? q[m].y : f == 2 ? q[m].z : q[m].w, mask));
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const char* xr = lds + xrow[t] + w * 2 * kWindow + (TR ? f * 64 + g * 16 : g * 64 + f * 16);
-            bf16x8_t x[P];
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int p = 0; p < P; ++p) x[p] = bf8(*reinterpret_cast<const uint4*>(xr + p * a.T * stride));
-            if (f % PER == 0) {
-              gone[t] = tab[f / PER * 4 * NT + t * 4];
+            for (int m = 0; m < M; ++m)
+              if (f % PER == 0) sum[t][m] = starts[f / PER & 1][t];
 #pragma unroll
-              for (int m = 0; m < M; ++m) sum[t][m] = gone[t];
-            }
+          for (int p = P - 1; p >= 0; --p)
 #pragma unroll
-            for (int p = P - 1; p >= 0; --p)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int m = 0; m < M; ++m) sum[t][m] = mfma16(x[p], wf[m], sum[t][m]);
-            if (f % PER == PER - 1) {
-              const int s = f / PER;
+              for (int m = 0; m < M; ++m) sum[t][m] = mfma16(x[f & 1][t][p], wf[m], sum[t][m]);
+          if (f % PER == PER - 1) {
+            const int s = f / PER;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
 #pragma unroll
               for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][m][i] += value(cur.sc[u][m][s]) * sum[t][m][i];
+                for (int i = 0; i < 4; ++i) acc[t][m][i] += cur.sc[u][m].at(s) * sum[t][m][i];
               if constexpr (OFF) {
-                const f32x4_t sx = gone[t] * (-1.f / 24.f);
+                const f32x4_t sx = starts[s & 1][t] * (-1.f / 24.f);
 #pragma unroll
                 for (int m = 0; m < M; ++m)
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) acc[t][m][i] += value(cur.of[u][m][s]) * sx[i];
+                  for (int i = 0; i < 4; ++i) acc[t][m][i] += cur.of[u][m].at(s) * sx[i];
               }
             }
           }
-          // operands of one f at a time: more of them in registers spill
-          if constexpr (NT > 1 || (GATED && NS == 4)) issue_barrier();
+          if constexpr (GATED && NS == 4) issue_barrier();  // one f at a time: more of them in registers spill
         }
       }
     };
@@ -306,6 +359,7 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
       products(even, odd);
       even = odd;
     }
+    if constexpr (BUFFERS == 2) buf = lds + (buf == lds ? gq_buffer(XF32, NT) : 0);
   }
 
   // The WK waves' sums joined in LDS, in their order; one token tile at a time.
@@ -530,7 +584,10 @@ hipError_t launch_tiles(const GqArgs& a, const GqPlan& p, hipStream_t st) {
     return p.wk == 4 ? go(Int<1>{}, Int<4>{}, Int<U>{}, yes) : go(Int<1>{}, Int<2>{}, Int<U>{}, yes);
   }
   if (p.nt == 1) return p.wk == 8 ? go(Int<1>{}, Int<8>{}, Int<1>{}, no) : go(Int<1>{}, Int<4>{}, Int<1>{}, no);
-  k_group_q_split<XF32, NS><<<ceil_div(a.T * a.windows * (kWindow / 8), 256), 256, 0, st>>>(a, 16 * p.nt);
+  const int windows = ceil_div(a.windows, kGqWaves) * kGqWaves, blocks = ceil_div(a.T * windows * (kWindow / 8), 256);
+  if (p.nt == 2) k_group_q_split<XF32, NS, 2><<<blocks, 256, 0, st>>>(a, windows);
+  else if (p.nt == 3) k_group_q_split<XF32, NS, 3><<<blocks, 256, 0, st>>>(a, windows);
+  else k_group_q_split<XF32, NS, 4><<<blocks, 256, 0, st>>>(a, windows);
   if (const hipError_t e = hipGetLastError()) return e;
   constexpr Int<kGqWaves> w;
   return p.nt == 2 ? go(Int<2>{}, w, Int<1>{}, no) : p.nt == 3 ? go(Int<3>{}, w, Int<1>{}, no) : go(Int<4>{}, w, Int<1>{}, no);

