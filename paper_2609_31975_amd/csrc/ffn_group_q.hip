@@ -11,7 +11,7 @@ namespace ffn {
 GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out) {
   GqPlan p{};
   p.nt = T == 1 ? 0 : ceil_div(T, 16);
-  p.ns = group % kWindow == 0 ? 1 : group % 64 == 0 ? 2 : 4;
+  p.ns = group % kWindow == 0 ? 1 : n_in % kWindow ? 8 : group == 64 ? 2 : group == 32 ? 4 : 8;
   const int windows = ceil_div(n_in, p.nt ? kWindow : 2 * kWindow);
   auto share = [&] {
     const int unit = p.wk * p.u, units = ceil_div(windows, unit);
@@ -115,7 +115,6 @@ int gq_call(ffn_dtype_t xdt, int T, int n_in, int n_out, const void* x, const ff
     a.chunk = p.chunk;
     a.div_group = (uint32_t)(((uint64_t)1 << 31) / (w->group / 32) + 1);
     a.groups = n_in / w->group;
-    a.packed = p.ns > 1 && w->group * p.ns == kWindow && n_in % kWindow == 0;
     a.x = static_cast<const char*>(x) + (size_t)t0 * n_in * xs;
     a.w[0] = GqMatrix{w->codes, w->scales, w->offsets};
     if (w2) a.w[1] = GqMatrix{w2->codes, w2->scales, w2->offsets};

@@ -23,7 +23,6 @@ struct GqArgs {
   int chunk;           // windows of x in LDS at a time
   uint32_t div_group;  // q = (n div_group) >> 31 divides a count of 32 codes by group / 32
   int groups;          // of a row
-  bool packed;         // a window's scales lie side by side, whole dwords of them
   const void* x;
   GqMatrix w[2];
   int act, silu_up;
@@ -34,6 +33,7 @@ struct GqArgs {
   float* sums;
 };
 
+constexpr int gq_scales(int nsx) { return nsx == 8 ? 4 : nsx; }
 // Windows of a wave in a batch, where the next batch's registers fit beside it.
 constexpr int gq_batch(bool gated, int ns) { return gated || ns > 1 ? 1 : 2; }
 
@@ -51,14 +51,14 @@ constexpr int gq_buffers(bool xf32, int nt) { return 2 * gq_buffer(xf32, nt) <= 
 struct GqPlan {
   int nt, wk, u;
   bool whole;
-  int ns;  // scales of a window
+  int ns;  // NSX of k_group_q
   int chunk, per_share, shares, blocks;
 };
 // x and its sums in LDS
 inline size_t gq_lds(bool xf32, const GqPlan& p, int T) {
   const size_t planes = xf32 ? 3 : 1;
-  if (p.nt == 0) return p.chunk * (planes * 4 * kWindow + 32);
-  const size_t sums = (size_t)p.chunk * p.ns * 64 * p.nt;
+  if (p.nt == 0) return p.chunk * (planes * 4 * kWindow + (xf32 ? 128 : 32));
+  const size_t sums = (size_t)p.chunk * gq_scales(p.ns) * 64 * p.nt;
   return p.nt > 1 ? gq_buffers(xf32, p.nt) * gq_buffer(xf32, p.nt) : planes * T * (p.chunk * 2 * kWindow + 16) + sums;
 }
 GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out);

@@ -5,6 +5,8 @@
 //   - The codes enter the bf16 products unscaled.  Two nibbles of a dword become two bf16 of value 24 + code (16 + u has
 //     u in its top mantissa bits; u = code + 8): 8 operations for 8 codes.  What the 24 add, 24 times the sum of the
 //     same x, is in a table in LDS that the sums start from.  A group's sum is then multiplied by its row's scale.
+//     (fp32 x: sums start from zero with the least of the three parts, and the table's value is added last.  What the 24 add
+//     is several times the result, and every addition beside it rounds by that.)
 //   - One token: dot products on the vector ALUs (k_group_q1).  More: v_mfma_f32_16x16x32_bf16 (k_group_q).
 //   - Tokens are the A operand, weight rows the B operand: a lane's results are of one weight row, whose scale it
 //     holds.
@@ -28,6 +30,10 @@ namespace {
 // each (mask, and an exclusive or that sets 16's bits and turns the code's sign bit over).  An instruction takes one constant
 // from the scalar side: `mask` is kMask in a vector register.
 constexpr uint32_t kMask = 0x00780078u;
+// A plain vector: the compiler takes LDS reads of types that it does not know to wait for all loads into LDS.
+__device__ __forceinline__ bf16x8_t lds_operand(const char* p) {
+  return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p));
+}
 // all vector memory operations of this wave, the ones into LDS among them
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t mask) {
@@ -146,16 +152,20 @@ struct XCopy {
       __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(const_cast<char*>(from) + at + lane_id() * 16),
                                        (__attribute__((address_space(3))) void*)(lds + at), 16, 0, 0);
     }
-    if ((int)threadIdx.x < SUMS) table(a, lds)[threadIdx.x] = a.sums[(size_t)w0 * NS * 16 * NT + threadIdx.x];
+    if (wave * 64 < SUMS)  // whole waves: the table's rows in memory and in LDS have room for four sums a window
+      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(a.sums + (size_t)w0 * NS * 16 * NT + wave * 64 + lane_id()),
+                                       (__attribute__((address_space(3))) void*)(lds + BYTES + wave * 256), 4, 0, 0);
   }
 };
 
 // 8 waves: WK of them share a row tile's windows, 8 / WK row tiles of 16 to a workgroup.  NT: 16-token
-// tiles.  U: windows of a wave in a batch; the next batch is on its way during a batch's products.  NS: scales of a window, 1,
-// 2 or 4 (groups that are multiples of 128, of 64, of 32).  OFF: there are offsets.  WHOLE: all of a share's x is in LDS at once.
-template <bool XF32, bool SF32, bool GATED, int NS, bool OFF, int NT, int WK, int U, bool WHOLE>
+// tiles.  U: windows of a wave in a batch; the next batch is on its way during a batch's products.  NSX: scales of a window, 1
+// (groups that are multiples of 128), 2 or 4 (of 64 and 32, a window's scales side by side in whole dwords), or 8: any other
+// group, a scale for every 32 codes.  OFF: there are offsets.  WHOLE: all of a share's x is in LDS at once.
+template <bool XF32, bool SF32, bool GATED, int NSX, bool OFF, int NT, int WK, int U, bool WHOLE>
 __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
-  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK * U, PER = 4 / NS;
+  constexpr int M = GATED ? 2 : 1, WR = 8 / WK, P = XF32 ? 3 : 1, UNIT = WK * U;
+  constexpr int NS = gq_scales(NSX), PER = 4 / NS;
   constexpr bool TR = NS > 1;
   extern __shared__ __align__(16) char lds[];
   const int lane = lane_id(), wave = uniform(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -188,7 +198,7 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
     Scales sc[U][M], of[OFF ? U : 1][M];
   };
   auto load_scales = [&](const Buf& b, int w, Scales& s) {
-    if (NS > 1 && a.packed) {
+    if constexpr (NSX == 2 || NSX == 4) {
       // one load: a gather of 16 rows' scales costs what one of their codes does (two a group with offsets; groups of 64,
       // 48 fp32 tokens of 4096 -> 14336 twice: 77 us, so 67)
       const uint32_t at = scale_at + (w < last ? w * NS * ss : kOOB);
@@ -206,17 +216,17 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
         s.v[SD - 2] = v.z;
         s.v[SD - 1] = v.w;
       }
-      return;
-    }
-    uint32_t raw[NS];
+    } else {
+      uint32_t raw[NS];
 #pragma unroll
-    for (int f = 0; f < NS; ++f) {
-      const uint32_t k32 = w * 4 + f * PER, gi = (uint32_t)((uint64_t)k32 * a.div_group >> 31);
-      const uint32_t at = scale_at + (w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB);
-      raw[f] = SF32 ? (uint32_t)ldb32(b, at) : (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, at, 0, 0);
-    }
+      for (int f = 0; f < NS; ++f) {
+        const uint32_t k32 = w * 4 + f * PER, gi = (uint32_t)((uint64_t)k32 * a.div_group >> 31);
+        const uint32_t at = scale_at + (w < last && (int)(k32 * 32) < a.n_in ? gi * ss : kOOB);
+        raw[f] = SF32 ? (uint32_t)ldb32(b, at) : (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, at, 0, 0);
+      }
 #pragma unroll
-    for (int i = 0; i < SD; ++i) s.v[i] = SF32 ? raw[i] : NS == 1 ? raw[0] : raw[2 * i] | raw[(2 * i + 1) % NS] << 16;
+      for (int i = 0; i < SD; ++i) s.v[i] = SF32 ? raw[i] : NS == 1 ? raw[0] : raw[2 * i] | raw[(2 * i + 1) % NS] << 16;
+    }
   };
   // Lines of 128 bytes are read in two halves, by the same wave or its neighbour: through the caches (streamed past them
   // the same reads came to 5.2 TB/s, through them to 5.6).  Codes behind the row's end, of the next row or zeros behind the
@@ -303,7 +313,7 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
             for (int p = 0; p < P; ++p) {
               const char* at = NT == 1 ? buf + xrow[t] + w * 2 * kWindow + (TR ? f * 64 + g * 16 : g * 64 + f * 16) + p * a.T * stride
                                        : buf + ((w * 4 + f) * P * NT + p * NT + t) * 1024 + lane * 16;
-              x[f & 1][t][p] = bf8(*reinterpret_cast<const uint4*>(at));
+              x[f & 1][t][p] = lds_operand(at);
             }
           }
         };
@@ -319,7 +329,7 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int m = 0; m < M; ++m)
-              if (f % PER == 0) sum[t][m] = starts[f / PER & 1][t];
+              if (f % PER == 0) sum[t][m] = XF32 ? f32x4_t{} : starts[f / PER & 1][t];
 #pragma unroll
           for (int p = P - 1; p >= 0; --p)
 #pragma unroll
@@ -333,7 +343,8 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
 #pragma unroll
               for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][m][i] += cur.sc[u][m].at(s) * sum[t][m][i];
+                for (int i = 0; i < 4; ++i)
+                  acc[t][m][i] += cur.sc[u][m].at(s) * (XF32 ? sum[t][m][i] + starts[s & 1][t][i] : sum[t][m][i]);
               if constexpr (OFF) {
                 const f32x4_t sx = starts[s & 1][t] * (-1.f / 24.f);
 #pragma unroll
@@ -461,10 +472,11 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
       uint4 v[XF32 ? 2 : 1], d[P];
       v[0] = ldb(xb, o);
       if constexpr (XF32) v[1] = ldb(xb, o + 16);
-      const float s = group_sum(split_piece<XF32>(v, d), 4);
+      const float s = XF32 ? split_piece<XF32>(v, d) : group_sum(split_piece<XF32>(v, d), 4);
 #pragma unroll
       for (int q = 0; q < P; ++q) *reinterpret_cast<uint4*>(p + q * plane) = d[q];
-      if ((i & 3) == 0) tab[i >> 2] = -24.f * s;
+      if constexpr (XF32) tab[i] = -24.f * s;  // of every piece: see below
+      else if ((i & 3) == 0) tab[i >> 2] = -24.f * s;
     }
     __syncthreads();
     auto products = [&](const Batch& cur, Batch& nxt) {
@@ -473,7 +485,9 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
       load(first + turn * UNIT, nxt);
       issue_barrier();
       const int w = here + wk;  // the chunk is a multiple of WK
-      const float gone = tab[w * 8 + c];
+      f32x4_t starts{};
+      if constexpr (XF32) starts = reinterpret_cast<const f32x4_t*>(tab)[w * 8 + c];
+      const float gone = XF32 ? (starts[0] + starts[1]) + (starts[2] + starts[3]) : tab[w * 8 + c];
       uint4 x[P][4];
 #pragma unroll
       for (int p = 0; p < P; ++p)
@@ -485,19 +499,27 @@ __global__ __launch_bounds__(512, 4) void k_group_q1(GqArgs a) {
         for (int m = 0; m < M; ++m) {
           const uint4 q = cur.codes[s][m];
           const uint4 d[4] = {codes8(q.x, mask), codes8(q.y, mask), codes8(q.z, mask), codes8(q.w, mask)};
-          float sum = gone;
+          auto dot = [&](float sum, const uint4& l, const uint4& r) {
+            auto two = [&](uint32_t a2, uint32_t b2) {
+              sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, a2), __builtin_bit_cast(bf16x2_t, b2), sum, false);
+            };
+            two(l.x, r.x);
+            two(l.y, r.y);
+            two(l.z, r.z);
+            two(l.w, r.w);
+            return sum;
+          };
+          float sum = XF32 ? 0.f : gone;
 #pragma unroll
-          for (int p = P - 1; p >= 0; --p)
+          for (int p = P - 1; p >= (XF32 ? 1 : 0); --p)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              auto dot = [&](uint32_t l, uint32_t r) {
-                sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, l), __builtin_bit_cast(bf16x2_t, r), sum, false);
-              };
-              dot(d[f].x, x[p][f].x);
-              dot(d[f].y, x[p][f].y);
-              dot(d[f].z, x[p][f].z);
-              dot(d[f].w, x[p][f].w);
-            }
+            for (int f = 0; f < 4; ++f) sum = dot(sum, d[f], x[p][f]);
+          if constexpr (XF32) {
+            // the largest part: eight columns at a time, each sum from its own start, so that no partial sum is larger than those
+            // eight make it (all 32 from one start: 1.3e-6 of the norm, so 6e-7)
+            sum += (dot(starts[0], d[0], x[0][0]) + dot(starts[1], d[1], x[0][1])) +
+                   (dot(starts[2], d[2], x[0][2]) + dot(starts[3], d[3], x[0][3]));
+          }
           acc[s][m] += value(cur.sc[s][m]) * sum;
           if constexpr (OFF) acc[s][m] += value(cur.of[s][m]) * (gone * (-1.f / 24.f));
         }
@@ -568,15 +590,15 @@ hipError_t launch_one(const GqArgs& a, const GqPlan& p, hipStream_t st) {
   return p.wk == 8 ? go(Int<8>{}) : p.wk == 4 ? go(Int<4>{}) : go(Int<2>{});
 }
 
-template <bool XF32, bool SF32, bool GATED, int NS, bool OFF>
+template <bool XF32, bool SF32, bool GATED, int NSX, bool OFF>
 hipError_t launch_tiles(const GqArgs& a, const GqPlan& p, hipStream_t st) {
   const size_t lds = std::max<size_t>(gq_lds(XF32, p, a.T), 8 * (GATED ? 2 : 1) * 1024);
   const dim3 grid(p.blocks, p.shares);
   auto go = [&](auto nt, auto wk, auto u, auto whole) {
-    k_group_q<XF32, SF32, GATED, NS, OFF, nt.value, wk.value, u.value, whole.value><<<grid, 512, lds, st>>>(a);
+    k_group_q<XF32, SF32, GATED, NSX, OFF, nt.value, wk.value, u.value, whole.value><<<grid, 512, lds, st>>>(a);
     return hipGetLastError();
   };
-  constexpr int U = gq_batch(GATED, NS);
+  constexpr int U = gq_batch(GATED, NSX), NS = gq_scales(NSX);
   constexpr Int<0> no;
   constexpr Int<1> yes;
   if (p.whole) {
@@ -599,7 +621,8 @@ hipError_t launch_form(bool sf32, const GqArgs& a, const GqPlan& p, hipStream_t 
     if (p.nt == 0) return launch_one<XF32, s.value, GATED, o.value>(a, p, st);
     return p.ns == 1 ? launch_tiles<XF32, s.value, GATED, 1, o.value>(a, p, st)
            : p.ns == 2 ? launch_tiles<XF32, s.value, GATED, 2, o.value>(a, p, st)
-                       : launch_tiles<XF32, s.value, GATED, 4, o.value>(a, p, st);
+           : p.ns == 4 ? launch_tiles<XF32, s.value, GATED, 4, o.value>(a, p, st)
+                       : launch_tiles<XF32, s.value, GATED, 8, o.value>(a, p, st);
   };
   const bool off = a.w[0].offsets != nullptr;
   const hipError_t e = sf32 ? (off ? by_scales(Int<1>{}, Int<1>{}) : by_scales(Int<1>{}, Int<0>{}))
