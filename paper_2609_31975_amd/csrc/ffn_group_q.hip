@@ -4,6 +4,7 @@
 
 #include "ffn_group_q.h"
 #include "ffn_group_q_internal.h"
+#include "ffn_step_host.h"
 
 namespace ffn {
 

@@ -2,8 +2,9 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
 
-#include "ffn_step_host.h"
 
 namespace ffn {
 

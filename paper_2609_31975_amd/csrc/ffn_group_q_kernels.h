@@ -605,7 +605,11 @@ hipError_t launch_tiles(const GqArgs& a, const GqPlan& p, hipStream_t st) {
     if (p.wk == 8) return go(Int<1>{}, Int<8>{}, Int<U>{}, yes);
     return p.wk == 4 ? go(Int<1>{}, Int<4>{}, Int<U>{}, yes) : go(Int<1>{}, Int<2>{}, Int<U>{}, yes);
   }
-  if (p.nt == 1) return p.wk == 8 ? go(Int<1>{}, Int<8>{}, Int<1>{}, no) : go(Int<1>{}, Int<4>{}, Int<1>{}, no);
+  if (p.nt == 1) {
+    if constexpr (XF32)  // bf16 tokens leave room for 8 waves' windows
+      if (p.wk == 4) return go(Int<1>{}, Int<4>{}, Int<1>{}, no);
+    return go(Int<1>{}, Int<8>{}, Int<1>{}, no);
+  }
   const int windows = ceil_div(a.windows, kGqWaves) * kGqWaves, blocks = ceil_div(a.T * windows * (kWindow / 8), 256);
   if (p.nt == 2) k_group_q_split<XF32, NS, 2><<<blocks, 256, 0, st>>>(a, windows);
   else if (p.nt == 3) k_group_q_split<XF32, NS, 3><<<blocks, 256, 0, st>>>(a, windows);

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ffn_norm.h"
 #include "ffn_step_device.h"
@@ -309,19 +310,11 @@ int back_groups(int T, int d) {
   return std::min(most, ceil_div(T, rows) * rows);
 }
 
-template <bool F32, bool VEC, class F>
+// go(threads, elements) of the plan; the plans of either call are all listed
+template <int TPR, int EPT, int... REST, class F>
 hipError_t with_plan(const NormPlan& p, const F& go) {
-  switch (p.tpr) {
-#define FFN_NORM_CASE(n)                                                              \
-  case n:                                                                             \
-    return p.ept == 8 ? go(std::integral_constant<int, n>{}, std::integral_constant<int, 8>{}) \
-                      : go(std::integral_constant<int, n>{}, std::integral_constant<int, 16>{});
-    FFN_NORM_CASE(64)
-    FFN_NORM_CASE(256)
-    FFN_NORM_CASE(512)
-    FFN_NORM_CASE(1024)
-#undef FFN_NORM_CASE
-  }
+  if (p.tpr == TPR && p.ept == EPT) return go(std::integral_constant<int, TPR>{}, std::integral_constant<int, EPT>{});
+  if constexpr (sizeof...(REST) > 0) return with_plan<REST...>(p, go);
   return hipErrorInvalidValue;
 }
 
@@ -330,7 +323,7 @@ hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
   // Rows that no backward call reads again, or too many to find them in a cache then, are streamed (4096 x 4096 bf16: 39.6
   // us through the caches, 36.7 past them; 513 x 3840 fp32, forward and backward: 3 us more past them).
   const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) >= (int64_t)64 << 20;
-  return with_plan<F32, VEC>(forward_plan(a.d), [&](auto tpr, auto ept) {
+  return with_plan<64, 8, 64, 16, 256, 8, 256, 16, 512, 16, 1024, 16>(forward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     const int blocks = std::min(ceil_div(a.T, ROWS), 1 << 20);
     if (stream) k_norm_fwd<F32, tpr.value, ept.value, VEC, true><<<blocks, WG, 0, st>>>(a);
@@ -340,7 +333,7 @@ hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
 }
 template <bool F32, bool VEC>
 hipError_t launch_bwd(const NormBack& a, int groups, hipStream_t st) {
-  return with_plan<F32, VEC>(backward_plan(a.d), [&](auto tpr, auto ept) {
+  return with_plan<64, 8, 256, 8, 512, 8, 1024, 8, 1024, 16>(backward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     k_norm_bwd<F32, tpr.value, ept.value, VEC><<<groups / ROWS, WG, 0, st>>>(a);
     return hipGetLastError();

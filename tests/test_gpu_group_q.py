@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2609_31975_amd import ffn
+from tests import group_q_cases
 from tests import group_q_ref as ref
 
 pytestmark = pytest.mark.gpu
@@ -193,3 +194,19 @@ def test_binding_refusals():
     with pytest.raises(ffn.FFNError) as e:
         ffn.ffn_group_q_forward(c.x, c.q[0], y, ws[:16])
     assert e.value.code == -5
+
+
+@pytest.mark.parametrize("xf32", [0, 1])
+@pytest.mark.parametrize("gated", [0, 1])
+def test_every_kernel(xf32, gated):
+    """The calls that tests/test_group_q_plans.py finds to reach all of them, scales and offsets of either kind in turn."""
+    for i, (xf, ga, group, T, n_in, n_out) in enumerate(group_q_cases.CASES):
+        if (xf, ga) != (xf32, gated):
+            continue
+        for sdt, offsets in (((BF16, True), (F32, False)) if i % 2 else ((F32, True), (BF16, False))):
+            c = Case(F32 if xf else BF16, T, n_in, n_out, group, sdt, offsets, mats=1 + ga)
+            what = f"{group} T={T} {n_in}x{n_out} {sdt} {offsets}"
+            if ga:
+                c.check_gated(c.run_gated(0.1, 1, True), 0.1, 1, True, what)
+            else:
+                c.check(c.run(), what)

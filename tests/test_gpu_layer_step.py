@@ -1,0 +1,99 @@
+"""The calls around and in place of a block run together, as a layer's step does: the norm before, the experts (or the
+block with 4-bit weights), the norm after with its gate and residual, and the head's product.  Each call is held to 64
+bits on what the one before it wrote; the whole step is captured and replayed."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_31975_amd import ffn
+from tests import group_q_ref, moe_ref, norm_ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class Step:
+    def __init__(self, dtype, T, d, d_ff, E, k, vocab, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed + T + d)
+        rnd = lambda *s, std=1.0, mid=0.0: (torch.randn(*s, generator=gen, device="cuda") * std + mid).to(dtype)
+        self.dtype, self.T, self.d, self.d_ff, self.E, self.k, self.vocab = dtype, T, d, d_ff, E, k, vocab
+        self.x = rnd(T, d, std=2.0)
+        self.g1, self.g2, self.g3, self.gp = (rnd(d, std=0.2, mid=1.0) for _ in range(4))
+        self.gate = rnd(1, d)
+        self.wr = rnd(E, d, std=d ** -0.5)
+        self.w = [rnd(E, d_ff, d, std=d ** -0.5), rnd(E, d_ff, d, std=d ** -0.5), rnd(E, d_ff, d, std=d_ff ** -0.5)]
+        self.q = []
+        for n_in, n_out in ((d, d_ff), (d, d_ff), (d_ff, d), (d, vocab)):
+            self.q.append((torch.randint(0, 256, (n_out, n_in // 2), generator=gen, device="cuda").to(torch.uint8),
+                           torch.randn(n_out, n_in // 32, generator=gen, device="cuda").abs() * 0.3 * n_in ** -0.5, None))
+        self.mats = [ffn.group_q(*q) for q in self.q]
+        self.first = ffn.norm(1e-5, pre_gain=self.g1)
+        self.between = ffn.norm(1e-5, pre_gain=self.g2, post=True, post_gain=self.gp, gate=self.gate, gate_sigmoid=True)
+        self.last = ffn.norm(1e-5, pre_gain=self.g3)
+        self.router = ffn.router(E, k, w=self.wr, sigmoid=True)
+        self.opt = ffn.options(act=ffn.FFN_ACT_SILU)
+        e = lambda *s, dt=dtype: torch.full(s, math.nan, dtype=dt, device="cuda")
+        self.b = {n: e(T, d) for n in ("n1", "f1", "x1", "n2", "f2", "x2", "n3")}
+        self.b.update(z=e(T, d_ff), logits=e(T, vocab), weights=e(T, k, dt=F32),
+                      ids=torch.full((T, k), -1, dtype=torch.int32, device="cuda"))
+        self.moe_ws = ffn.alloc_moe_workspace(T, d, d_ff, E, k, dtype)
+        self.q_ws = max((ffn.alloc_group_q_workspace(T, n_in, n_out, gated) for n_in, n_out, gated in
+                         ((d, d_ff, True), (d_ff, d, False), (d, vocab, False))), key=lambda w: w.numel())
+
+    def run(self):
+        b = self.b
+        ffn.ffn_norm_forward(self.x, None, self.first, None, b["n1"])
+        ffn.ffn_moe_forward(b["n1"], self.router, *self.w, 0.0, self.opt, b["ids"], b["weights"], b["f1"], self.moe_ws)
+        ffn.ffn_norm_forward(self.x, b["f1"], self.between, b["x1"], b["n2"])
+        ffn.ffn_group_q_gated_forward(b["n2"], self.mats[0], self.mats[1], 0.1, self.opt, b["z"], self.q_ws)
+        ffn.ffn_group_q_forward(b["z"], self.mats[2], b["f2"], self.q_ws)
+        ffn.ffn_norm_forward(b["x1"], b["f2"], self.last, b["x2"], b["n3"])
+        ffn.ffn_group_q_forward(b["n3"], self.mats[3], b["logits"], self.q_ws)
+        return {n: v.clone() for n, v in b.items()}
+
+    def check(self, o):
+        dt, form = self.dtype, norm_ref.Form
+        n1 = norm_ref.forward(self.x, None, form(pre_gain=self.g1))
+        norm_ref.check(o["n1"], n1["n_out"], n1["e_n_out"], dt, "n1")
+        ids, weights = moe_ref.route(o["n1"], self.wr, None, self.k, True, True, 1.0)
+        assert torch.equal(o["ids"], ids)
+        moe_ref.check(o["f1"], *moe_ref.experts(o["n1"], *self.w, 0.0, 2, False, o["ids"], o["weights"]), dt, "experts")
+        n2 = norm_ref.forward(self.x, o["f1"], form(pre_gain=self.g2, post=True, post_gain=self.gp, gate=self.gate, sigmoid=True))
+        norm_ref.check(o["x1"], n2["x_out"], n2["e_x_out"], dt, "x1")
+        norm_ref.check(o["n2"], n2["n_out"], n2["e_n_out"], dt, "n2")
+        h, v = (group_q_ref.product(o["n2"], *self.q[i]) for i in (0, 1))
+        group_q_ref.check(o["z"], *group_q_ref.gated(2, False, 0.1, *h, *v), dt, "z")
+        group_q_ref.check(o["f2"], *group_q_ref.product(o["z"], *self.q[2]), dt, "f2")
+        n3 = norm_ref.forward(o["x1"], o["f2"], form(pre_gain=self.g3))
+        norm_ref.check(o["x2"], n3["x_out"], n3["e_x_out"], dt, "x2")
+        norm_ref.check(o["n3"], n3["n_out"], n3["e_n_out"], dt, "n3")
+        group_q_ref.check(o["logits"], *group_q_ref.product(o["n3"], *self.q[3]), dt, "logits")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1, 5, 30])
+def test_a_layers_step(dtype, T):
+    step = Step(dtype, T, 544, 416, 12, 3, 1001)
+    step.check(step.run())
+
+
+@pytest.mark.parametrize("T", [1, 24])
+def test_captured_steps(T):
+    """Replays on changing tokens, the eager step between them on the same buffers and workspaces."""
+    step, other = Step(BF16, T, 256, 320, 8, 2, 500), Step(BF16, T, 256, 320, 8, 2, 500, seed=9)
+    eager = step.run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.run()
+    first, want = step.x.clone(), {}
+    for turn in range(4):
+        step.x.copy_(other.x if turn % 2 else first)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: v.clone() for n, v in step.b.items()}
+        now = step.run()
+        assert all(torch.equal(got[n], now[n]) for n in now), turn
+        if turn % 2 == 0:
+            assert all(torch.equal(got[n], eager[n]) for n in eager), turn

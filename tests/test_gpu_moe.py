@@ -53,7 +53,10 @@ class Layer:
 
 SHAPES = [(1, 8, 1, 1, 1), (1, 64, 96, 8, 2), (1, 256, 1000, 64, 8), (2, 40, 33, 3, 3), (3, 1032, 31, 16, 4), (5, 33, 100, 7, 2),
           (7, 100, 64, 65, 5), (8, 520, 200, 200, 8), (9, 128, 257, 12, 12), (16, 2048, 64, 4, 1), (17, 192, 320, 5, 3),
-          (33, 264, 96, 512, 16), (64, 72, 160, 16, 6), (65, 136, 40, 2, 2), (256, 64, 48, 9, 4), (1, 4096, 130, 2, 2), (20, 31, 7, 6, 6)]
+          (33, 264, 96, 512, 16), (64, 72, 160, 16, 6), (65, 136, 40, 2, 2), (256, 64, 48, 9, 4), (1, 4096, 130, 2, 2), (20, 31, 7, 6, 6),
+          # narrow and misaligned rows with more token tiles, the logits of many tokens and experts, the choice of a few tokens
+          (40, 33, 20, 2, 2), (24, 40, 33, 3, 2), (3, 33, 20, 5, 2), (2, 64, 32, 512, 16), (40, 64, 32, 130, 4), (30, 33, 16, 200, 3),
+          (4, 40, 48, 100, 3), (32, 96, 40, 4, 3)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
