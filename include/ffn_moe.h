@@ -20,9 +20,8 @@
  * w_down_t [experts][d_ff][d], ids int32 and weights fp32 [T][k] (4-byte aligned), bias [experts] (4-byte aligned).
  * Any d and d_ff; rows that are not whole 16-byte chunks take narrower loads.
  *
- * Ownership, streams, errors: as in ffn_sparse.h.  The workspace is zero-filled once before its
- * first use, and every call leaves it ready for the next one, of any shape that fits; a call that returned
- * FFN_ERR_HIP may leave it unusable until it is zero-filled again.  Outputs overlap nothing.
+ * Ownership, streams, errors: as in ffn_sparse.h.  The workspace needs no initialisation, holds nothing
+ * from one call to the next, and serves calls of fewer tokens too.  Outputs overlap nothing.
  *
  * Determinism: results are bit-reproducible (no floating-point atomic adds).
  *

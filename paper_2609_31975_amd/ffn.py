@@ -1,4 +1,4 @@
-"""Thin ctypes binding of ``include/ffn_sparse.h`` (argument marshalling only).
+"""Thin ctypes binding of the headers in ``include/`` (argument marshalling only).
 
 Every function takes torch device tensors, checks the dtypes, shapes and devices the
 C ABI cannot see (it receives bare pointers and sizes), and passes raw device pointers
@@ -865,9 +865,8 @@ def router(experts, k, w=None, bias=None, sigmoid=False, normalize=True, scale=1
 
 
 def alloc_moe_workspace(T, d, d_ff, experts, k, dtype, device="cuda"):
-    """A zero-filled workspace (the header asks for zeros before the first call)."""
     return _bytes(int(lib().ffn_moe_workspace_bytes(_type_of(dtype), T, d, d_ff, experts, k)), "ffn_moe_workspace_bytes",
-                  device).zero_()
+                  device)
 
 
 def ffn_moe_forward(x, router, w_gate, w_up, w_down_t, t, opt, ids, weights, y, ws, stream=None):

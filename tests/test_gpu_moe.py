@@ -28,7 +28,7 @@ class Layer:
         self.weights = torch.randn((T, k), generator=gen, device="cuda") if given else None
 
     def ws(self):
-        return ffn.alloc_moe_workspace(self.T, self.d, self.d_ff, self.E, self.k, self.dtype)
+        return torch.full_like(ffn.alloc_moe_workspace(self.T, self.d, self.d_ff, self.E, self.k, self.dtype), 0xFF)
 
     def run(self, t=0.25, kind=2, silu=False, ws=None, out=None, x=None, **kw):
         x = self.x if x is None else x
@@ -126,11 +126,12 @@ def test_equal_scores_go_to_the_lower_index():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_a_tokens_experts_do_not_depend_on_its_batch(dtype):
-    layer = Layer(dtype, 37, 1000, 32, 100, 6, sigmoid=True, bias=True)
-    _, ids, weights = layer.run()
-    for i in (0, 7, 8, 36):
-        _, one, w = layer.run(x=layer.x[i:i + 1].clone())
-        assert torch.equal(one[0], ids[i]) and torch.equal(w[0], weights[i])
+    for T in (37, 50):    # a wave computes the logits of one token, or of eight
+        layer = Layer(dtype, T, 1000, 32, 100, 6, sigmoid=True, bias=True)
+        _, ids, weights = layer.run()
+        for i in (0, 7, 8, T - 1):
+            _, one, w = layer.run(x=layer.x[i:i + 1].clone())
+            assert torch.equal(one[0], ids[i]) and torch.equal(w[0], weights[i])
 
 
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
