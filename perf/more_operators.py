@@ -294,7 +294,7 @@ def _kept(s):
     k, x, T = {}, s["x"], s["tokens"]
     if s["op"].startswith("norm"):
         k["norm"] = ffn.norm(EPS, pre_gain=s["pre_gain"], post=s["post"], post_gain=s["post_gain"], gate=s["gate_in"],
-                             gate_sigmoid=s["sigmoid"], alpha=s["alpha"])
+                             gate_sigmoid=s["sigmoid"] and s["gate_in"] is not None, alpha=s["alpha"])
         k["x_out"], k["n_out"] = torch.empty_like(x), torch.empty_like(x)
         if s["op"] == "norm_train":
             k["rstd"] = torch.empty((2, T), dtype=torch.float32, device="cuda")
