@@ -51,10 +51,14 @@ struct MoeArgs {
 };
 
 // A 16-byte chunk's worth of elements from element i on, `left` of them there: one load, or narrower ones.  VEC: 2, rows are
-// whole lines of 128 bytes (weights are streamed past the caches); 1, whole chunks; 0, neither.
+// whole lines of 128 bytes (weights are streamed past the caches); 1, whole chunks; 3, rows start at whole dwords, which
+// is all that a 16-byte load needs, but end inside a chunk; 0, bf16 rows of odd length.
 template <bool F32, int VEC, bool WEIGHTS = false>
 __device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
-  if constexpr (VEC) {
+  if constexpr (VEC == 3) {
+    if (left >= (F32 ? 4 : 8)) return ldb(b, i * (F32 ? 4u : 2u));
+    return ld_chunk<F32, 0>(b, i, left);
+  } else if constexpr (VEC) {
     const uint32_t o = left > 0 ? i * (F32 ? 4u : 2u) : kOOB;
     return WEIGHTS && VEC == 2 ? ldb_nt(b, o) : ldb(b, o);
   } else if constexpr (F32) {
@@ -323,7 +327,7 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) 
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int r = (n & 7) + 8 * h;
-          w[q + h][m] = ld_chunk<F32, VEC, true>(wb[m], (uint32_t)r * a.d + k, VEC || r < rows ? left : 0);
+          w[q + h][m] = ld_chunk<F32, VEC, true>(wb[m], (uint32_t)r * a.d + k, (VEC && VEC != 3) || r < rows ? left : 0);
         }
     }
   };
@@ -438,7 +442,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
     const Buf wb = make_buf(wbase + (size_t)s * 32 * a.d * es, rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if constexpr (VEC != 0) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
+      if constexpr (VEC == 1 || VEC == 2) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
       else w[j] = ld_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
     }
   };
@@ -650,12 +654,11 @@ int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t*
                     w.logits, ids, weights};
   const MoeArgs a{T, d, d_ff, E, k, moe_ldz(d_ff), moe_slots(T, E, k), moe_pieces(f32, T, d, d_ff, E, k),
                   x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, w.part, y};
-  // rows of whole lines, of whole chunks, of neither
-  const int vec = d % (f32 ? 32 : 64) == 0 ? 2 : d % (f32 ? 4 : 8) == 0 ? 1 : 0;
-  auto go = [&](auto f) {
-    return vec == 2 ? launch_moe<f.value, 2>(r, a, stream) : vec ? launch_moe<f.value, 1>(r, a, stream) : launch_moe<f.value, 0>(r, a, stream);
-  };
-  const hipError_t e = f32 ? go(Int<1>{}) : go(Int<0>{});
+  const bool lines = d % (f32 ? 32 : 64) == 0, chunks = d % (f32 ? 4 : 8) == 0;
+  hipError_t e;
+  if (f32) e = lines ? launch_moe<true, 2>(r, a, stream) : chunks ? launch_moe<true, 1>(r, a, stream) : launch_moe<true, 3>(r, a, stream);
+  else e = lines ? launch_moe<false, 2>(r, a, stream) : chunks ? launch_moe<false, 1>(r, a, stream)
+         : d % 2 == 0 ? launch_moe<false, 3>(r, a, stream) : launch_moe<false, 0>(r, a, stream);
   return e == hipSuccess ? FFN_OK : FFN_ERR_HIP;
 }
 

@@ -56,7 +56,10 @@ SHAPES = [(1, 8, 1, 1, 1), (1, 64, 96, 8, 2), (1, 256, 1000, 64, 8), (2, 40, 33,
           (33, 264, 96, 512, 16), (64, 72, 160, 16, 6), (65, 136, 40, 2, 2), (256, 64, 48, 9, 4), (1, 4096, 130, 2, 2), (20, 31, 7, 6, 6),
           # narrow and misaligned rows with more token tiles, the logits of many tokens and experts, the choice of a few tokens
           (40, 33, 20, 2, 2), (24, 40, 33, 3, 2), (3, 33, 20, 5, 2), (2, 64, 32, 512, 16), (40, 64, 32, 130, 4), (30, 33, 16, 200, 3),
-          (4, 40, 48, 100, 3), (32, 96, 40, 4, 3)]
+          (4, 40, 48, 100, 3), (32, 96, 40, 4, 3),
+          # rows that end inside a chunk: even and odd lengths, one token to four tiles, logits of many
+          (1, 1716, 200, 8, 3), (3, 10, 40, 4, 2), (20, 602, 70, 6, 5), (52, 130, 64, 2, 2), (40, 350, 20, 110, 2), (7, 2, 9, 3, 1),
+          (2, 803, 60, 5, 2)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
