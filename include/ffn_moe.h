@@ -18,7 +18,8 @@
  *
  * Layouts: row-major device pointers, 16-byte aligned: x, y [T][d], w_router [experts][d], w_gate, w_up,
  * w_down_t [experts][d_ff][d], ids int32 and weights fp32 [T][k] (4-byte aligned), bias [experts] (4-byte aligned).
- * Any d and d_ff; rows that are not whole 16-byte chunks take narrower loads.
+ * Any d and d_ff.  bf16 rows of odd length take narrow loads and are several times slower; other rows that are not whole
+ * 16-byte chunks are somewhat slower (those of whole 128-byte lines are fastest).
  *
  * Ownership, streams, errors: as in ffn_sparse.h.  The workspace needs no initialisation, holds nothing
  * from one call to the next, and serves calls of fewer tokens too.  Outputs overlap nothing.
@@ -26,8 +27,8 @@
  * Determinism: results are bit-reproducible (no floating-point atomic adds).
  *
  * Special values: an Inf or NaN of a token stays in that token's y and weights; its experts are then k different ones
- * with no further meaning.  A NaN score counts as the lowest.  Experts that no token chose are not read.  A NaN gate
- * value behaves as in ffn_gated.h.
+ * with no further meaning.  A NaN score counts as the lowest.  An expert's weights reach
+ * the tokens that chose it alone.  A NaN gate value behaves as in ffn_gated.h.
  */
 #ifndef FFN_MOE_H
 #define FFN_MOE_H

@@ -22,7 +22,7 @@
  *
  * Layouts: row-major device pointers, 16-byte aligned: x, f, x_out, n_out and their gradients
  * [T][d], gains [d], the gate [1][d] or [T][d].  Any d up to 16384; d not a multiple of 8 (bf16) or 4
- * (fp32) takes narrower loads.
+ * (fp32) takes 16-byte loads too, but for the chunk that a row ends in, and is slower for it.
  *
  * Ownership, streams, errors: as in ffn_sparse.h.  x_out may be x itself, and dx may be
  * dx_out; outputs otherwise overlap nothing.  The backward call's workspace needs no

@@ -71,9 +71,6 @@ __device__ __forceinline__ uint4 ld_chunk(const Buf& b, uint32_t i, int left) {
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
   }
 }
-__device__ __forceinline__ uint4 ldb_nt(const Buf& b, uint32_t off, uint32_t uniform_off) {
-  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b.r, off, uniform_off, 2));
-}
 // ------------------------------------------------------------------ the router
 template <int CTRL>
 __device__ __forceinline__ double dpp_move64(double v) {
@@ -442,7 +439,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
     const Buf wb = make_buf(wbase + (size_t)s * 32 * a.d * es, rows > 0 ? (uint32_t)(rows * a.d * es) : 0u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if constexpr (VEC == 1 || VEC == 2) w[j] = ldb_nt(wb, vo, (uint32_t)(j * a.d * es));
+      // the whole offset in the lane's: a wave's own, behind the buffer's end, is no part of the bounds that are checked
+      if constexpr (VEC == 1 || VEC == 2) w[j] = ldb_nt(wb, vo + (uint32_t)(j * a.d * es));
       else w[j] = ld_chunk<F32, VEC>(wb, (uint32_t)(g * 8 + j) * a.d + col, g * 8 + j < rows ? a.d - col : 0);
     }
   };

@@ -161,6 +161,22 @@ def test_unused_experts_are_not_read():
     assert torch.equal(layer.run()[0], y)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 136, 38, 33])
+@pytest.mark.parametrize("d_ff", [33, 47, 1, 16])
+def test_rows_behind_an_expert_s_last_are_not_read(dtype, d, d_ff):
+    """The next expert's rows, where a step of 32 neurons or a tile of 16 ends behind the expert's own."""
+    for T in (2, 20):
+        layer = Layer(dtype, T, d, d_ff, 4, 1, given=True)
+        layer.ids.copy_(torch.arange(T)[:, None] % 2 * 2)
+        out = layer.run()
+        layer.check(out)
+        want = out[0].clone()
+        for w in layer.w:
+            w[1], w[3] = math.nan, math.inf
+        assert torch.equal(layer.run()[0], want)
+
+
 def test_nan_weights_reach_their_experts_tokens_alone():
     layer = Layer(BF16, 10, 64, 40, 5, 1)
     y, ids, _ = layer.run()
