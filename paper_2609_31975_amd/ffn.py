@@ -257,6 +257,15 @@ def _raw_stream(stream, x):
     return _stream(stream, x.device).value
 
 
+def _own_stream(stream, x):
+    """_raw_stream of a call whose tensors lie on the current device: the default stream is that device's, and a kernel on it
+    would reach for another one's memory."""
+    here = _torch()._C._cuda_getDevice()
+    if x.get_device() != here:
+        raise ValueError(f"x is on device {x.get_device()}, the current device is {here}")
+    return _raw_stream(stream, x)
+
+
 def workspace_bytes(T: int, d: int, d_ff: int, r: int = 0) -> int:
     return int(lib().ffn_workspace_bytes(T, d, d_ff, r))
 
@@ -743,7 +752,7 @@ def ffn_norm_forward(x, f, form, x_out, n_out, rstd=None, stream=None):
     _check_rstd(rstd, T, dev)
     form.check(x, d, dev)
     rc = _function("ffn_norm_forward")(dt, T, d, x.data_ptr(), _p(f), form.ref, _p(x_out), _p(n_out), _p(rstd),
-                                       _raw_stream(stream, x))
+                                       _own_stream(stream, x))
     _check("ffn_norm_forward", rc)
     return x_out, n_out
 
@@ -769,7 +778,7 @@ def ffn_norm_backward(x_out, f, form, rstd, dn, dx_out, ws, dx=None, df=None, dg
     form.check(like, d, dev)
     rc = _function("ffn_norm_backward")(dt, T, d, _p(x_out), _p(f), form.ref, _p(rstd), _p(dn),
                                         _p(dx_out), _p(dx), _p(df), _p(dgate), _p(dpost_gain), _p(dpre_gain),
-                                        ws.data_ptr(), _size(ws), _raw_stream(stream, like))
+                                        ws.data_ptr(), _size(ws), _own_stream(stream, like))
     _check("ffn_norm_backward", rc)
     return dx, df, dgate, dpost_gain, dpre_gain
 
@@ -824,7 +833,7 @@ def ffn_group_q_forward(x, w, y, ws, stream=None):
     args = _group_q_args(x, (w,), y)
     _check_buffers(x.get_device(), (ws, "ws"))
     rc = _function("ffn_group_q_forward")(*args, x.data_ptr(), w.ref, y.data_ptr(), ws.data_ptr(),
-                                          _size(ws), _raw_stream(stream, x))
+                                          _size(ws), _own_stream(stream, x))
     _check("ffn_group_q_forward", rc)
     return y
 
@@ -835,7 +844,7 @@ def ffn_group_q_gated_forward(x, w_gate, w_up, t, opt, z, ws, stream=None):
     _check_buffers(x.get_device(), (ws, "ws"))
     rc = _function("ffn_group_q_gated_forward")(*args, x.data_ptr(), w_gate.ref, w_up.ref,
                                                 ctypes.c_float(t), _opt(opt), z.data_ptr(), ws.data_ptr(), _size(ws),
-                                                _raw_stream(stream, x))
+                                                _own_stream(stream, x))
     _check("ffn_group_q_gated_forward", rc)
     return z
 
@@ -888,7 +897,7 @@ def ffn_moe_forward(x, router, w_gate, w_up, w_down_t, t, opt, ids, weights, y, 
     _check_buffers(dev, (ws, "ws"))
     rc = _function("ffn_moe_forward")(wdt, T, d, d_ff, router.ref, x.data_ptr(), w_gate.data_ptr(),
                                       w_up.data_ptr(), w_down_t.data_ptr(), ctypes.c_float(t), _opt(opt), ids.data_ptr(),
-                                      weights.data_ptr(), y.data_ptr(), ws.data_ptr(), _size(ws), _raw_stream(stream, x))
+                                      weights.data_ptr(), y.data_ptr(), ws.data_ptr(), _size(ws), _own_stream(stream, x))
     _check("ffn_moe_forward", rc)
     return y
 

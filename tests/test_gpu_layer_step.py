@@ -2,6 +2,7 @@
 block with 4-bit weights), the norm after with its gate and residual, and the head's product.  Each call is held to 64
 bits on what the one before it wrote; the whole step is captured and replayed."""
 import math
+import types
 
 import pytest
 import torch
@@ -97,3 +98,10 @@ def test_captured_steps(T):
         assert all(torch.equal(got[n], now[n]) for n in now), turn
         if turn % 2 == 0:
             assert all(torch.equal(got[n], eager[n]) for n in eager), turn
+
+
+def test_tensors_of_another_device_are_refused():
+    """The calls launch on the current device."""
+    x = types.SimpleNamespace(get_device=lambda: torch.cuda.current_device() + 1)
+    with pytest.raises(ValueError, match="current device"):
+        ffn._own_stream(None, x)
