@@ -30,41 +30,45 @@ struct NormArgs {
 typedef uint32_t any4_t __attribute__((ext_vector_type(4), aligned(2)));
 
 // The elements of a row that a thread holds: 16-byte chunks, a row's chunks dealt out over its threads.  VEC: rows
-// are whole chunks.  Otherwise a row starts anywhere, and the chunk that it ends in goes by elements (4096 rows of 4097
-// bf16: 56 us, all of it by elements 133, rows of 4096 30; forward and backward 164, 600 and 95).
+// are whole chunks, and a row is a buffer, behind whose end loads give zeros and stores nothing (with compares of
+// each element and 64-bit addresses instead, the vector ALUs were busy for 87% of 8192 x 8192's forward call).
+// Otherwise a row starts anywhere, and the chunk that it ends in goes by elements (4096 rows of 4097 bf16: 56 us, all of
+// it by elements 133, rows of 4096 30; forward and backward 164, 600 and 95).
 template <bool F32, int TPR, int EPT, bool VEC>
 struct Part {
-  static constexpr int E = F32 ? 4 : 8, N = EPT / E;
+  static constexpr int E = F32 ? 4 : 8, N = EPT / E, ES = F32 ? 4 : 2;
   static __device__ __forceinline__ int at(int t, int i) { return (i * TPR + t) * E; }
 
   static __device__ __forceinline__ float element(const void* p, int64_t o) {
     return F32 ? static_cast<const float*>(p)[o] : bf_to_f(static_cast<const uint16_t*>(p)[o]);
   }
+  // row: the same for a wave
   template <bool STREAM = false>
   static __device__ __forceinline__ void load(const void* p, int64_t row, int d, int t, float (&v)[EPT]) {
     uint4 c[N];
+    if constexpr (VEC) {
+      const Buf b = make_buf(static_cast<const char*>(p) + row * d * ES, (uint32_t)d * ES);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int e = at(t, i);
-      const int64_t o = row * d + (e < d ? e : 0);
-      const char* at = static_cast<const char*>(p) + o * (F32 ? 4 : 2);
-      if constexpr (VEC) {
-        c[i] = STREAM ? ld_weights(reinterpret_cast<const uint4*>(at)) : *reinterpret_cast<const uint4*>(at);
-      } else {
+      for (int i = 0; i < N; ++i) c[i] = STREAM ? ldb_nt(b, (uint32_t)at(t, i) * ES) : ldb(b, (uint32_t)at(t, i) * ES);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int e = at(t, i);
+        const char* from = static_cast<const char*>(p) + (row * d + (e < d ? e : 0)) * ES;
         any4_t u = {0, 0, 0, 0};
-        if (e + E <= d) u = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const any4_t*>(at)) : *reinterpret_cast<const any4_t*>(at);
+        if (e + E <= d) u = STREAM ? __builtin_nontemporal_load(reinterpret_cast<const any4_t*>(from)) : *reinterpret_cast<const any4_t*>(from);
         c[i] = make_uint4(u[0], u[1], u[2], u[3]);
       }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = at(t, i);
       float u[E];
       if constexpr (F32) unpack(WF32{}, c[i], u);
       else unpack(WBf16{}, c[i], u);
 #pragma unroll
-      for (int j = 0; j < E; ++j) v[i * E + j] = e < d ? u[j] : 0.f;
+      for (int j = 0; j < E; ++j) v[i * E + j] = u[j];
       if constexpr (!VEC) {
+        const int e = at(t, i);
         if (e < d && e + E > d) {
 #pragma unroll
           for (int j = 0; j < E - 1; ++j)
@@ -77,20 +81,19 @@ struct Part {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int e = at(t, i);
-      if (e >= d) continue;
-      const int64_t o = row * d + e;
       any4_t w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (F32) w[j] = __float_as_uint(v[i * 4 + j]);
         else w[j] = f_to_bf2(v[i * 8 + 2 * j], v[i * 8 + 2 * j + 1]);
       }
-      char* to = static_cast<char*>(p) + o * (F32 ? 4 : 2);
       if constexpr (VEC) {
-        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+        const Buf b = make_buf(static_cast<const char*>(p) + row * d * ES, (uint32_t)d * ES);
+        __builtin_amdgcn_raw_buffer_store_b128(w, b.r, (uint32_t)e * ES, 0, 0);
       } else if (e + E <= d) {
-        *reinterpret_cast<any4_t*>(to) = w;
-      } else {
+        *reinterpret_cast<any4_t*>(static_cast<char*>(p) + (row * d + e) * ES) = w;
+      } else if (e < d) {
+        const int64_t o = row * d + e;
 #pragma unroll
         for (int j = 0; j < E - 1; ++j) {
           if (e + j >= d) continue;
@@ -101,6 +104,19 @@ struct Part {
     }
   }
 };
+
+// sigma(c) = 1 / (1 + 2^(-c log2 e)), the exponent in two parts and the quotient with a step of Newton's: within 3 units in
+// the last place, at half of what expf and a division cost.  NaN stays NaN.  |c| up to 88, behind which sigma is 0 or
+// 1 to fp32's range.
+__device__ __forceinline__ float sigma(float c) {
+  c = c > 88.f ? 88.f : c;
+  c = c < -88.f ? -88.f : c;
+  constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f;  // log2 e = their sum
+  const float p = -c * kLog2e, rest = fmaf(-c, kLog2e, -p) - c * kRest;
+  const float e = __builtin_amdgcn_exp2f(p), a = 1.f + fmaf(e, rest * 0.693147181f, e);
+  const float r = __builtin_amdgcn_rcpf(a);
+  return fmaf(fmaf(-a, r, 1.f), r, r);
+}
 
 // Sum over the threads of a row.  `room`: TPR / 64 floats of LDS that no earlier sum of the same row used, and none
 // that is still being read: the sums of a row use rooms of their own, and each row's first barrier lies between
@@ -125,7 +141,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
   __shared__ float room[2][2][16];
   const int t = threadIdx.x % TPR;
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + uniform(threadIdx.x / TPR); row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
     float x[EPT], u[EPT], c[EPT];
     P::template load<STREAM>(a.x, row, a.d, t, x);
     if (a.f) {
@@ -147,8 +163,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
         }
       }
       if (a.gate_rows) {
+        if (a.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) u[i] *= a.sigmoid ? 1.f / (1.f + expf(-c[i])) : c[i];
+          for (int i = 0; i < EPT; ++i) c[i] = sigma(c[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) u[i] *= c[i];
       }
 #pragma unroll
       for (int i = 0; i < EPT; ++i) x[i] = a.alpha * x[i] + u[i];
@@ -160,10 +180,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
       for (int i = 0; i < EPT; ++i) s += x[i] * x[i];
       const float r = 1.f / sqrtf(row_sum<TPR>(s, room[turn][1]) / (float)a.d + a.eps);
       if (t == 0 && a.rstd) a.rstd[(int64_t)a.T + row] = r;
-      float w[EPT];
-      if (a.pre_gain) P::load(a.pre_gain, 0, a.d, t, w);
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) x[i] *= a.pre_gain ? r * w[i] : r;
+      for (int i = 0; i < EPT; ++i) x[i] *= r;
+      if (a.pre_gain) {
+        float w[EPT];
+        P::load(a.pre_gain, 0, a.d, t, w);
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) x[i] *= w[i];
+      }
       P::store(a.n_out, row, a.d, t, x);
     }
   }
@@ -187,7 +211,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_nor
   constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
   __shared__ float room[2][2][16];
   const int t = threadIdx.x % TPR;
-  const int64_t group = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const int64_t group = (int64_t)blockIdx.x * ROWS + uniform(threadIdx.x / TPR);
   float sp[EPT] = {}, so[EPT] = {}, sg[EPT] = {};
   const bool block_side = a.f && (a.df || a.dgate || a.part[1] || a.part[2]);
   int turn = 0;
@@ -206,12 +230,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_nor
       const float r = a.rstd[(int64_t)a.T + row];
       float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        xh[i] *= r;
-        if (a.part[0]) sp[i] += n[i] * xh[i];
-        if (a.pre_gain) n[i] *= w[i];
-        s += n[i] * xh[i];
+      for (int i = 0; i < EPT; ++i) xh[i] *= r;
+      if (a.part[0]) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) sp[i] += n[i] * xh[i];
       }
+      if (a.pre_gain) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) n[i] *= w[i];
+      }
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) s += n[i] * xh[i];
       const float m = row_sum<TPR>(s, room[turn][0]) / (float)a.d;
 #pragma unroll
       for (int i = 0; i < EPT; ++i) {
@@ -239,23 +268,28 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_nor
     if (a.gate_rows) {
       float dg[EPT];
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        float slope = 1.f;
-        if (a.sigmoid) {
-          c[i] = 1.f / (1.f + expf(-c[i]));
-          slope = c[i] * (1.f - c[i]);
+      for (int i = 0; i < EPT; ++i) dg[i] = g[i] * (f[i] * w[i]);
+      if (a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) {
+          c[i] = sigma(c[i]);
+          dg[i] *= c[i] * (1.f - c[i]);
         }
-        dg[i] = g[i] * (f[i] * w[i]) * slope;
-        if (a.part[2]) sg[i] += dg[i];
-        g[i] *= c[i];
       }
+      if (a.part[2]) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) sg[i] += dg[i];
+      }
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) g[i] *= c[i];
       if (a.dgate && a.gate_rows != 1) P::store(a.dgate, row, a.d, t, dg);
     }
     if (a.post) {
       float s = 0.f;
 #pragma unroll
+      for (int i = 0; i < EPT; ++i) so[i] += g[i] * f[i];  // a sum that is not wanted is not stored
+#pragma unroll
       for (int i = 0; i < EPT; ++i) {
-        if (a.part[1]) so[i] += g[i] * f[i];
         g[i] *= w[i];
         s += g[i] * f[i];
       }

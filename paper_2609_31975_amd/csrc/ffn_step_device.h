@@ -9,7 +9,12 @@ namespace {
 
 __device__ __forceinline__ float bf_to_f(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ uint16_t f_to_bf(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-__device__ __forceinline__ uint32_t f_to_bf2(float lo, float hi) { return (uint32_t)f_to_bf(lo) | (uint32_t)f_to_bf(hi) << 16; }
+__device__ __forceinline__ uint32_t f_to_bf2(float lo, float hi) {
+  typedef float f2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+  const f2_t v = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2_t));
+}
 
 template <bool F32>
 __device__ __forceinline__ void store_as(void* p, size_t i, float v) {
