@@ -5,7 +5,6 @@
 #include <stddef.h>
 #include <stdint.h>
 
-
 namespace ffn {
 
 constexpr int kWindow = 128;                // codes of a row that four lanes load at once
@@ -37,7 +36,6 @@ struct GqArgs {
 constexpr int gq_scales(int nsx) { return nsx == 8 ? 4 : nsx; }
 // Windows of a wave in a batch, where the next batch's registers fit beside it.
 constexpr int gq_batch(bool gated, int ns) { return gated || ns > 1 ? 1 : 2; }
-
 
 // Waves that share a row tile's windows with two tiles of tokens and more
 constexpr int kGqWaves = 2;

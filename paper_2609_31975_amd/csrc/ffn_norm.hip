@@ -133,7 +133,8 @@ __device__ __forceinline__ float row_sum(float v, float* room) {
   return s;
 }
 
-// STREAM: rows are read past the caches.
+// STREAM: rows are read past the caches.  Bound by bytes: 4096 x 4096 bf16 with a gate for each token, 168 MB, 32 us (5.2
+// TB/s); 8192 x 8192, 671 MB, 109 us (6.2 TB/s); one token 3.3 us, the loads' latency twice and two sums.
 template <bool F32, int TPR, int EPT, bool VEC, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) {
   using P = Part<F32, TPR, EPT, VEC>;
@@ -204,7 +205,9 @@ struct NormBack {
   float* part[3];          // [groups][d] of dpre_gain, dpost_gain, dgate of one row; null: not wanted
 };
 
-// One group of threads takes every groups-th row and keeps its columns' sums over them in registers.
+// One group of threads takes every groups-th row and keeps its columns' sums over them in registers.  Bound by bytes: 8192 x
+// 8192 bf16 with a gate for each token reads five rows and writes three, 1.07 GB, in 252 us (4.3 TB/s); a row's two means
+// leave its loads waiting for the row before (those of the next row a row early, in two sets of registers, spill).
 template <bool F32, int TPR, int EPT, bool VEC>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_norm_bwd(NormBack a) {
   using P = Part<F32, TPR, EPT, VEC>;
@@ -316,6 +319,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_nor
 
 // out[i] [d] = sum over the groups' rows of part[i], in a fixed order: 16 threads to a column take every
 // 16th row each, and one joins them.
+// Latency: 512 rows of 8192, two sums 8 us, of 3840, three 5 us.
 constexpr int kSumLoads = 8;
 struct NormSums {
   int groups, d;
@@ -359,7 +363,7 @@ NormPlan forward_plan(int d) {
   return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
 }
 // The backward call holds six rows and up to three sums: 8 elements to a thread leave room for twice the waves (8192 x 8192
-// bf16: 282 us with 16, so 273).
+// bf16: 256 us with 16, so 252).
 NormPlan backward_plan(int d) {
   const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
   return NormPlan{tpr, d <= 8192 ? 8 : 16};
@@ -381,8 +385,9 @@ hipError_t with_plan(const NormPlan& p, const F& go) {
 
 template <bool F32, bool VEC>
 hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
-  // Rows that no backward call reads again, or too many to find them in a cache then, are streamed (4096 x 4096 bf16: 39.6
-  // us through the caches, 36.7 past them; 513 x 3840 fp32, forward and backward: 3 us more past them).
+  // Rows that no backward call reads again, or too many to find them in a cache then, are streamed (4096 x 4096 bf16: 35.7
+  // us through the caches, 32.4 past them, 5.2 TB/s; 8192 x 8192 118 and 108; 513 x 3840 fp32, forward and backward: 3 us
+  // more past them).
   const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) >= (int64_t)64 << 20;
   return with_plan<64, 8, 64, 16, 256, 8, 256, 16, 512, 16, 1024, 16>(forward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
