@@ -206,7 +206,7 @@ struct NormBack {
 };
 
 // One group of threads takes every groups-th row and keeps its columns' sums over them in registers.  Bound by bytes: 8192 x
-// 8192 bf16 with a gate for each token reads five rows and writes three, 1.07 GB, in 252 us (4.3 TB/s); a row's two means
+// 8192 bf16 with a gate for each token reads five rows and writes three, 1.07 GB, in 250 us (4.3 TB/s); a row's two means
 // leave its loads waiting for the row before (those of the next row a row early, in two sets of registers, spill).
 template <bool F32, int TPR, int EPT, bool VEC>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_norm_bwd(NormBack a) {
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_nor
 
 // out[i] [d] = sum over the groups' rows of part[i], in a fixed order: 16 threads to a column take every
 // 16th row each, and one joins them.
-// Latency: 512 rows of 8192, two sums 8 us, of 3840, three 5 us.
+// Latency: 256 rows of 8192, two sums 5 us, 257 of 3840, three 4 us.
 constexpr int kSumLoads = 8;
 struct NormSums {
   int groups, d;
@@ -368,11 +368,13 @@ NormPlan backward_plan(int d) {
   const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
   return NormPlan{tpr, d <= 8192 ? 8 : 16};
 }
-// Rows in flight in the backward call, and so rows of the partial sums: what the card holds at once.
+// Rows in flight in the backward call, and so rows of the partial sums: what the card holds at once (8192 x 8192 bf16: twice
+// as many 309 us forward and backward, so 292).  Of more than 128 wide rows no more than leave every group two: the partial
+// sums are read and written once more (300 x 8192 bf16: 49 us with a row each, so 33; 40 x 6000 23 with two, so 21).
 int back_groups(int T, int d) {
   const NormPlan p = backward_plan(d);
-  const int most = p.tpr == 64 ? 2048 : p.tpr == 256 ? 1024 : 512, rows = p.tpr == 64 ? 4 : 1;
-  return std::min(most, ceil_div(T, rows) * rows);
+  if (p.tpr == 64) return std::min(2048, ceil_div(T, 4) * 4);
+  return std::min(p.tpr == 256 ? 1024 : p.tpr == 512 ? 512 : 256, std::max(ceil_div(T, 2), std::min(T, 128)));
 }
 
 // go(threads, elements) of the plan; the plans of either call are all listed

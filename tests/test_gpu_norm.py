@@ -70,7 +70,9 @@ class Layer:
 # rows of one element, of a wave, behind each border of threads and elements a row, that end inside a chunk
 SIZES = [(1, 1), (3, 8), (5, 7), (64, 512), (9, 520), (2, 1024), (3, 1025), (7, 2048), (2, 2056), (4, 4096), (3, 4100), (2, 8192),
          (3, 8200), (2, 9999), (2, 16384), (1, 16383), (777, 264), (2050, 24), (1030, 1032)] + [(5, 1024 + i) for i in range(2, 8)] + \
-    [(4, 2), (6, 511), (3, 2047), (5, 4095), (3, 8191), (700, 1001)]
+    [(4, 2), (6, 511), (3, 2047), (5, 4095), (3, 8191), (700, 1001),
+     # one row a group, two, more than are in flight at once
+     (128, 2056), (129, 4104), (300, 4104), (1025, 520), (2049, 1040), (515, 8192)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
