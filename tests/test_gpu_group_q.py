@@ -210,3 +210,18 @@ def test_every_kernel(xf32, gated):
                 c.check_gated(c.run_gated(0.1, 1, True), 0.1, 1, True, what)
             else:
                 c.check(c.run(), what)
+
+
+def test_two_calls_at_once():
+    """Two streams with workspaces of their own; more tokens than a pass takes."""
+    cases = [Case(F32, T, 1024, 300, 64, BF16, True) for T in (40, 130)]
+    want = [c.run().clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        outs = []
+        for c, st in zip(cases, streams):
+            with torch.cuda.stream(st):
+                outs.append(c.run())
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))

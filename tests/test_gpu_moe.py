@@ -269,3 +269,19 @@ def test_binding_refusals():
     with pytest.raises(ffn.FFNError) as e:
         call(ws=ws[:256])
     assert e.value.code == -5
+
+
+def test_experts_past_32_bits():
+    """An expert whose matrices lie past 2^32 bytes is what it is alone."""
+    E, d, d_ff = 40, 4096, 14336
+    one = Layer(BF16, 3, d, d_ff, 1, 1, given=True)
+    one.ids.fill_(0)
+    want = one.run()[0].clone()
+    stacks = []
+    for w in one.w:
+        stacks.append(torch.zeros((E, d_ff, d), dtype=BF16, device="cuda"))
+        stacks[-1][E - 1] = w[0]
+    one.router, one.E, one.w = ffn.router(E, 1), E, stacks
+    one.ids.fill_(E - 1)
+    got = one.run()[0]
+    assert torch.equal(got, want)

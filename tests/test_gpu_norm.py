@@ -235,3 +235,61 @@ def test_binding_refusals():
     with pytest.raises(ffn.FFNError) as e:
         call(form=ffn.norm(-1.0))
     assert e.value.code == -7
+
+
+def test_rows_past_32_bits():
+    """Rows whose offsets pass 2^32 bytes are what they are alone; so are their gradients."""
+    T, d, few = 131080, 8200, 5
+    big = torch.zeros((T, d), dtype=F32, device="cuda")
+    layer = Layer(F32, few, d, post=True, gains=True, gate="row", sigmoid=True)
+    want = layer.run()
+
+    def wide(v):
+        o = big.clone()
+        o[-few:] = v
+        return o
+    x, f, dn, dxo = (wide(v) for v in (layer.x, layer.f, layer.dn, layer.dxo))
+    x_out, n_out = torch.empty_like(big), torch.empty_like(big)
+    rstd = torch.empty((2, T), dtype=F32, device="cuda")
+    ffn.ffn_norm_forward(x, f, layer.form, x_out, n_out, rstd)
+    ffn.ffn_norm_backward(x_out, f, layer.form, rstd, dn, dxo, ffn.alloc_norm_workspace(T, d), dx=x, df=big)
+    for got, name in ((x_out, "x_out"), (n_out, "n_out"), (x, "dx"), (big, "df")):
+        assert torch.equal(got[-few:], want[name]), name
+        assert not bool(got[:-few].any()), name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,d", [(3, 8), (5, 33), (2, 1032), (3, 1001), (1, 4095), (2, 5000), (1, 16383)])
+def test_what_lies_behind_the_rows_stays(dtype, T, d):
+    layer = Layer(dtype, T, d, **KINDS["token"])
+    want = layer.run()
+
+    def room(like):
+        o = torch.full((like.numel() + 4096,), 7.0, dtype=like.dtype, device="cuda")
+        return o, o[:like.numel()].view(like.shape)
+    rooms = {n: room(want[n]) for n in want}
+    v = {n: r[1] for n, r in rooms.items()}
+    ffn.ffn_norm_forward(layer.x, layer.f, layer.form, v["x_out"], v["n_out"], v["rstd"])
+    names = [n for n in want if n.startswith("d")]
+    ffn.ffn_norm_backward(v["x_out"], layer.f, layer.form, v["rstd"], layer.dn, layer.dxo, ffn.alloc_norm_workspace(T, d),
+                          **{n: v[n] for n in names})
+    for n, (whole, got) in rooms.items():
+        assert torch.equal(got, want[n]), n
+        assert bool((whole[got.numel():] == 7).all()), n
+
+
+def test_two_calls_at_once():
+    """Two streams with workspaces of their own."""
+    layers = [Layer(BF16, 600, 2056, **KINDS["row"], seed=s) for s in (0, 1)]
+    want = [layer.run() for layer in layers]
+    streams = [torch.cuda.Stream() for _ in layers]
+    spaces = [ffn.alloc_norm_workspace(600, 2056) for _ in layers]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        outs = []
+        for layer, st, ws in zip(layers, streams, spaces):
+            with torch.cuda.stream(st):
+                outs.append(layer.run(ws=ws))
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert all(torch.equal(out[n], w[n]) for n in w)
