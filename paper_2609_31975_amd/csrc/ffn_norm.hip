@@ -32,8 +32,8 @@ typedef uint32_t any4_t __attribute__((ext_vector_type(4), aligned(2)));
 // The elements of a row that a thread holds: 16-byte chunks, a row's chunks dealt out over its threads.  VEC: rows
 // are whole chunks, and a row is a buffer, behind whose end loads give zeros and stores nothing (with compares of
 // each element and 64-bit addresses instead, the vector ALUs were busy for 87% of 8192 x 8192's forward call).
-// Otherwise a row starts anywhere, and the chunk that it ends in goes by elements (4096 rows of 4097 bf16: 56 us, all of
-// it by elements 133, rows of 4096 30; forward and backward 164, 600 and 95).
+// Otherwise a row starts anywhere, and the chunk that it ends in goes by elements (4096 rows of 4097 bf16: 51 us, all of
+// it by elements 133, rows of 4096 29; forward and backward 157, 600 and 92).
 template <bool F32, int TPR, int EPT, bool VEC>
 struct Part {
   static constexpr int E = F32 ? 4 : 8, N = EPT / E, ES = F32 ? 4 : 2;
