@@ -287,14 +287,21 @@ def _options(s):
                        silu_up=s["silu_up"])
 
 
+def _norm_form(s):
+    from paper_2609_31975_amd import ffn
+
+    return ffn.norm(EPS, pre_gain=s["pre_gain"], post=s["post"], post_gain=s["post_gain"], gate=s["gate_in"],
+                    gate_sigmoid=s["sigmoid"] and s["gate_in"] is not None, alpha=s["alpha"])
+
+
 def _kept(s):
-    """Buffers, options and descriptors that a program makes once."""
+    """Buffers, options and descriptors that a program makes once.  A gate of each token is a step's own input: the form that
+    holds it is made with the call."""
     from paper_2609_31975_amd import ffn
 
     k, x, T = {}, s["x"], s["tokens"]
     if s["op"].startswith("norm"):
-        k["norm"] = ffn.norm(EPS, pre_gain=s["pre_gain"], post=s["post"], post_gain=s["post_gain"], gate=s["gate_in"],
-                             gate_sigmoid=s["sigmoid"] and s["gate_in"] is not None, alpha=s["alpha"])
+        k["norm"] = None if s["gate"] == "token" else _norm_form(s)
         k["x_out"], k["n_out"] = torch.empty_like(x), torch.empty_like(x)
         if s["op"] == "norm_train":
             k["rstd"] = torch.empty((2, T), dtype=torch.float32, device="cuda")
@@ -326,10 +333,11 @@ def _own(s):
         s["kept"] = _kept(s)
     k = s["kept"]
     if s["op"].startswith("norm"):
-        ffn.ffn_norm_forward(s["x"], s["f"], k["norm"], k["x_out"], k["n_out"], rstd=k.get("rstd"))
+        form = k["norm"] or _norm_form(s)
+        ffn.ffn_norm_forward(s["x"], s["f"], form, k["x_out"], k["n_out"], rstd=k.get("rstd"))
         out = {"x_out": k["x_out"], "n_out": k["n_out"]}
         if s["op"] == "norm_train":
-            ffn.ffn_norm_backward(k["x_out"], s["f"], k["norm"], k["rstd"], s["dn"], s["dx_out"], k["ws"], **k["grads"])
+            ffn.ffn_norm_backward(k["x_out"], s["f"], form, k["rstd"], s["dn"], s["dx_out"], k["ws"], **k["grads"])
             out.update((n, v) for n, v in k["grads"].items() if v is not None)
         return out
     if s["op"] == "q4":
