@@ -1,0 +1,43 @@
+"""Products with group scales of tokens of one sign, whose sums do not cancel: what the codes' offset of 24 adds to a group's
+sum is then many times the result.
+
+Bound, in U = 2^-24: a group's sum is K = 9 group additions at most ((24 + code) x and -24 x, in three parts each, and the
+table's), each off by U of a partial sum that is at most A = 31 sum |x| over the group; 8 + 3 sqrt(K) of them are more than five
+deviations of their sum (group_q_ref).  Groups are independent: the root of the sum of (scale A)^2.  The scaled groups and
+offsets are added in chains of at most G = 3 groups + 64 additions, waves and shares included, of partial sums of at most
+the sum of the terms' sizes."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_31975_amd import ffn
+from tests import group_q_ref as ref
+from tests.test_gpu_group_q import BF16, F32, Case
+
+pytestmark = pytest.mark.gpu
+
+
+def bound(x, codes, scales, offsets):
+    c, x = ref.codes_of(codes), x.double()
+    groups = scales.shape[1]
+    g = c.shape[1] // groups
+    s = scales.double()
+    o = torch.zeros_like(s) if offsets is None else offsets.double()
+    a = 31 * x.abs().view(-1, groups, g).sum(2)                                   # [T][groups]
+    w = s.repeat_interleave(g, dim=1) * c + o.repeat_interleave(g, dim=1)
+    size = x.abs() @ w.abs().t() + x.abs() @ o.abs().repeat_interleave(g, dim=1).t()
+    inner = (8 + 3 * math.sqrt(9 * g)) * torch.sqrt((a * a) @ (s * s + o * o).t())
+    return x @ w.t(), ref.U * (inner + (3 * groups + 64) * size)
+
+
+@pytest.mark.parametrize("xdt", [BF16, F32])
+@pytest.mark.parametrize("T", [1, 3, 16, 40, 64])
+@pytest.mark.parametrize("n_in,group", [(1280, 32), (2304, 128), (1152, 96), (4096, 4096)])
+def test_tokens_of_one_sign(xdt, T, n_in, group):
+    for offsets in (False, True):
+        c = Case(xdt, T, n_in, 333, group, offsets=offsets, mats=2)
+        c.x = (c.x.abs() + 0.5).to(xdt)
+        h = bound(c.x, *c.w[0])
+        ref.check(c.run(), *h, xdt, f"offsets={offsets}")
+        ref.check(c.run_gated(0.1, 2, False), *ref.gated(2, False, 0.1, *h, *bound(c.x, *c.w[1])), xdt, f"gated offsets={offsets}")
