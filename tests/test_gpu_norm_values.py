@@ -1,0 +1,35 @@
+"""Values at which the norms' arithmetic is hardest: gates that saturate."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_31975_amd import ffn
+from tests import norm_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+U = ref.U
+
+
+@pytest.mark.parametrize("gate_rows", [1, 2])
+def test_the_gate_s_slope_where_it_saturates(gate_rows):
+    """dgate = dx_out f sigma (1 - sigma), relative to itself however small 1 - sigma is (no norms: G is dx_out, u is f).
+
+    Roundings, in U = 2^-24: 2^(-g log2 e) 2 (one unit in the last place) and 1 for its rest, so 3 in 1 - sigma's numerator; the
+    denominator at most as many and its own, 4; the quotient's reciprocal and Newton step 2; so sigma 6, 1 - sigma (numerator
+    times it) 3 + 6 + 1, their product 17, f dx_out 1, the last product 1: 19.  Products below 2^-126 are rounded to a multiple of 2^-149, by
+    half of that.  One row: a sum of one token, exact."""
+    d = 4096
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    T = gate_rows
+    gate = torch.linspace(-80, 80, T * d, device="cuda").view(T, d)
+    f, dxo = (torch.randn((T, d), generator=gen, device="cuda") for _ in range(2))
+    form = ffn.norm(1e-5, gate=gate, gate_sigmoid=True)
+    dgate = torch.full_like(gate, math.nan)
+    ffn.ffn_norm_backward(None, f, form, None, None, dxo, ffn.alloc_norm_workspace(T, d), dgate=dgate)
+    g = gate.double()
+    want = dxo.double() * f.double() * torch.sigmoid(g) * torch.sigmoid(-g)
+    over = (dgate.double() - want).abs() - (20 * U * want.abs() + 2.0 ** -150)
+    k = int(over.argmax())
+    assert float(over.max()) <= 0, (float(g.flatten()[k]), float(dgate.flatten()[k]), float(want.flatten()[k]))
