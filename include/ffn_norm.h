@@ -31,6 +31,9 @@
  * Determinism: results are bit-reproducible (no atomic adds; sums over tokens are joined in a fixed
  * order that depends on T and d alone).
  *
+ * Range: rows of any finite values are normed, also those whose squares pass fp32's range.  r is fp32: below 2^-126 (rows
+ * of more than 2^126) with fewer bits.  Squares below 2^-126 are held to multiples of 2^-149, which only an eps of that size shows.
+ *
  * Special values: an Inf or NaN of a token stays in that token's outputs, dx, df and dgate rows; it
  * reaches the gradients that are summed over tokens.
  */

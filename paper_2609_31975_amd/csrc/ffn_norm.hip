@@ -137,13 +137,32 @@ __device__ __forceinline__ float row_sum(float v, float* room) {
   return s;
 }
 
+// 1 / sqrt(mean v^2 + eps) of a row.  `room`: two of row_sum's, the second for a row whose sum of squares passes fp32's range
+// (values of 2^57 and more): its values times 2^-80, of squares from 2^-46 to 2^96.  A row that holds an Inf keeps it.  The
+// branch is the same for all threads of a row.
+template <int TPR, int EPT>
+__device__ __forceinline__ float row_rms(const float (&v)[EPT], int d, float eps, float (*room)[16]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPT; ++i) s += v[i] * v[i];
+  s = row_sum<TPR>(s, room[0]);
+  if (s == INFINITY) {
+    constexpr float kDown = 0x1p-80f;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) s += (v[i] * kDown) * (v[i] * kDown);
+    return kDown / sqrtf(row_sum<TPR>(s, room[1]) / (float)d + eps * kDown * kDown);
+  }
+  return 1.f / sqrtf(s / (float)d + eps);
+}
+
 // STREAM: rows are read past the caches.  Bound by bytes: 4096 x 4096 bf16 with a gate for each token, 168 MB, 32 us (5.2
 // TB/s); 8192 x 8192, 671 MB, 109 us (6.2 TB/s); one token 3.3 us, the loads' latency twice and two sums.
 template <bool F32, int TPR, int EPT, bool VEC, bool STREAM>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) {
   using P = Part<F32, TPR, EPT, VEC>;
   constexpr int WG = TPR < 256 ? 256 : TPR, ROWS = WG / TPR;
-  __shared__ float room[2][2][16];
+  __shared__ float room[2][4][16];
   const int t = threadIdx.x % TPR;
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + uniform(threadIdx.x / TPR); row < a.T; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
@@ -153,10 +172,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
       P::template load<STREAM>(a.f, row, a.d, t, u);
       if (a.gate_rows) P::template load<STREAM>(a.gate, a.gate_rows == 1 ? 0 : row, a.d, t, c);
       if (a.post) {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) s += u[i] * u[i];
-        const float r = 1.f / sqrtf(row_sum<TPR>(s, room[turn][0]) / (float)a.d + a.eps);
+        const float r = row_rms<TPR>(u, a.d, a.eps, room[turn]);
         if (t == 0 && a.rstd) a.rstd[row] = r;
 #pragma unroll
         for (int i = 0; i < EPT; ++i) u[i] *= r;
@@ -180,10 +196,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_fwd(NormArgs a) 
     }
     if (a.x_out) P::store(a.x_out, row, a.d, t, x);
     if (a.n_out) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) s += x[i] * x[i];
-      const float r = 1.f / sqrtf(row_sum<TPR>(s, room[turn][1]) / (float)a.d + a.eps);
+      const float r = row_rms<TPR>(x, a.d, a.eps, room[turn] + 2);
       if (t == 0 && a.rstd) a.rstd[(int64_t)a.T + row] = r;
 #pragma unroll
       for (int i = 0; i < EPT; ++i) x[i] *= r;
