@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "ffn_norm.h"
+#include "ffn_norm_internal.h"
 #include "ffn_step_device.h"
 
 namespace ffn {
@@ -373,28 +374,6 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormSums a) {
   }
 }
 
-struct NormPlan {
-  int tpr, ept;
-};
-NormPlan forward_plan(int d) {
-  const int tpr = d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
-  return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
-}
-// The backward call holds six rows and up to three sums: 8 elements to a thread leave room for twice the waves (8192 x 8192
-// bf16: 256 us with 16, so 252).
-NormPlan backward_plan(int d) {
-  const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
-  return NormPlan{tpr, d <= 8192 ? 8 : 16};
-}
-// Rows in flight in the backward call, and so rows of the partial sums: what the card holds at once (8192 x 8192 bf16: twice
-// as many 309 us forward and backward, so 292).  Of more than 128 wide rows no more than leave every group two: the partial
-// sums are read and written once more (300 x 8192 bf16: 49 us with a row each, so 33; 40 x 6000 23 with two, so 21).
-int back_groups(int T, int d) {
-  const NormPlan p = backward_plan(d);
-  if (p.tpr == 64) return std::min(2048, ceil_div(T, 4) * 4);
-  return std::min(p.tpr == 256 ? 1024 : p.tpr == 512 ? 512 : 256, std::max(ceil_div(T, 2), std::min(T, 128)));
-}
-
 // go(threads, elements) of the plan; the plans of either call are all listed
 template <int TPR, int EPT, int... REST, class F>
 hipError_t with_plan(const NormPlan& p, const F& go) {
@@ -409,9 +388,9 @@ hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
   // us through the caches, 32.4 past them, 5.2 TB/s; 8192 x 8192 118 and 108; 513 x 3840 fp32, forward and backward: 3 us
   // more past them).
   const bool stream = !a.rstd || (int64_t)a.T * a.d * (F32 ? 4 : 2) >= (int64_t)64 << 20;
-  return with_plan<64, 8, 64, 16, 256, 8, 256, 16, 512, 16, 1024, 16>(forward_plan(a.d), [&](auto tpr, auto ept) {
-    constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
-    const int blocks = std::min(ceil_div(a.T, ROWS), 1 << 20);
+  return with_plan<64, 8, 64, 16, 256, 8, 256, 16, 512, 16, 1024, 16>(norm_forward_plan(a.d), [&](auto tpr, auto ept) {
+    constexpr int WG = tpr.value < 256 ? 256 : tpr.value;
+    const int blocks = norm_blocks(a.T, a.d);
     if (stream) k_norm_fwd<F32, tpr.value, ept.value, VEC, true><<<blocks, WG, 0, st>>>(a);
     else k_norm_fwd<F32, tpr.value, ept.value, VEC, false><<<blocks, WG, 0, st>>>(a);
     return hipGetLastError();
@@ -419,7 +398,7 @@ hipError_t launch_fwd(const NormArgs& a, hipStream_t st) {
 }
 template <bool F32, bool VEC>
 hipError_t launch_bwd(const NormBack& a, int groups, hipStream_t st) {
-  return with_plan<64, 8, 256, 8, 512, 8, 1024, 8, 1024, 16>(backward_plan(a.d), [&](auto tpr, auto ept) {
+  return with_plan<64, 8, 256, 8, 512, 8, 1024, 8, 1024, 16>(norm_backward_plan(a.d), [&](auto tpr, auto ept) {
     constexpr int WG = tpr.value < 256 ? 256 : tpr.value, ROWS = WG / tpr.value;
     k_norm_bwd<F32, tpr.value, ept.value, VEC><<<groups / ROWS, WG, 0, st>>>(a);
     return hipGetLastError();
@@ -442,6 +421,27 @@ int check_norm_form(const ffn_norm_t* n, int T, bool f) {
 }
 
 }  // namespace
+
+NormPlan norm_forward_plan(int d) {
+  const int tpr = d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024;
+  return NormPlan{tpr, d <= tpr * 8 ? 8 : 16};
+}
+// The backward call holds six rows and up to three sums: 8 elements to a thread leave room for twice the waves (8192 x 8192
+// bf16: 256 us with 16, so 252).
+NormPlan norm_backward_plan(int d) {
+  const int tpr = d <= 512 ? 64 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024;
+  return NormPlan{tpr, d <= 8192 ? 8 : 16};
+}
+int norm_blocks(int T, int d) { return std::min(ceil_div(T, norm_forward_plan(d).tpr == 64 ? 4 : 1), 1 << 20); }
+// Rows in flight in the backward call: what the card holds at once (8192 x 8192 bf16: twice as many 309 us forward and
+// backward, so 292).  Of more than 128 wide rows no more than leave every group two: the partial sums are read and written
+// once more (300 x 8192 bf16: 49 us with a row each, so 33; 40 x 6000 23 with two, so 21).
+int norm_groups(int T, int d) {
+  const NormPlan p = norm_backward_plan(d);
+  if (p.tpr == 64) return std::min(512, ceil_div(T, 4)) * 4;
+  return std::min(p.tpr == 256 ? 1024 : p.tpr == 512 ? 512 : 256, std::max(ceil_div(T, 2), std::min(T, 128)));
+}
+
 }  // namespace ffn
 
 using namespace ffn;
@@ -466,7 +466,7 @@ int ffn_norm_forward(ffn_dtype_t dt, int T, int d, const void* x, const void* f,
 size_t ffn_norm_workspace_bytes(int T, int d) {
   if (check_norm_shape(T, d) != FFN_OK) return 0;
   Carver c{nullptr};
-  for (int i = 0; i < 3; ++i) c.take(sizeof(float) * back_groups(T, d) * (size_t)d);
+  for (int i = 0; i < 3; ++i) c.take(sizeof(float) * norm_groups(T, d) * (size_t)d);
   return c.off;
 }
 
@@ -485,7 +485,7 @@ int ffn_norm_backward(ffn_dtype_t dt, int T, int d, const void* x_out, const voi
   if ((dn && !x_out) || ((dn || form->post) && !rstd)) return FFN_ERR_NULL;
   if (ws_bytes < ffn_norm_workspace_bytes(T, d)) return FFN_ERR_WORKSPACE;
 
-  const int groups = back_groups(T, d);
+  const int groups = norm_groups(T, d);
   Carver c{static_cast<char*>(ws)};
   float* room[3];
   for (float*& p : room) p = static_cast<float*>(c.take(sizeof(float) * groups * (size_t)d));

@@ -15,8 +15,8 @@ constexpr int64_t kMaxElems = (int64_t)1 << 31;
 inline bool aligned(const void* p, uintptr_t a = 16) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool known(ffn_dtype_t w) { return w == FFN_F32 || w == FFN_BF16; }
 template <class T>
-T ceil_div(T a, T b) {
-  return (a + b - 1) / b;
+T ceil_div(T a, T b) {  // a up to the type's largest
+  return a / b + (a % b != 0);
 }
 
 struct Carver {
