@@ -1,5 +1,5 @@
-// Host side of include/ffn_group_q.h: argument checks, the choice of tiles, one launch for 64 tokens (two where
-// the windows go in shares).  No allocation, no synchronization.
+// Host side of include/ffn_group_q.h: argument checks, the choice of tiles, the launches for 64 tokens: the products, before
+// them x taken apart (17 tokens and more), behind them a join (windows in shares).  No allocation, no synchronization.
 #include <algorithm>
 
 #include "ffn_group_q.h"
@@ -66,6 +66,12 @@ int check_gq_shape(int T, int n_in, int n_out) {
   if ((int64_t)T * n_in >= kMaxElems || (int64_t)T * n_out >= kMaxElems || (int64_t)n_in * n_out >= kMaxElems) return FFN_ERR_SHAPE;
   return FFN_OK;
 }
+// Rows of partial sums a token and matrix, shares x n_out at most whatever T: gq_plan makes shares only of rows for half the
+// card's workgroups or fewer (512 of 32 rows at most, or 256 of 64), and no more of them than fill it.
+constexpr size_t kGqShareRows = 512 * 32;
+size_t gq_share_rows(int n_out) {
+  return 2 * (size_t)n_out <= kGqShareRows ? std::min(kGqSharesMost * (size_t)n_out, kGqShareRows) : 0;
+}
 // A pass's shares, and x in parts with the table of its sums: every region grows with T.
 struct GqWs {
   float* part;
@@ -77,7 +83,7 @@ GqWs gq_layout(int T, int n_in, int n_out, bool gated, void* base) {
   const size_t tokens = std::min(T, kGqTokens), columns = (size_t)ceil_div(n_in, kGqWaves * kWindow) * kGqWaves * kWindow;
   Carver c{static_cast<char*>(base)};
   GqWs w;
-  w.part = static_cast<float*>(c.take(sizeof(float) * kGqSharesMost * (gated ? 2 : 1) * tokens * n_out));
+  w.part = static_cast<float*>(c.take(sizeof(float) * (gated ? 2 : 1) * tokens * gq_share_rows(n_out)));
   w.planes = static_cast<uint4*>(c.take(3 * 2 * ceil_div<size_t>(tokens, 16) * 16 * columns));
   w.sums = static_cast<float*>(c.take(sizeof(float) * columns / 32 * kGqTokens));
   w.bytes = c.off;
