@@ -24,7 +24,7 @@ HEADERS = [os.path.join(ROOT, "include", h) for h in ("ffn_sparse.h", "ffn_lopa_
                                                        "ffn_norm.h", "ffn_group_q.h", "ffn_moe.h")] + \
     [os.path.join(PKG, "csrc", f) for f in ("ffn_internal.h", "ffn_device.h", "ffn_mfma.h", "ffn_gemm.h",
                                                "ffn_gemm_host.h", "ffn_gated_internal.h", "ffn_step_host.h",
-                                               "ffn_step_device.h", "ffn_norm_internal.h", "ffn_group_q_internal.h",
+                                               "ffn_step_device.h", "ffn_norm_internal.h", "ffn_moe_internal.h", "ffn_group_q_internal.h",
                                                "ffn_group_q_kernels.h")]
 LIB = os.path.join(PKG, "libffn_sparse.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -16,13 +16,14 @@
 
 #include "ffn_mfma.h"
 #include "ffn_moe.h"
+#include "ffn_moe_internal.h"
 #include "ffn_step_device.h"
 
 namespace ffn {
 namespace {
 
 constexpr int kMoeTokens = 256, kMoeK = 16, kMoeExperts = 512;
-constexpr int kPiecesMost = 8;   // of an expert's neurons
+constexpr int kDownGroups = 1024;  // workgroups of k_moe_down, where the neurons go in pieces to come to so many
 constexpr int kRouteTokens = 8;  // tokens of a wave that computes logits
 constexpr int kChooseTokens = 4; // tokens that k_moe_hidden chooses for itself: a wave each
 
@@ -539,11 +540,11 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs a) {
     const int p = t * a.k + j, e = uniform(a.ids[p]);
     if (e < 0 || e >= a.E || c >= a.d) continue;
     const float w = a.weights[p];
-    float v[kPiecesMost];
+    float v[kMoePieces];
 #pragma unroll
-    for (int s = 0; s < kPiecesMost; ++s) v[s] = s < a.pieces ? a.part[(s * rows + p) * a.d + c] : 0.f;
+    for (int s = 0; s < kMoePieces; ++s) v[s] = s < a.pieces ? a.part[(s * rows + p) * a.d + c] : 0.f;
 #pragma unroll
-    for (int s = 1; s < kPiecesMost; ++s) v[0] += v[s];
+    for (int s = 1; s < kMoePieces; ++s) v[0] += v[s];
     y += w * v[0];
   }
   red[wave][lane] = y;
@@ -552,15 +553,6 @@ __global__ __launch_bounds__(256) void k_moe_join(MoeArgs a) {
 }
 
 // ------------------------------------------------------------------ host side
-int moe_slots(int T, int E, int k) { return std::min(T * k, E); }
-int moe_ldz(int d_ff) { return ceil_div(d_ff, 32) * 32; }
-// Pieces of the neurons: enough workgroups for the card, each with a step of 32 for every wave.
-int moe_pieces(bool f32, int T, int d, int d_ff, int E, int k) {
-  const int64_t blocks = (int64_t)moe_slots(T, E, k) * ceil_div(d, f32 ? 64 : 128);
-  const int64_t want = std::min<int64_t>(ceil_div<int64_t>(1024, blocks), moe_ldz(d_ff) / 128);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, kPiecesMost));
-}
-
 struct MoeWs {
   double* logits;
   void* z;
@@ -571,7 +563,7 @@ size_t moe_layout(bool f32, int T, int d, int d_ff, int E, int k, void* base, Mo
   MoeWs w;
   w.logits = static_cast<double*>(c.take(sizeof(double) * T * E));
   w.z = c.take((size_t)(f32 ? 4 : 2) * T * k * moe_ldz(d_ff));
-  w.part = static_cast<float*>(c.take(sizeof(float) * kPiecesMost * T * k * (size_t)d));
+  w.part = static_cast<float*>(c.take(sizeof(float) * moe_part_rows(f32, T, d, d_ff, E, k) * (size_t)d));
   if (out) *out = w;
   return c.off;
 }
@@ -620,6 +612,23 @@ hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+int moe_slots(int T, int E, int k) { return std::min(T * k, E); }
+int moe_ldz(int d_ff) { return ceil_div(d_ff, 32) * 32; }
+// Enough workgroups for the card, each with a step of 32 for every wave.
+static int moe_groups(bool f32, int d) { return ceil_div(kDownGroups, ceil_div(d, f32 ? 64 : 128)); }
+static int moe_pieces_most(int d_ff) { return std::max(1, std::min(moe_ldz(d_ff) / 128, kMoePieces)); }
+int moe_pieces(bool f32, int T, int d, int d_ff, int E, int k) {
+  return std::min(ceil_div(moe_groups(f32, d), moe_slots(T, E, k)), moe_pieces_most(d_ff));
+}
+// With g groups to find and s slots, pieces = ceil(g / s): up to E places, places times pieces are s + g - 1 at most; with more of
+// them pieces stay what they are with E slots.
+size_t moe_part_rows(bool f32, int T, int d, int d_ff, int E, int k) {
+  const size_t places = (size_t)T * k, slots = moe_slots(T, E, k);
+  const size_t few = std::min(slots * moe_pieces_most(d_ff), slots + moe_groups(f32, d) - 1);
+  return std::max(few, places > slots ? places * moe_pieces(f32, T, d, d_ff, E, k) : 0);
+}
+
 }  // namespace ffn
 
 using namespace ffn;
