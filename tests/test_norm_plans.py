@@ -7,6 +7,7 @@ import subprocess
 import pytest
 
 from paper_2609_31975_amd import ffn
+from tests import norm_chains
 from tests.test_gated_launches import compile_driver
 
 MOST = (1 << 31) - 1        # T d of a call
@@ -37,6 +38,7 @@ def test_every_row_has_a_group_and_every_grid_is_one_that_hip_takes(tmp_path):
         assert blocks == 1 << 20 or blocks * rows >= T, what
         assert blocks * max(tpr, 256) < 1 << 32, what
         assert 1 <= groups <= 2048 and groups % (4 if b_tpr == 64 else 1) == 0 and groups < T + 4, what
+        assert groups == norm_chains.groups(T, d), what
 
 
 def test_workspaces_of_the_most_rows():
