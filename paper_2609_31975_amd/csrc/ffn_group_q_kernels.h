@@ -5,8 +5,11 @@
 //   - The codes enter the bf16 products unscaled.  Two nibbles of a dword become two bf16 of value 24 + code (16 + u has
 //     u in its top mantissa bits; u = code + 8): 8 operations for 8 codes.  What the 24 add, 24 times the sum of the
 //     same x, is in a table in LDS that the sums start from.  A group's sum is then multiplied by its row's scale.
-//     (fp32 x: sums start from zero with the least of the three parts, and the table's value is added last.  What the 24 add
-//     is several times the result, and every addition beside it rounds by that.)
+//     One fp32 token: a table of every eight columns' sums, see k_group_q1.
+//   - More fp32 tokens: the codes enter as code / 16, exactly, from a conversion of nibbles (19 operations for 8 codes), and the
+//     16 comes off the joined sums.  With 24 in them a group's sums are several times the result, for x of one sign many times,
+//     and every addition rounds by that (4096 columns of one sign: 3.0e-6 of the result's norm, so 1.1e-7, a plain fp32 product 4.8e-7; 48
+//     tokens of 4096 -> 14336 twice, groups of 64 with offsets: 60 us, so 61; 16 tokens, groups of 128: 31, so 35).
 //   - One token: dot products on the vector ALUs (k_group_q1).  More: v_mfma_f32_16x16x32_bf16 (k_group_q).
 //   - Tokens are the A operand, weight rows the B operand: a lane's results are of one weight row, whose scale it
 //     holds.
@@ -39,6 +42,12 @@ __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70
 __device__ __forceinline__ uint4 codes8(uint32_t w, uint32_t mask) {
   constexpr uint32_t s = 0x41C041C0u;
   return make_uint4((w << 3 & mask) ^ s, (w >> 1 & mask) ^ s, (w >> 5 & mask) ^ s, (w >> 9 & mask) ^ s);
+}
+
+// The same pairs as code / 16, exactly (a signed nibble's conversion divides by 16).
+__device__ __forceinline__ uint4 codes8_exact(uint32_t w) {
+  auto two = [&](int j) { return f_to_bf2(__builtin_amdgcn_cvt_off_f32_i4(w >> (4 * j)), __builtin_amdgcn_cvt_off_f32_i4(w >> (4 * j + 16))); };
+  return make_uint4(two(0), two(1), two(2), two(3));
 }
 
 // dword f of lane group g <- dword g of lane group f
@@ -81,7 +90,8 @@ __device__ __forceinline__ float split_piece(const uint4 (&v)[XF32 ? 2 : 1], uin
 
 // A chunk of windows of x's T rows, on its way into LDS: rows of chunk * 256 + 16 bytes (the 16 spread the rows over the
 // banks), plane after plane, in pieces of 8 columns, of which a thread holds up to gq_units.  Columns past n_in are zero.
-// Behind the planes the table of -24 times the sum of x: SUMS rows for a window, of all tokens of the tiles.
+// Behind the planes the table of -24 times the sum of x: SUMS rows for a window, of all tokens of the tiles.  fp32 x: for offsets
+// alone.
 template <bool XF32, int SUMS, int TOKENS>
 struct XPieces {
   static constexpr int N = gq_units(XF32), THREADS = 512, SPAN = N * THREADS;
@@ -311,7 +321,7 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
         auto load_x = [&](int f) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            if (f % PER == 0) starts[f / PER & 1][t] = tab[f / PER * 4 * NT + t * 4];
+            if ((!XF32 || OFF) && f % PER == 0) starts[f / PER & 1][t] = tab[f / PER * 4 * NT + t * 4];
 #pragma unroll
             for (int p = 0; p < P; ++p) {
               const char* at = NT == 1 ? buf + xrow[t] + w * 2 * kWindow + (TR ? f * 64 + g * 16 : g * 64 + f * 16) + p * a.T * stride
@@ -327,7 +337,10 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
           if constexpr (NT > 1) issue_barrier();
           bf16x8_t wf[M];
 #pragma unroll
-          for (int m = 0; m < M; ++m) wf[m] = bf8(codes8(f == 0 ? q[m].x : f == 1 ? q[m].y : f == 2 ? q[m].z : q[m].w, mask));
+          for (int m = 0; m < M; ++m) {
+            const uint32_t w8 = f == 0 ? q[m].x : f == 1 ? q[m].y : f == 2 ? q[m].z : q[m].w;
+            wf[m] = bf8(XF32 ? codes8_exact(w8) : codes8(w8, mask));
+          }
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -347,9 +360,9 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
               for (int m = 0; m < M; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                  acc[t][m][i] += cur.sc[u][m].at(s) * (XF32 ? sum[t][m][i] + starts[s & 1][t][i] : sum[t][m][i]);
+                  acc[t][m][i] += cur.sc[u][m].at(s) * sum[t][m][i];
               if constexpr (OFF) {
-                const f32x4_t sx = starts[s & 1][t] * (-1.f / 24.f);
+                const f32x4_t sx = starts[s & 1][t] * (XF32 ? -1.f / 384.f : -1.f / 24.f);
 #pragma unroll
                 for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -395,6 +408,10 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
       for (int k = 0; k < WK; ++k)
 #pragma unroll
         for (int m = 0; m < M; ++m) v[m] += red[(((r * WK + k) * M + m) * 4 + i) * 64 + l];
+      if constexpr (XF32) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) v[m] *= 16.f;
+      }
       if (a.part) {
 #pragma unroll
         for (int m = 0; m < M; ++m) a.part[(((size_t)blockIdx.y * M + m) * a.T + tok) * a.n_out + o] = v[m];

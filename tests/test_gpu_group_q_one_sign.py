@@ -41,3 +41,19 @@ def test_tokens_of_one_sign(xdt, T, n_in, group):
         h = bound(c.x, *c.w[0])
         ref.check(c.run(), *h, xdt, f"offsets={offsets}")
         ref.check(c.run_gated(0.1, 2, False), *ref.gated(2, False, 0.1, *h, *bound(c.x, *c.w[1])), xdt, f"gated offsets={offsets}")
+
+
+@pytest.mark.parametrize("sign", ["one", "both"])
+@pytest.mark.parametrize("T", [1, 2, 3, 16, 17, 40, 64])
+@pytest.mark.parametrize("n_in,group", [(4096, 128), (2048, 64), (1280, 32), (1152, 96)])
+def test_fp32_tokens_as_a_sum_of_fp32(sign, T, n_in, group):
+    """The norm of the error against that of the result, in U: a group's 3 g additions (three parts of x) are off by U of a
+    partial sum each, independently, a deviation of U / sqrt(3) of it at most; codes do not depend on x, so partial sums
+    grow in the mean square up to the group's own: sqrt(3 g / 3) of that.  The groups' additions in the same way: sqrt(G).
+    Two more for the scales' product and the last rounding.  (Sums that hold 24 times the x beside the codes are 50 U off.)"""
+    c = Case(F32, T, n_in, 2048, group)
+    if sign == "one":
+        c.x = c.x.abs() + 0.5
+    want, _ = ref.product(c.x, *c.w[0])
+    off = float((c.run().double() - want).norm() / want.norm())
+    assert off <= (math.sqrt(group) + math.sqrt(n_in // group) + 2) * ref.U, off / ref.U
