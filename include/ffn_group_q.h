@@ -15,8 +15,9 @@
  *
  * Types: x and y are xdt, FFN_BF16 or FFN_F32; scales and offsets are w->sdt, either of the two.
  * Products and sums are fp32: the codes enter the bf16 matrix products as they are (small integers), x as
- * itself, or with FFN_F32 as a sum of three bf16 parts that hold its 24 bits (parts below 2^-122 are flushed); each
- * group's sum is then scaled.  fp32 results are as exact as a plain fp32 sum's, whatever the tokens' signs.  With FFN_BF16 y and z are rounded once.
+ * itself, or with FFN_F32 as a sum of three bf16 parts that hold its 24 bits (parts below 2^-122 are flushed);
+ * each group's sum is then scaled.  fp32 results are as exact as a plain fp32 sum's, whatever the tokens'
+ * signs.  With FFN_BF16 y and z are rounded once.
  *
  * Layouts: row-major device pointers, 16-byte aligned: x [T][n_in], y [T][n_out], codes
  * [n_out][n_in / 2], scales and offsets [n_out][n_in / group].  group is a multiple of 32 and divides

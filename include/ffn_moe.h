@@ -27,8 +27,9 @@
  * Determinism: results are bit-reproducible (no floating-point atomic adds).
  *
  * Special values: an Inf or NaN of a token stays in that token's y and weights; its experts are then k different ones
- * with no further meaning.  A NaN score counts as the lowest.  An expert's weights reach
- * the tokens that chose it alone.  A NaN gate value behaves as in ffn_gated.h.
+ * with no further meaning.  A NaN score counts as the lowest.  With normalize, chosen scores
+ * that are all below what 64 bits hold (logits more than 700 under 0, or under the largest) give NaN weights.  An
+ * expert's weights reach the tokens that chose it alone.  A NaN gate value behaves as in ffn_gated.h.
  */
 #ifndef FFN_MOE_H
 #define FFN_MOE_H
@@ -62,7 +63,8 @@ size_t ffn_moe_workspace_bytes(ffn_dtype_t wdt, int T, int d, int d_ff, int expe
  * ffn_gated_forward (NULL: the default form).  T at most 256: more tokens than a decode step has are
  * the gated block's, expert by expert.
  * Errors: FFN_ERR_NULL, _SHAPE (T, d, d_ff < 1, T above 256, d or d_ff above 2^20, d_ff d of 2^31 and
- * more, T k d_ff (d_ff rounded up to 32) of 2^29 and more, experts or k outside the bounds above), _DTYPE, _ALIGN, _OPTION (a field of the router or of opt), _WORKSPACE, _HIP. */
+ * more, T k d_ff (d_ff rounded up to 32) of 2^29 and more, experts or k outside the bounds above), _DTYPE, _ALIGN, _OPTION (a
+ * field of the router or of opt), _WORKSPACE, _HIP. */
 int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t* router, const void* x,
                     const void* w_gate, const void* w_up, const void* w_down_t, float t, const ffn_options_t* opt,
                     int32_t* ids, float* weights, void* y, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -172,8 +172,8 @@ struct XCopy {
 // tiles.  U: windows of a wave in a batch; the next batch is on its way during a batch's products.  NSX: scales of a window, 1
 // (groups that are multiples of 128), 2 or 4 (of 64 and 32, a window's scales side by side in whole dwords), or 8: any other
 // group, a scale for every 32 codes.  OFF: there are offsets.  WHOLE: all of a share's x is in LDS at once.
-// 48 fp32 tokens of 4096 -> 14336 twice, groups of 64 with offsets: 52 us, 0.65 PFLOP/s of the three parts' products, the matrix
-// pipes busy for 24% and the vector ALUs for 32%: each step's operands come from LDS behind a barrier, and the codes of a batch
+// 48 fp32 tokens of 4096 -> 14336 twice, groups of 64 with offsets: 55 us, 0.61 PFLOP/s of the three parts' products, the matrix
+// pipes busy for 23% and the vector ALUs for 33%: each step's operands come from LDS behind a barrier, and the codes of a batch
 // are taken apart between its products.
 template <bool XF32, bool SF32, bool GATED, int NSX, bool OFF, int NT, int WK, int U, bool WHOLE>
 __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
@@ -370,7 +370,10 @@ __global__ __launch_bounds__(512, NT == 1 ? 4 : 2) void k_group_q(GqArgs a) {
               }
             }
           }
-          if constexpr (GATED && NS == 4) issue_barrier();  // one f at a time: more of them in registers spill
+          // one f at a time: more of them in registers spill, and with NSX 8, whose scales are 16-bit or 32-bit loads of their own,
+          // gated kernels of one token tile spill all the same, 17 to 48 registers (10752 -> 10688, 8 bf16 tokens, fp32 scales and
+          // offsets: groups of 128 54 us, of 32 63, of 96 223)
+          if constexpr (GATED && NS == 4) issue_barrier();
         }
       }
     };

@@ -1,6 +1,7 @@
 // include/ffn_moe.h: a mixture-of-experts layer for a decode step's tokens.
 //
-// The chosen experts' three matrices are read once (for up to 64 tokens of an expert) and bound it.  Launches:
+// The chosen experts' three matrices bound it: each is read once for every 16, 32 or 64 of its expert's tokens, by the mean number of
+// them (launch_moe).  Launches:
 //   1. k_moe_logits  the router's products in 64 bits, a wave to an expert
 //      k_moe_choose  the choice, a wave to a token; up to 4 tokens' is made by every workgroup of k_moe_hidden instead (a
 //                    launch less)
@@ -23,9 +24,13 @@ namespace ffn {
 namespace {
 
 constexpr int kMoeTokens = 256, kMoeK = 16, kMoeExperts = 512;
-constexpr int kDownGroups = 1024;  // workgroups of k_moe_down, where the neurons go in pieces to come to so many
+// Workgroups of k_moe_down, where the neurons go in pieces to come to so many (bf16: 8 experts of 4096 x 14336, 16 tokens, 458 us with
+// 256, 434 to 440 with 512 to 4096; 64 of 2048 x 1408, 64 tokens, 198 with 256 to 1024, 203 and 208 with 2048 and 4096).
+constexpr int kDownGroups = 1024;
 constexpr int kRouteTokens = 8;  // tokens of a wave that computes logits
-constexpr int kChooseTokens = 4; // tokens that k_moe_hidden chooses for itself: a wave each
+// Tokens that k_moe_hidden chooses for itself, a wave each (64 experts of 2048 x 256 bf16, one token: a launch of its own 24.3 us, so
+// 22.3; four tokens 32.8 and 30.9, of 512 experts 38.2 and 38.1).
+constexpr int kChooseTokens = 4;
 
 struct RouteArgs {
   int T, d, E, k;
@@ -418,6 +423,8 @@ constexpr int down_columns() {
 
 // Four waves take turns at the piece's neurons, 32 at once: a lane has 16 bytes of 8 neurons' rows.  Bound by the weights'
 // bytes, rows of 256 bytes at a time: 939 MB in 149 us (6.3 TB/s), 369 in 59-74, 34 in 9.5 (the calls named at k_moe_hidden).
+// Where rows end inside a chunk (VEC 3 and 0) the narrow loads of a row's end are in every workgroup's loop, and the kernels
+// spill, 58 to 73 registers with one tile of bf16: 52 tokens, 16 experts of 1728 x 6272 239 us, of 1716 312, of 1715 764.
 template <bool F32, int VEC, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   constexpr int E = F32 ? 4 : 8, COLS = down_columns<F32>();
@@ -598,7 +605,8 @@ hipError_t launch_moe(const RouteArgs& r, const MoeArgs& a, hipStream_t st) {
   const bool choose = r.w && a.T <= kChooseTokens;
   if (r.w) {
     // Waves of one token while there are few of them: 8 tokens of a wave save its expert's row 7 times, one after the
-    // other (8 experts, 16 tokens of 4096: 10.9 us, so 4.4).
+    // other (8 experts, 16 tokens of 4096: 10.9 us, so 4.4).  Layers of 64 hidden neurons, bf16, T E = 4096: 64 tokens of 4096 47.2
+    // us, so 42.5, of 1024 22.5 and 21.9; 8192: 52.8 and 51.3, 24.2 and 25.1; 16384: 65.4 and 67.9, 28.5 and 31.5.
     if (a.T * a.E <= 4096) k_moe_logits<F32, VEC, 1><<<dim3(ceil_div(a.E, 4), a.T), 256, 0, st>>>(r);
     else k_moe_logits<F32, VEC, kRouteTokens><<<dim3(ceil_div(a.E, 4), ceil_div(a.T, kRouteTokens)), 256, 0, st>>>(r);
     if (!choose) k_moe_choose<<<a.T, kWave, 0, st>>>(r);

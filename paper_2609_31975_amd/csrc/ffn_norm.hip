@@ -225,7 +225,9 @@ struct NormBack {
 
 // One group of threads takes every groups-th row and keeps its columns' sums over them in registers.  Bound by bytes: 8192 x
 // 8192 bf16 with a gate for each token reads five rows and writes three, 1.07 GB, in 250 us (4.3 TB/s); a row's two means
-// leave its loads waiting for the row before (those of the next row a row early, in two sets of registers, spill).
+// leave its loads waiting for the row before (those of the next row a row early, in two sets of registers, spill).  Rows of more than
+// 8192 take 16 elements to each of 1024 threads, which do not fit: 76 to 155 registers spill inside the loop over the rows (2048 x
+// 12288, gate of each token, forward and backward: bf16 272 us, 1.9 TB/s, fp32 373, 2.7).
 template <bool F32, int TPR, int EPT, bool VEC>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, EPT == 8 ? 4 : 1) void k_norm_bwd(NormBack a) {
   using P = Part<F32, TPR, EPT, VEC>;
