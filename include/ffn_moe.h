@@ -13,8 +13,8 @@
  * expert; a token without any gets zeros; an expert named twice for a token counts twice.
  *
  * Types: wdt is FFN_BF16 or FFN_F32 and is the type of x, y, the router's and the experts' weights alike; bias and
- * `weights` are fp32.  Sums are fp32 (the router's: fp64).  With FFN_BF16, A(.) (*) U(.) is rounded to bf16 where it
- * enters W2's product, as in the gated block, and y once; y sums the experts in fp32.
+ * `weights` are fp32.  Sums are fp32 (the router's: fp64).  With FFN_BF16, A(.) (*) U(.) enters W2's
+ * product in two bf16 parts, which hold 16 of its bits, and y is rounded once; y sums the experts in fp32.
  *
  * Layouts: row-major device pointers, 16-byte aligned: x, y [T][d], w_router [experts][d], w_gate, w_up,
  * w_down_t [experts][d_ff][d], ids int32 and weights fp32 [T][k] (4-byte aligned), bias [experts] (4-byte aligned).

@@ -51,7 +51,8 @@ struct MoeArgs {
   ActForm form;
   const int32_t* ids;
   const float* weights;
-  void* z;      // [T k][ldz]
+  void* z;      // [T k][ldz], with bf16 twice: the values, and behind them what their rounding leaves
+  size_t z_plane;
   float* part;  // [pieces][T k][d]
   void* y;
 };
@@ -284,6 +285,19 @@ __device__ __forceinline__ void exchange8(uint4& a, uint4& b) {
   one(a.w, b.w);
 }
 
+// One value of z: fp32, or with bf16 weights two bf16 parts that hold 16 of its bits, a plane each.  Rounded to one part, z would
+// put as much error into y as y's own rounding does (2.3e-3 of its norm, so 1.65e-3), and the second product, which the weights'
+// bytes bound, has room for both parts: 8 experts of 4096 x 14336, 16 tokens 433 us, so 441; 64 of 2048 x 1408, one token 34.7 and 34.9,
+// 64 tokens 198 and 203, 256 tokens 322 and 336.  An Inf or NaN has no second part.
+template <bool F32>
+__device__ __forceinline__ void put_z(const MoeArgs& a, size_t i, float v) {
+  store_as<F32>(a.z, i, v);
+  if constexpr (!F32) {
+    const float hi = bf_to_f(f_to_bf(v));
+    static_cast<uint16_t*>(a.z)[a.z_plane + i] = f_to_bf(hi - hi == 0.f ? v - hi : 0.f);
+  }
+}
+
 // Four waves share the summed dimension of 16 hidden neurons' two rows.  NT: 16-token tiles at a time.  CHOOSE: the
 // tokens' choice is made here, from the logits.  Bound by the weights' bytes: 8 experts of 4096 x 14336, 16 tokens 1.88 GB in
 // 272 us (6.9 TB/s); 64 of 2048 x 1408, 64 tokens 738 MB in 121 us (6.1); 8 of 64, 2048 x 1024, one token 67 MB in 17 us, of
@@ -409,7 +423,7 @@ __global__ __launch_bounds__(256) void k_moe_hidden(MoeArgs a, RouteArgs route) 
           v += red[w][1][wave][lane];
         }
         // rows up to ldz are zeros for the next product
-        store_as<F32>(a.z, (size_t)list[p] * a.ldz + row, row < a.d_ff ? act_product(a.form, h, v) : 0.f);
+        put_z<F32>(a, (size_t)list[p] * a.ldz + row, row < a.d_ff ? act_product(a.form, h, v) : 0.f);
       }
     }
   }
@@ -424,7 +438,7 @@ constexpr int down_columns() {
 // Four waves take turns at the piece's neurons, 32 at once: a lane has 16 bytes of 8 neurons' rows.  Bound by the weights'
 // bytes, rows of 256 bytes at a time: 939 MB in 149 us (6.3 TB/s), 369 in 59-74, 34 in 9.5 (the calls named at k_moe_hidden).
 // Where rows end inside a chunk (VEC 3 and 0) the narrow loads of a row's end are in every workgroup's loop, and the kernels
-// spill, 58 to 73 registers with one tile of bf16: 52 tokens, 16 experts of 1728 x 6272 239 us, of 1716 312, of 1715 764.
+// spill, 63 to 73 registers with one tile of bf16: 52 tokens, 16 experts of 1728 x 6272 243 us, of 1716 325, of 1715 775.
 template <bool F32, int VEC, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   constexpr int E = F32 ? 4 : 8, COLS = down_columns<F32>();
@@ -438,7 +452,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
   // the piece's neurons: whole steps of 32
   const int steps = a.ldz / 32, s0 = (int)((int64_t)steps * blockIdx.z / a.pieces), s1 = (int)((int64_t)steps * (blockIdx.z + 1) / a.pieces);
   const size_t es = F32 ? 4 : 2;
-  const Buf zb = make_buf(a.z, (uint32_t)a.T * a.k * a.ldz * es);
+  const Buf zb = make_buf(a.z, (uint32_t)(a.T * a.k * a.ldz) * 4u);  // fp32, or two planes of bf16
   const uint32_t vo = col < a.d ? (uint32_t)((g * 8 * (size_t)a.d + col) * es) : kOOB;
   const char* wbase = static_cast<const char*>(a.w[2]) + (size_t)e * a.d_ff * a.d * es;
 
@@ -503,8 +517,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_moe_down(MoeArgs a) {
 #pragma unroll
           for (int c = 0; c < E; ++c) acc[t][c] += sum[c];
         } else {
+          const uint4 z1 = ldb(zb, zi + (uint32_t)a.z_plane * 2u);
 #pragma unroll
-          for (int c = 0; c < E; ++c) acc[t][c] = mfma16(bf8(z0), bf8(b[c]), acc[t][c]);
+          for (int c = 0; c < E; ++c) acc[t][c] = mfma16(bf8(z0), bf8(b[c]), mfma16(bf8(z1), bf8(b[c]), acc[t][c]));
         }
       }
       load(s + 4);
@@ -569,7 +584,7 @@ size_t moe_layout(bool f32, int T, int d, int d_ff, int E, int k, void* base, Mo
   Carver c{static_cast<char*>(base)};
   MoeWs w;
   w.logits = static_cast<double*>(c.take(sizeof(double) * T * E));
-  w.z = c.take((size_t)(f32 ? 4 : 2) * T * k * moe_ldz(d_ff));
+  w.z = c.take(sizeof(float) * T * k * (size_t)moe_ldz(d_ff));
   w.part = static_cast<float*>(c.take(sizeof(float) * moe_part_rows(f32, T, d, d_ff, E, k) * (size_t)d));
   if (out) *out = w;
   return c.off;
@@ -671,7 +686,7 @@ int ffn_moe_forward(ffn_dtype_t wdt, int T, int d, int d_ff, const ffn_router_t*
   const RouteArgs r{T, d, E, k, x, router->w, router->bias, router->sigmoid, router->normalize, router->scale,
                     w.logits, ids, weights};
   const MoeArgs a{T, d, d_ff, E, k, moe_ldz(d_ff), moe_slots(T, E, k), moe_pieces(f32, T, d, d_ff, E, k),
-                  x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, w.part, y};
+                  x, {w_gate, w_up, w_down_t}, form, ids, weights, w.z, (size_t)T * k * moe_ldz(d_ff), w.part, y};
   const bool lines = d % (f32 ? 32 : 64) == 0, chunks = d % (f32 ? 4 : 8) == 0;
   hipError_t e;
   if (f32) e = lines ? launch_moe<true, 2>(r, a, stream) : chunks ? launch_moe<true, 1>(r, a, stream) : launch_moe<true, 3>(r, a, stream);

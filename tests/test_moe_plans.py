@@ -46,7 +46,7 @@ def test_every_plan_fits_its_workspace(tmp_path):
         # what the pieces leave fits, and little room is left: at most as many rows as workgroups fill the card, or a row a place
         assert pieces * T * k <= rows <= 8 * T * k and rows <= T * k + (-(-1024 // columns) - 1) * -(-T * k // E), (c, p)
         assert L.ffn_moe_workspace_bytes(0 if f32 else 1, T, d, d_ff, E, k) == \
-            up(8 * T * E) + up((4 if f32 else 2) * T * k * ldz) + up(4 * rows * d), (c, p)
+            up(8 * T * E) + up(4 * T * k * ldz) + up(4 * rows * d), (c, p)
         cut += pieces > 1
     assert cut > 3000
 
