@@ -19,9 +19,9 @@ GqPlan gq_plan(bool xf32, bool gated, int group, int T, int n_in, int n_out) {
     p.blocks = ceil_div(n_out, 8 / p.wk * 16);
     // Rows for fewer workgroups than the card holds at once (one to a CU with more than one token tile, else two): the
     // windows in shares, which a second launch joins, where that launch (about 5 us) is little beside the rest: eight
-    // rounds of the waves or more, and four to a share.  us for shares never, so, of one round or more: bf16 16384 -> 512, 3 tokens
-    // 13.4, 10.7, 7.3; 28672 -> 2048, one 13.2, 12.1, 11.8; 4096 -> 1024, 20 tokens 20.0, 11.6, 9.9; 14336 -> 1024, 40 61, 16.4, 16.4;
-    // the other way round 14336 -> 4096, 8 16.7, 18.0, 17.9 (fp32 29, 23, 23).
+    // rounds of the waves or more, and four to a share.  us without shares, so, and with one round to a share, bf16: 16384 -> 512, 3
+    // tokens 13.4, 10.7, 7.3; 28672 -> 2048, one token 13.2, 12.1, 11.8; 4096 -> 1024, 20 tokens 20.0, 11.6, 9.9; 14336 -> 1024, 40
+    // tokens 61, 16.4, 16.4; the other way round 14336 -> 4096, 8 tokens 16.7, 18.0, 17.9 (fp32 29, 23, 23).
     const int room = p.nt > 1 ? 256 : 512;
     p.shares = units < 8 ? 1 : std::max(1, std::min({room / p.blocks, units / 4, kGqSharesMost}));
     p.per_share = ceil_div(units, p.shares) * unit;
